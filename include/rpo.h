@@ -260,6 +260,94 @@ int rpo_sample_rows_noalloc(int32_t n_rows, int32_t vocab, const float* d_logits
                             const int64_t* d_seq_ids, int32_t step, int32_t* d_tokens_out, float* d_logprobs_out,
                             void* cuda_stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators on a paged KV cache that the caller owns
+ *
+ * A rollout whose cache is to stay bounded appends a chunk of new tokens and attends to the cache
+ * (rpo_chunk_attention), gathers how much weight every cached key received (rpo_attention_mass)
+ * and drops the keys that received least (rpo_evict_cache).  One layer per call; storage type =
+ * the context's (K, V, queries and outputs); the context's decoder shape and its own KV pool play
+ * no part, so any context of the right type serves.  (The paper has no counterpart: its rollouts
+ * keep every key.)
+ *
+ * The calls enqueue work on the context's stream, allocate nothing, do not synchronise and can be
+ * captured into a CUDA graph; split work goes through workspaces of the context, so calls on one
+ * context (replays of graphs that hold them included) must not overlap on the GPU.
+ *
+ * Device arrays are checked on the device: a length beyond the block table, a chunk offset out of
+ * range, a chunk longer than max_chunk or a slot beyond the mass array is clamped and sets bit 3
+ * of rpo_device_status; a block id outside the pool sets bit 2, nothing is written through it and
+ * it reads as some block of the pool.  Block-table entries of tokens that no row can see are not
+ * used.  Memory behind a sequence's last token, in its last block or elsewhere, may hold anything,
+ * NaN included; keys and values that some row of the same sequence sees must be finite. */
+typedef struct rpo_paged_kv {
+  void* d_k;                     /* [n_kv_heads][n_blocks][16][head_dim], 16-byte aligned               */
+  void* d_v;
+  const int32_t* d_block_table;  /* [n_seqs][table_stride]: block of tokens 16 b .. 16 b + 15           */
+  const int32_t* d_lens;         /* [n_seqs] tokens in the cache, those of the call's chunk included    */
+  int32_t n_blocks, n_seqs, table_stride, n_kv_heads, head_dim;      /* head_dim 64 or 128              */
+} rpo_paged_kv;
+
+/* Row i of a chunk of n tokens sits at position p = len - n + i and sees the keys j <= p of its
+ * sequence, with window > 0 only those with j > p - window or j < sinks. */
+typedef struct rpo_chunk_cfg {
+  float scale;      /* of q . k; > 0                                                              */
+  int32_t window;   /* 0: no window                                                               */
+  int32_t sinks;    /* first tokens that stay visible under a window                              */
+} rpo_chunk_cfg;
+
+/* Attention of a chunk of new tokens per sequence over the paged cache:
+ *   o_i = sum_j exp(scale q_i . k_j - lse_i) v_j,   lse_i = log sum_j exp(scale q_i . k_j)
+ *   d_q              [n_rows][n_q_heads][head_dim], rows q_stride elements apart (16-byte aligned rows)
+ *   d_k_new, d_v_new NULL (the chunk's K and V are in the cache), or [n_rows][n_kv_heads][head_dim],
+ *                    rows kv_new_stride elements apart: written to their pages first.  Pages that are
+ *                    written to must belong to one sequence only
+ *   d_q_offsets      device int32 [n_seqs + 1]: sequence s owns rows [d_q_offsets[s], d_q_offsets[s+1]),
+ *                    at most max_chunk of them, none allowed.  Rows behind the last sequence are left alone
+ *   d_out            [n_rows][n_q_heads][head_dim]; a row that sees no key becomes 0
+ *   d_lse_out        NULL or float [n_rows][n_q_heads]; -inf for a row that sees no key
+ * Decode steps are chunks of one token.  Softmax and sums are float32; 16-bit storage rounds the
+ * unnormalised weights (as the rollout's own attention does) and the output.
+ * Errors: RPO_ERR_INVALID_ARG (NULL, misaligned, scale <= 0, negative sizes), RPO_ERR_SHAPE (head_dim,
+ * n_q_heads not a multiple of n_kv_heads or more than 64 query heads per KV head), RPO_ERR_LIMIT (more
+ * than 4096 sequences, 2^30 rows x heads or 2^31 tokens x KV heads in the pool). */
+int rpo_chunk_attention(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_chunk,
+                        const void* d_q, int64_t q_stride, const void* d_k_new, const void* d_v_new,
+                        int64_t kv_new_stride, const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg, void* d_out,
+                        float* d_lse_out);
+
+/* Attention weight every cached key received from the chunk's rows, per KV head:
+ *   mass_out[s][h][j] = mass_in[s][h][j] + sum over rows i of sequence s and the query heads of KV head h
+ *                       of exp(scale q_i . k_j - lse_i)
+ * for j < len; entries behind are left as they are.  The chunk's K must be in the cache, d_lse as
+ * rpo_chunk_attention wrote it.  d_mass_in NULL: zeros; d_mass_out may be d_mass_in (accumulation
+ * over steps).  Both float [n_seqs][n_kv_heads][mass_stride].  Sums are float32 in a fixed order.
+ * Errors as in rpo_chunk_attention. */
+int rpo_attention_mass(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_chunk,
+                       const void* d_q, int64_t q_stride, const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg,
+                       const float* d_lse, const float* d_mass_in, float* d_mass_out, int32_t mass_stride);
+
+/* Eviction by accumulated weight: every (sequence, KV head) with more than `budget` tokens keeps
+ * exactly budget of its slots -- tokens at positions < sinks and the `recent` newest positions first,
+ * then the heaviest; equal weights go to the lower slot, a NaN counts least.  (Where more than budget
+ * slots are protected, the heaviest of those stay.)
+ *   d_mass       float [n_seqs][n_kv_heads][mass_stride]
+ *   d_positions  int32, same shape: position of the token in every slot (attention after an eviction
+ *                no longer has slot = position; the caller fills in the slots it appends)
+ *   d_lens_out   [n_seqs] min(len, budget); may be kv->d_lens
+ *   d_src_out    int32 [n_seqs][n_kv_heads][budget]: the slot each kept slot's row came from; -1 behind
+ *                the last.  Kept slots below budget stay; the i-th kept slot at or above it moves to the
+ *                i-th free one below (K, V, weight and position; the order of cached keys is free)
+ *   d_mass_out, d_positions_out  [n_seqs][n_kv_heads][out_stride >= budget], written below lens_out only;
+ *                may be d_mass / d_positions themselves (then out_stride = mass_stride), no other overlap
+ * The pages of a sequence must belong to it alone.  A causal chunk may follow at once; a window may
+ * not (slots are no longer in order).
+ * Errors: RPO_ERR_INVALID_ARG (also sinks + recent > budget), RPO_ERR_SHAPE, RPO_ERR_LIMIT
+ * (mass_stride > 2^19, n_seqs * n_kv_heads > 65535). */
+int rpo_evict_cache(rpo_ctx* ctx, const rpo_paged_kv* kv, const float* d_mass, const int32_t* d_positions,
+                    int32_t mass_stride, int32_t budget, int32_t sinks, int32_t recent, int32_t* d_lens_out,
+                    int32_t* d_src_out, float* d_mass_out, int32_t* d_positions_out, int32_t out_stride);
+
 /* Dense product C[M,N] = A[M,K] * W[N,K]^T through the same GEMM kernel the layers use
  * (storage type of the context; C is float32).  For kernel-level parity tests.
  * impl: 0 = the kernel the context would choose, 1 = plain CUDA-core kernel,
@@ -278,7 +366,8 @@ int rpo_gemm_bench(rpo_ctx* ctx, int32_t M, int32_t N, int32_t K, const void* d_
 
 /* Device status word, sticky until read: 0 = clean; bit 0 = a bounded wait expired
  * (TMA / MMA pipeline), bit 1 = token id out of range (clamped), bit 2 = block-table
- * index out of range (access skipped).  Synchronises the stream; *out receives the word
+ * index out of range (access skipped), bit 3 = a length or offset given to an operator on a
+ * caller-owned cache out of range (clamped).  Synchronises the stream; *out receives the word
  * and the word is cleared.  Returns RPO_ERR_DEVICE_TIMEOUT when bit 0 was set (the results of
  * the work enqueued since the last read are not to be trusted; the context stays usable),
  * else RPO_OK.  The asynchronous entry points (prefill, decode, token log-probs) cannot

@@ -14,7 +14,7 @@ _LIB = None
 EXPORTED_SYMBOLS = [
     "rpo_strerror", "rpo_shape_preset", "rpo_create", "rpo_destroy", "rpo_init_weights", "rpo_read_tensor",
     "rpo_write_tensor", "rpo_prefill_prefix", "rpo_decode_suffix", "rpo_decode_wave", "rpo_token_logprobs", "rpo_release_groups",
-    "rpo_policy_objective", "rpo_rollout_host", "rpo_sample_rows", "rpo_sample_rows_noalloc", "rpo_gemm", "rpo_gemm_bench", "rpo_device_status", "rpo_debug_tap", "rpo_counters", "rpo_set_option", "rpo_profile_read",
+    "rpo_policy_objective", "rpo_rollout_host", "rpo_sample_rows", "rpo_sample_rows_noalloc", "rpo_gemm", "rpo_gemm_bench", "rpo_chunk_attention", "rpo_attention_mass", "rpo_evict_cache", "rpo_device_status", "rpo_debug_tap", "rpo_counters", "rpo_set_option", "rpo_profile_read",
 ]
 
 
@@ -55,6 +55,37 @@ class Group(C.Structure):
     _fields_ = [("group_id", C.c_int32), ("prefix_len", C.c_int32), ("slot", C.c_int32), ("n_blocks", C.c_int32)]
 
 
+class _PagedKVStruct(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_block_table", C.c_void_p), ("d_lens", C.c_void_p), ("n_blocks", C.c_int32),
+                ("n_seqs", C.c_int32), ("table_stride", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class _ChunkCfg(C.Structure):
+    _fields_ = [("scale", C.c_float), ("window", C.c_int32), ("sinks", C.c_int32)]
+
+
+class PagedKV:
+    """rpo_paged_kv: one layer's paged K/V cache in tensors of the caller.
+
+    d_k, d_v [n_kv_heads, n_blocks, 16, head_dim] (float32 or bfloat16), d_block_table int32 [n_seqs, table_stride],
+    d_lens int32 [n_seqs].  Keeps references to the tensors; build it once and reuse it."""
+
+    def __init__(self, d_k, d_v, d_block_table, d_lens):
+        if d_k.dim() != 4 or d_k.shape[2] != 16 or d_v.shape != d_k.shape or d_v.dtype != d_k.dtype:
+            raise ValueError("d_k and d_v must be [n_kv_heads, n_blocks, 16, head_dim] of one type")
+        _expect(d_block_table, "d_block_table", "int32", (d_lens.shape[0], d_block_table.shape[-1]))
+        _expect(d_lens, "d_lens", "int32", (d_block_table.shape[0],))
+        self.d_k, self.d_v, self.d_block_table, self.d_lens = d_k, d_v, d_block_table, d_lens
+        hkv, n_blocks, _, dh = d_k.shape
+        self.struct = _PagedKVStruct(_ptr(d_k), _ptr(d_v), _ptr(d_block_table), _ptr(d_lens), n_blocks, d_block_table.shape[0],
+                                     d_block_table.shape[1], hkv, dh)
+        self.ref = C.byref(self.struct)
+
+    @property
+    def dtype(self):
+        return self.d_k.dtype
+
+
 def load_library(path=None):
     """Load librpo.so (building it first if it is missing) and declare the prototypes."""
     global _LIB
@@ -84,6 +115,10 @@ def load_library(path=None):
     lib.rpo_sample_rows_noalloc.argtypes = [i32, i32, vp, C.POINTER(Sampler), vp, i32, vp, vp, vp]
     lib.rpo_gemm.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp]
     lib.rpo_gemm_bench.argtypes = [vp, i32, i32, i32, vp, C.POINTER(vp), i32, i32, C.POINTER(f32)]
+    pkv, ccfg = C.POINTER(_PagedKVStruct), C.POINTER(_ChunkCfg)
+    lib.rpo_chunk_attention.argtypes = [vp, pkv, i32, i32, i32, vp, i64, vp, vp, i64, vp, ccfg, vp, vp]
+    lib.rpo_attention_mass.argtypes = [vp, pkv, i32, i32, i32, vp, i64, vp, ccfg, vp, vp, vp, i32]
+    lib.rpo_evict_cache.argtypes = [vp, pkv, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, i32]
     lib.rpo_device_status.argtypes = [vp, C.POINTER(i32)]
     lib.rpo_debug_tap.argtypes = [vp, vp, i64, C.POINTER(i64)]
     lib.rpo_counters.argtypes = [vp, C.POINTER(i64), C.POINTER(i64)]
@@ -126,6 +161,21 @@ def _ptr(t):
         return t.ctypes.data
     assert t.is_contiguous()
     return t.data_ptr()
+
+
+def _expect(t, name, dtype, shape):
+    """Refuse a tensor of another type, shape or layout than a call takes."""
+    if str(t.dtype) != "torch." + dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _head_rows(t, name, dtype, heads, dh, n_rows=None):
+    """Elements between the rows of a [rows, heads, head_dim] view whose rows are contiguous (a slice of a fused projection is)."""
+    if t.dim() != 3 or t.dtype != dtype or t.shape[1:] != (heads, dh) or (n_rows is not None and t.shape[0] != n_rows):
+        raise ValueError(f"{name} must be {dtype} [{'rows' if n_rows is None else n_rows}, {heads}, {dh}], got {t.dtype} {tuple(t.shape)}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dh):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else heads * dh
 
 
 def _check(rc, what):
@@ -268,6 +318,72 @@ class Context:
         _check(self.lib.rpo_gemm_bench(self.handle, M, N, K, _ptr(d_A), ptrs, len(d_W_list), int(iters), C.byref(ms)),
                "rpo_gemm_bench")
         return ms.value
+
+    def _paged_dtype(self, kv):
+        if (str(kv.dtype) == "torch.bfloat16") != (self.shape.dtype == 1) or str(kv.dtype) not in ("torch.bfloat16", "torch.float32"):
+            raise ValueError(f"a cache of {kv.dtype} needs a context of that storage type")
+        return kv.dtype
+
+    def _chunk_cfg(self, kv, scale, window, sinks):
+        return _ChunkCfg(kv.struct.head_dim ** -0.5 if scale is None else scale, window, sinks)
+
+    def chunk_attention(self, d_q, kv, d_q_offsets, max_chunk, d_out, d_lse_out=None, d_k_new=None, d_v_new=None, scale=None, window=0, sinks=0):
+        """rpo_chunk_attention: d_q [rows, n_q_heads, head_dim] (rows may be strided), kv a PagedKV, d_out contiguous, d_lse_out
+        float32 [rows, n_q_heads].  scale defaults to head_dim ** -0.5."""
+        dt, st = self._paged_dtype(kv), kv.struct
+        n, hq = d_q.shape[0], d_q.shape[1]
+        q_stride = _head_rows(d_q, "d_q", dt, hq, st.head_dim)
+        new_stride = 0
+        if (d_k_new is None) != (d_v_new is None):
+            raise ValueError("d_k_new and d_v_new go together")
+        if d_k_new is not None:
+            new_stride = _head_rows(d_k_new, "d_k_new", dt, st.n_kv_heads, st.head_dim, n)
+            if _head_rows(d_v_new, "d_v_new", dt, st.n_kv_heads, st.head_dim, n) != new_stride:
+                raise ValueError("d_k_new and d_v_new must have the same row stride")
+        _expect(d_q_offsets, "d_q_offsets", "int32", (st.n_seqs + 1,))
+        if d_out.dtype != dt or d_out.shape != d_q.shape or not d_out.is_contiguous():
+            raise ValueError("d_out must be contiguous, of d_q's type and shape")
+        if d_lse_out is not None:
+            _expect(d_lse_out, "d_lse_out", "float32", (n, hq))
+        cfg = self._chunk_cfg(kv, scale, window, sinks)
+        _check(self.lib.rpo_chunk_attention(self.handle, kv.ref, n, hq, max_chunk, d_q.data_ptr(), q_stride,
+                                            None if d_k_new is None else d_k_new.data_ptr(), None if d_v_new is None else d_v_new.data_ptr(),
+                                            new_stride, d_q_offsets.data_ptr(), C.byref(cfg), d_out.data_ptr(),
+                                            None if d_lse_out is None else d_lse_out.data_ptr()), "rpo_chunk_attention")
+
+    def attention_mass(self, d_q, kv, d_q_offsets, max_chunk, d_lse, d_mass_out, d_mass_in=None, scale=None, window=0, sinks=0):
+        """rpo_attention_mass: d_lse float32 [rows, n_q_heads] of chunk_attention, d_mass_out (and d_mass_in, which may be the same
+        tensor) float32 [n_seqs, n_kv_heads, slots]."""
+        dt, st = self._paged_dtype(kv), kv.struct
+        n, hq = d_q.shape[0], d_q.shape[1]
+        q_stride = _head_rows(d_q, "d_q", dt, hq, st.head_dim)
+        _expect(d_q_offsets, "d_q_offsets", "int32", (st.n_seqs + 1,))
+        _expect(d_lse, "d_lse", "float32", (n, hq))
+        slots = d_mass_out.shape[-1]
+        _expect(d_mass_out, "d_mass_out", "float32", (st.n_seqs, st.n_kv_heads, slots))
+        if d_mass_in is not None:
+            _expect(d_mass_in, "d_mass_in", "float32", (st.n_seqs, st.n_kv_heads, slots))
+        cfg = self._chunk_cfg(kv, scale, window, sinks)
+        _check(self.lib.rpo_attention_mass(self.handle, kv.ref, n, hq, max_chunk, d_q.data_ptr(), q_stride, d_q_offsets.data_ptr(), C.byref(cfg),
+                                           d_lse.data_ptr(), None if d_mass_in is None else d_mass_in.data_ptr(), d_mass_out.data_ptr(), slots),
+               "rpo_attention_mass")
+
+    def evict_cache(self, kv, d_mass, d_positions, budget, d_lens_out, d_src_out, d_mass_out, d_positions_out, sinks=0, recent=0):
+        """rpo_evict_cache: d_mass float32 and d_positions int32 [n_seqs, n_kv_heads, slots], d_src_out int32 [n_seqs, n_kv_heads,
+        budget], d_mass_out / d_positions_out of at least budget slots (or d_mass / d_positions themselves), d_lens_out int32
+        [n_seqs] (or the cache's own d_lens)."""
+        self._paged_dtype(kv)
+        n, h = kv.struct.n_seqs, kv.struct.n_kv_heads
+        slots, out_slots = d_mass.shape[-1], d_mass_out.shape[-1]
+        _expect(d_mass, "d_mass", "float32", (n, h, slots))
+        _expect(d_positions, "d_positions", "int32", (n, h, slots))
+        _expect(d_lens_out, "d_lens_out", "int32", (n,))
+        _expect(d_src_out, "d_src_out", "int32", (n, h, budget))
+        _expect(d_mass_out, "d_mass_out", "float32", (n, h, out_slots))
+        _expect(d_positions_out, "d_positions_out", "int32", (n, h, out_slots))
+        _check(self.lib.rpo_evict_cache(self.handle, kv.ref, d_mass.data_ptr(), d_positions.data_ptr(), slots, budget, sinks, recent,
+                                        d_lens_out.data_ptr(), d_src_out.data_ptr(), d_mass_out.data_ptr(), d_positions_out.data_ptr(), out_slots),
+               "rpo_evict_cache")
 
     def device_status(self, raise_on_timeout=True):
         """The device status word (cleared by the read).  An expired device-side wait (bit 0) raises

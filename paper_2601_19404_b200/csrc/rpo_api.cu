@@ -15,11 +15,14 @@
 #include "attn_tc5.cuh"
 #include "attn_dec5.cuh"
 #include "attn_pre5.cuh"
+#include "cache_evict.cuh"
 #include "context.h"
 #include "gemm_tc.cuh"
 #include "gemm_tc2.cuh"
 #include "kernels.cuh"
 #include "objective.cuh"
+#include "paged_attn.cuh"
+#include "paged_mass.cuh"
 #include "ref_kernels.cuh"
 #include "sampler.cuh"
 
@@ -1447,6 +1450,8 @@ extern "C" int rpo_gemm_bench(rpo_ctx* c, int32_t M, int32_t N, int32_t K, const
   *h_ms_out = ms / iters;
   return RPO_OK;
 }
+
+#include "paged_api.cuh"
 
 // Reads and clears the device status word (synchronises the stream).  After an expired wait the
 // arrival counters of the split-K launches may be left half-counted: they are cleared too.
