@@ -68,6 +68,11 @@ struct Workspace {
   int32_t* step_ctr = nullptr;   // device counter of the decode step being computed
   int64_t* seq_ids = nullptr;
   int R = 0, HR = 0;
+  // operators on a caller-owned cache (paged_*.cuh): parts of items that several CTAs share, the list of items
+  float* op_part_o = nullptr;
+  void* op_part_ml = nullptr;     // float2
+  void* op_rec = nullptr;         // SplitRec per CTA
+  void* op_items = nullptr;       // ChunkItem[OP_MAX_ITEMS], then one ChunkPlan
 };
 
 }  // namespace rpo

@@ -33,7 +33,9 @@ static int check_chunk(const rpo_ctx* c, const rpo_paged_kv* kv, int n_rows, int
     return RPO_ERR_INVALID_ARG;
   if (hq % kv->n_kv_heads || hq / kv->n_kv_heads > OP_MAX_REP) return RPO_ERR_SHAPE;
   if (n_rows > 1 && q_stride < (int64_t)hq * kv->head_dim) return RPO_ERR_INVALID_ARG;
-  if (kv->n_seqs > OP_MAX_SEQS || (int64_t)n_rows * hq >= ((int64_t)1 << 30)) return RPO_ERR_LIMIT;
+  if (kv->n_seqs > OP_MAX_SEQS || (int64_t)n_rows * hq >= ((int64_t)1 << 30) ||
+      (int64_t)kv->n_seqs * kv->table_stride * kv->n_kv_heads >= ((int64_t)1 << 31) - (1 << 20))
+    return RPO_ERR_LIMIT;
   return RPO_OK;
 }
 
@@ -52,6 +54,76 @@ static ChunkArgs chunk_args(int n_rows, int hq, int max_chunk, const int32_t* of
   return a;
 }
 
+static SplitWs split_ws(rpo_ctx* c, int rows_cap) {
+  SplitWs w;
+  w.o = c->ws.op_part_o; w.ml = (float2*)c->ws.op_part_ml; w.rec = (SplitRec*)c->ws.op_rec; w.rows_cap = rows_cap;
+  return w;
+}
+
+// Few rows per sequence (decode steps): one CTA pair per SM over an equal share of all pages.
+template <int DH, int MT>
+static int chunk_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, float scale, bf16* out, float* lse) {
+  using Cfg = StepCfg<DH, MT>;
+  static bool attr_done[64] = {};
+  if (tc_first_use_on_device(c, attr_done))
+    CUDA_TRY(cudaFuncSetAttribute(paged_step_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4));
+  const int grid = 2 * c->sm_count;
+  StepArgs s;
+  s.kv = view; s.c = a; s.q = q; s.q_stride = q_stride; s.scale_log2 = scale * 1.4426950408889634f;
+  s.o.out = out; s.o.lse = lse; s.o.hq = a.hq; s.o.rep = a.hq / view.hkv; s.ws = split_ws(c, Cfg::ROWS); s.min_share = 4;
+  LAUNCH_OP(c, (paged_step_kernel<DH, MT>), grid, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, s);
+  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(grid, Cfg::ROWS / 4), 128, 0, s.ws, s.o);
+  return RPO_OK;
+}
+
+// Tensor map over rows of head_dim 16-bit values in 128-byte swizzled boxes: 2 or 3 dimensions.
+static int op_map(rpo_ctx* c, CUtensorMap* m, const void* ptr, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+  TcState* s = (TcState*)c->tc_state;
+  if (!s || !s->encode) return RPO_ERR_CUDA;
+  const cuuint32_t ones[3] = {1, 1, 1};
+  return s->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(ptr), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? RPO_OK : RPO_ERR_CUDA;
+}
+// Pages of K or V: one box is 16 tokens x 64 dims.
+static int op_map_pages(rpo_ctx* c, CUtensorMap* m, const PagedView<bf16>& v, const bf16* base, int dh) {
+  const cuuint64_t dims[2] = {(cuuint64_t)dh, (cuuint64_t)v.hkv * v.n_blocks * KV_BLOCK}, strides[1] = {(cuuint64_t)dh * 2};
+  const cuuint32_t box[2] = {64, KV_BLOCK};
+  return op_map(c, m, base, 2, dims, strides, box);
+}
+// Queries: one box is `tok` tokens x the rep heads of a KV head x 64 dims.
+static int op_map_rows(rpo_ctx* c, CUtensorMap* m, const bf16* q, int64_t q_stride, int n_rows, int hq, int dh, int rep, int tok) {
+  const cuuint64_t dims[3] = {(cuuint64_t)dh, (cuuint64_t)hq, (cuuint64_t)n_rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)dh * 2, (cuuint64_t)(n_rows > 1 ? q_stride : (int64_t)hq * dh) * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)rep, (cuuint32_t)tok};
+  return op_map(c, m, q, 3, dims, strides, box);
+}
+
+// Many rows per sequence: tensor-core tiles of 2 x (tokens x heads of a KV head <= 128) rows against 128 keys.
+template <int DH>
+static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, float scale, bf16* out, float* lse) {
+  using Cfg = ChunkCfg<DH>;
+  static bool attr_done[64] = {};
+  if (tc_first_use_on_device(c, attr_done))
+    CUDA_TRY(cudaFuncSetAttribute(paged_chunk_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+  ChunkTcArgs t;
+  t.kv = view; t.c = a; t.scale_log2 = scale * 1.4426950408889634f;
+  t.o.out = out; t.o.lse = lse; t.o.hq = a.hq; t.o.rep = a.hq / view.hkv; t.ws = split_ws(c, OP_PART_ROWS);
+  t.tq = CH_BM / t.o.rep;
+  if ((int64_t)a.n_rows / (2 * t.tq) + view.n_seqs > OP_MAX_ITEMS) return RPO_ERR_LIMIT;
+  ChunkItem* items = (ChunkItem*)c->ws.op_items;
+  ChunkPlan* plan = (ChunkPlan*)(items + OP_MAX_ITEMS);
+  t.items = items; t.plan = plan;
+  CUtensorMap qm, km, vm;
+  RPO_TRY(op_map_rows(c, &qm, q, q_stride, a.n_rows, a.hq, DH, t.o.rep, t.tq));
+  RPO_TRY(op_map_pages(c, &km, view, view.k, DH));
+  RPO_TRY(op_map_pages(c, &vm, view, view.v, DH));
+  LAUNCH_OP(c, (chunk_plan_kernel<bf16, CH_BN / KV_BLOCK>), 1, 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4, items, plan);
+  LAUNCH_OP(c, (paged_chunk_kernel<DH>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
+  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, 8), 128, 0, t.ws, t.o);
+  return RPO_OK;
+}
+
 template <typename T, int DH>
 static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs& a, const void* q, int64_t q_stride, const void* k_new,
                              const void* v_new, int64_t new_stride, float scale, void* out, float* lse) {
@@ -59,6 +131,11 @@ static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs
   if (k_new) {
     const int64_t n = (int64_t)a.n_rows * view.hkv * 2 * (DH * sizeof(T) / 16);
     LAUNCH_OP(c, (paged_append_kernel<T, DH>), grid_for(n, 256), 256, 0, view, a, (const T*)k_new, (const T*)v_new, new_stride);
+  }
+  if constexpr (std::is_same<T, bf16>::value) {
+    if (a.max_chunk * (a.hq / kv->n_kv_heads) <= 16) return chunk_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
+    if (a.max_chunk * (a.hq / kv->n_kv_heads) <= 32) return chunk_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
+    return chunk_tiles<DH>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
   }
   LAUNCH_OP(c, (paged_attn_simple_kernel<T, DH>), ceil_div((int64_t)a.n_rows * a.hq, 4), 128, 0, view, a, (const T*)q, q_stride, scale, (T*)out, lse);
   return RPO_OK;

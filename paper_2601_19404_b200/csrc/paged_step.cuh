@@ -1,0 +1,345 @@
+// Attention of few rows per sequence over a caller-owned paged cache (16-bit storage): decode steps, and chunks whose
+// rows x query heads of a KV head fit MT 16-row tensor-core tiles.
+//
+// Bound by HBM: K and V of every visible page are read once per (sequence, KV head), all query heads of the group at
+// once.  All pages of all (sequence, KV head) items form one list; every CTA takes an equal piece of it, whatever the
+// lengths are, found on the device from the lengths alone.  A CTA's four warps walk the pages of their piece
+// independently (warp w takes every fourth page; no barrier in the loop), each with its own ring of pages filled by
+// 16-byte asynchronous copies; scores and P V run on mma.sync m16n8k16 with the online softmax in registers.  The
+// warps' results are joined through shared memory at the end of an item; an item that runs over several CTAs leaves
+// unnormalised parts, joined in piece order by split_merge_kernel.
+#pragma once
+#include "attn_tc.cuh"
+#include "paged_kv.cuh"
+
+namespace rpo {
+
+// ---- items that are worked on in pieces ---------------------------------------------------------------------------
+// CTA b's first and last pieces may belong to items that others work on too: slots 2 b and 2 b + 1.  An item's pieces
+// lie in slot 2 b + 1 of the CTA b it begins in and in slot 2 c of every following CTA c.  CTA b records the item that
+// begins in it and goes on behind it (n_parts 0: there is none).
+struct SplitRec { int row0, head0, rows, n_parts; };       // rows: packed (token, head of the group), token-major
+
+struct SplitWs {
+  float* o;            // [slot][rows_cap][head_dim], unnormalised
+  float2* ml;          // [slot][rows_cap]: running maximum (log2 domain) and sum
+  SplitRec* rec;       // [CTA]
+  int rows_cap;
+};
+
+template <typename T>
+struct AttnOut { T* out; float* lse; int hq, rep; };
+
+constexpr float LN2_F = 0.69314718055994531f;
+
+// One warp per row of an item: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p over the item's pieces, in order.
+template <typename T, int DH>
+__global__ void __launch_bounds__(128) split_merge_kernel(SplitWs ws, AttnOut<T> a) {
+  constexpr int DPL = DH / 32;
+  const SplitRec rec = ws.rec[blockIdx.x];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.x;
+  if (rec.n_parts == 0) return;
+  for (int r = blockIdx.y * 4 + warp; r < rec.rows; r += gridDim.y * 4) {
+    auto slot = [&](int p) -> int64_t { return (int64_t)(p == 0 ? 2 * b + 1 : 2 * (b + p)) * ws.rows_cap + r; };
+    float m = -INFINITY;
+    for (int p = lane; p < rec.n_parts; p += 32) m = fmaxf(m, ws.ml[slot(p)].x);
+    m = warp_max(m);
+    const float mu = m == -INFINITY ? 0.f : m;
+    float l = 0.f, acc[DPL];
+  #pragma unroll
+    for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
+    for (int p0 = 0; p0 < rec.n_parts; p0 += 32) {
+      const int mine = p0 + lane;
+      float w = 0.f, lp = 0.f;
+      if (mine < rec.n_parts) { const float2 ml = ws.ml[slot(mine)]; w = fa::ex2(ml.x - mu); lp = w * ml.y; }
+      const int n = min(32, rec.n_parts - p0);
+  #pragma unroll 4
+      for (int p = 0; p < n; ++p) {
+        const float wp = __shfl_sync(0xffffffffu, w, p);
+        const float* o = ws.o + slot(p0 + p) * DH + lane * DPL;
+        l += __shfl_sync(0xffffffffu, lp, p);
+        if (DPL == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(o);
+          acc[0] = fmaf(wp, x.x, acc[0]); acc[1] = fmaf(wp, x.y, acc[1]); acc[DPL - 2] = fmaf(wp, x.z, acc[DPL - 2]); acc[DPL - 1] = fmaf(wp, x.w, acc[DPL - 1]);
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(o);
+          acc[0] = fmaf(wp, x.x, acc[0]); acc[1] = fmaf(wp, x.y, acc[1]);
+        }
+      }
+    }
+    const int64_t dst = (int64_t)(rec.row0 + r / a.rep) * a.hq + rec.head0 + r % a.rep;
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+  #pragma unroll
+    for (int i = 0; i < DPL; ++i) a.out[dst * DH + lane * DPL + i] = from_f32<T>(acc[i] * inv);
+    if (lane == 0 && a.lse) a.lse[dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
+  }
+}
+
+// ---- the keys a run of rows can see -------------------------------------------------------------------------------
+// Positions [p0, p1] (p0 may be negative: rows before the first token).  Pages [0, n_first) hold the sinks (all pages
+// when there is no window or it reaches them), pages [lo_page, end_page) the window; keys below `lo` that are no sinks
+// are seen by none of the rows.
+struct KeyPages {
+  int n_first, lo_page, end_page, lo;
+  __device__ __forceinline__ int count() const { return n_first + end_page - lo_page; }
+  __device__ __forceinline__ int page(int i) const { return i < n_first ? i : lo_page + i - n_first; }
+};
+
+__device__ __forceinline__ KeyPages key_pages(const ChunkArgs& c, int p0, int p1) {
+  KeyPages k;
+  const int n = max(p1 + 1, 0);
+  k.end_page = (n + KV_BLOCK - 1) / KV_BLOCK;
+  k.lo = c.window > 0 ? max(0, p0 - c.window + 1) : 0;
+  const int sinks = min(c.sinks, n);
+  k.n_first = (sinks + KV_BLOCK - 1) / KV_BLOCK;
+  k.lo_page = k.lo / KV_BLOCK;
+  if (c.window <= 0 || k.lo_page <= k.n_first) { k.n_first = 0; k.lo_page = 0; if (k.lo <= sinks || c.window <= 0) k.lo = 0; }
+  return k;
+}
+
+template <int DH, int MT>
+struct StepCfg {
+  static constexpr int WARPS = 4;
+  static constexpr int PAGE_BYTES = KV_BLOCK * DH * 2;                 // of K or of V
+  static constexpr int STAGES = 3;
+  static constexpr int RING = WARPS * STAGES * 2 * PAGE_BYTES;
+  static constexpr int ROWS = 16 * MT;
+  static constexpr int XO = DH + 4;                                    // floats per row of a warp's result in shared memory
+  static constexpr int XCH = WARPS * ROWS * (XO + 2) * 4;
+  static constexpr int SMEM = (RING > XCH ? RING : XCH);               // + (n_seqs + 1) ints
+};
+
+struct StepArgs {
+  PagedView<bf16> kv; ChunkArgs c;
+  const bf16* q; int64_t q_stride; float scale_log2;
+  AttnOut<bf16> o; SplitWs ws;
+  int min_share;
+};
+
+template <int DH, int MT>
+__global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
+  using Cfg = StepCfg<DH, MT>;
+  constexpr int ROWS = Cfg::ROWS, STAGES = Cfg::STAGES, PB = Cfg::PAGE_BYTES, KS = DH / 16, NT = DH / 8, CPR = DH / 8;
+  extern __shared__ __align__(128) uint8_t st_smem[];
+  int* s_pref = reinterpret_cast<int*>(st_smem + Cfg::SMEM);          // pages of all items of the sequences before s
+  __shared__ int s_scan[4];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, tq = lane & 3;
+  const int n_seqs = a.kv.n_seqs, hkv = a.kv.hkv, rep = a.o.rep;
+
+  // ---- the list: pages per sequence, summed up (thread t: `per` consecutive sequences)
+  const int per = (n_seqs + 127) / 128;
+  int sum = 0;
+  for (int i = 0; i < per; ++i) {
+    const int s = tid * per + i;
+    if (s >= n_seqs) break;
+    const ChunkSpan sp = chunk_span(a.kv, a.c, s);
+    const int n = sp.rows > 0 ? max(1, key_pages(a.c, sp.len - sp.rows, sp.len - 1).count()) * hkv : 0;
+    s_pref[s] = n;
+    sum += n;
+  }
+  int incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int n = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += n; }
+  if (lane == 31) s_scan[warp] = incl;
+  __syncthreads();
+  int run = incl - sum;
+  for (int w = 0; w < warp; ++w) run += s_scan[w];
+  const int total = s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3];
+  for (int i = 0; i < per; ++i) {
+    const int s = tid * per + i;
+    if (s >= n_seqs) break;
+    const int n = s_pref[s];
+    s_pref[s] = run;
+    run += n;
+  }
+  __syncthreads();
+  const int share = max(a.min_share, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+  const int f_end = (int)min((int64_t)total, (int64_t)(blockIdx.x + 1) * share);
+  int f = (int)min((int64_t)total, (int64_t)blockIdx.x * share);
+  if (tid == 0) a.ws.rec[blockIdx.x] = SplitRec{0, 0, 0, 0};
+
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(st_smem) + warp * (STAGES * 2 * PB);
+  float* x_o = reinterpret_cast<float*>(st_smem);                      // results of the warps (the ring is idle then)
+  float2* x_ml = reinterpret_cast<float2*>(st_smem + Cfg::WARPS * ROWS * Cfg::XO * 4);
+  auto sw = [](int row, int chunk) -> uint32_t { return (uint32_t)(row * (DH * 2) + ((chunk ^ (row & 7)) << 4)); };
+
+  while (f < f_end) {
+    int lo = 0, hi = n_seqs - 1;                                       // last sequence that begins at or before f (and is not empty)
+    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (s_pref[mid] <= f) lo = mid; else hi = mid - 1; }
+    const int s = lo;
+    const ChunkSpan sp = chunk_span(a.kv, a.c, s);
+    const int R = sp.rows * rep, p0 = sp.len - sp.rows, p1 = sp.len - 1;
+    const KeyPages kp = key_pages(a.c, p0, p1);
+    const int n_pages = max(1, kp.count()), in_seq = f - s_pref[s], h = in_seq / n_pages, i0 = in_seq % n_pages;
+    const int i1 = min(n_pages, i0 + (f_end - f)), item0 = f - i0;     // my pages of the item, its place in the list
+    const bf16* kb = a.kv.k + h * a.kv.head_stride;
+    const bf16* vb = a.kv.v + h * a.kv.head_stride;
+    const int32_t* tbl = a.kv.table + (int64_t)s * a.kv.table_stride;
+
+    // ---- queries as A fragments: rows g, g + 8 of every 16
+    uint32_t qf[MT][KS][4];
+    int prow[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        const int r = mt * 16 + hh * 8 + g;
+        const bool v = r < R;
+        prow[mt][hh] = v ? p0 + r / rep : p1;
+        const uint32_t* qp = reinterpret_cast<const uint32_t*>(a.q + (int64_t)(sp.row0 + (v ? r / rep : 0)) * a.q_stride + (h * rep + (v ? r % rep : 0)) * DH) + tq;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          qf[mt][k][hh] = v ? qp[k * 8] : 0u;
+          qf[mt][k][hh + 2] = v ? qp[k * 8 + 4] : 0u;
+        }
+      }
+
+    float o[MT][NT][4], m[MT][2], l[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      m[mt][0] = m[mt][1] = -INFINITY; l[mt][0] = l[mt][1] = 0.f;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
+    }
+    const int n_mine = (i1 - i0 - warp + 3) / 4;                       // pages i0 + warp, i0 + warp + 4, ...
+    int ids = 0;                                                       // lane t: block of my page 32 b + t
+    auto fetch_ids = [&](int base) {
+      const int i = i0 + warp + 4 * (base + lane);
+      ids = -1;
+      if (i < i1 && kp.page(i) < kp.end_page) {
+        ids = tbl[kp.page(i)];
+        if (ids < 0 || ids >= a.kv.n_blocks) { atomicOr(a.kv.status, STATUS_BAD_BLOCK); ids = -1; }
+      }
+    };
+    auto load = [&](int it) {                                          // page `it` of mine into stage it % STAGES
+      const int blk = __shfl_sync(0xffffffffu, ids, it & 31);
+      const int key0 = kp.page(i0 + warp + 4 * it) * KV_BLOCK;
+      const uint32_t dst = ring + (it % STAGES) * (2 * PB);
+#pragma unroll
+      for (int e = 0; e < KV_BLOCK * CPR / 32; ++e) {
+        const int x = e * 32 + lane, row = x / CPR, ch = x % CPR, j = key0 + row;
+        // rows that none of the queries sees become zeros: whatever the cache holds there, 0 x NaN included
+        const int bytes = (blk >= 0 && j <= p1 && (j >= kp.lo || j < a.c.sinks)) ? 16 : 0;
+        const int64_t at = ((int64_t)max(blk, 0) * KV_BLOCK + row) * DH + ch * 8;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + sw(row, ch)), "l"(kb + at), "r"(bytes) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + PB + sw(row, ch)), "l"(vb + at), "r"(bytes) : "memory");
+      }
+    };
+    if (n_mine > 0) fetch_ids(0);
+#pragma unroll
+    for (int it = 0; it < STAGES - 1; ++it) { if (it < n_mine) load(it); fa::cp_commit(); }
+    for (int it = 0; it < n_mine; ++it) {
+      if (it + STAGES - 1 < n_mine) {
+        if (((it + STAGES - 1) & 31) == 0) fetch_ids(it + STAGES - 1);
+        load(it + STAGES - 1);
+      }
+      fa::cp_commit();
+      fa::cp_wait<STAGES - 1>();
+      __syncwarp();
+      const uint32_t sk = ring + (it % STAGES) * (2 * PB), sv = sk + PB;
+      float sc[MT][2][4];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) sc[mt][n][0] = sc[mt][n][1] = sc[mt][n][2] = sc[mt][n][3] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        uint32_t b0, b1, b2, b3;
+        fa::ldsm_x4(sk + sw(((lane >> 4) << 3) + (lane & 7), k * 2 + ((lane >> 3) & 1)), b0, b1, b2, b3);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) { fa::mma_bf16(sc[mt][0], qf[mt][k], b0, b1); fa::mma_bf16(sc[mt][1], qf[mt][k], b2, b3); }
+      }
+      const int key0 = kp.page(i0 + warp + 4 * it) * KV_BLOCK;
+      const bool whole = key0 + KV_BLOCK - 1 <= p0 && (a.c.window <= 0 || key0 > p1 - a.c.window || key0 + KV_BLOCK <= a.c.sinks);
+      uint32_t pf[MT][4];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          float x[4] = {sc[mt][0][2 * hh], sc[mt][0][2 * hh + 1], sc[mt][1][2 * hh], sc[mt][1][2 * hh + 1]};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[e] *= a.scale_log2;
+            if (!whole && !chunk_visible(a.c, key0 + (e >> 1) * 8 + tq * 2 + (e & 1), prow[mt][hh])) x[e] = -INFINITY;
+          }
+          float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          // the reference maximum moves when it is outgrown; the sums are exact for any reference
+          const float mn = fmaxf(m[mt][hh], mx);
+          if (__any_sync(0xffffffffu, mn > m[mt][hh])) {
+            const float corr = mn == -INFINITY ? 1.f : fa::ex2(m[mt][hh] - mn);
+            l[mt][hh] *= corr;
+            m[mt][hh] = mn;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) { o[mt][n][2 * hh] *= corr; o[mt][n][2 * hh + 1] *= corr; }
+          }
+          const float mu = m[mt][hh] == -INFINITY ? 0.f : m[mt][hh];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { x[e] = fa::ex2(x[e] - mu); l[mt][hh] += x[e]; }
+          pf[mt][hh] = fa::pack_bf16(x[0], x[1]);
+          pf[mt][hh + 2] = fa::pack_bf16(x[2], x[3]);
+        }
+#pragma unroll
+      for (int n = 0; n < NT; n += 2) {
+        uint32_t b0, b1, b2, b3;
+        fa::ldsm_x4_t(sv + sw((((lane >> 3) & 1) << 3) + (lane & 7), n + (lane >> 4)), b0, b1, b2, b3);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) { fa::mma_bf16(o[mt][n], pf[mt], b0, b1); fa::mma_bf16(o[mt][n + 1], pf[mt], b2, b3); }
+      }
+      __syncwarp();
+    }
+    fa::cp_wait<0>();
+    __syncthreads();
+
+    // ---- join the warps
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        const int r = mt * 16 + hh * 8 + g;
+        float ls = l[mt][hh];
+        ls += __shfl_xor_sync(0xffffffffu, ls, 1);
+        ls += __shfl_xor_sync(0xffffffffu, ls, 2);
+        if (tq == 0) x_ml[warp * ROWS + r] = make_float2(m[mt][hh], ls);
+        if (r < R)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            *reinterpret_cast<float2*>(x_o + (warp * ROWS + r) * Cfg::XO + n * 8 + tq * 2) = make_float2(o[mt][n][2 * hh], o[mt][n][2 * hh + 1]);
+      }
+    __syncthreads();
+    const bool begins = i0 == 0, ends = i1 == n_pages;
+    const int slot = begins ? 2 * blockIdx.x + 1 : 2 * blockIdx.x;
+    for (int x = tid; x < R * (DH / 2); x += 128) {
+      const int r = x / (DH / 2), d = (x % (DH / 2)) * 2;
+      float2 ml[4];
+      float mm = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) { ml[w] = x_ml[w * ROWS + r]; mm = fmaxf(mm, ml[w].x); }
+      const float mu = mm == -INFINITY ? 0.f : mm;
+      float ls = 0.f, y0 = 0.f, y1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float wt = fa::ex2(ml[w].x - mu);
+        const float2 v = *reinterpret_cast<const float2*>(x_o + (w * ROWS + r) * Cfg::XO + d);
+        ls = fmaf(wt, ml[w].y, ls); y0 = fmaf(wt, v.x, y0); y1 = fmaf(wt, v.y, y1);
+      }
+      if (begins && ends) {
+        const int64_t dst = (int64_t)(sp.row0 + r / rep) * a.o.hq + h * rep + r % rep;
+        const float inv = ls > 0.f ? 1.0f / ls : 0.f;
+        *reinterpret_cast<uint32_t*>(a.o.out + dst * DH + d) = fa::pack_bf16(y0 * inv, y1 * inv);
+        if (d == 0 && a.o.lse) a.o.lse[dst] = ls > 0.f ? mm * LN2_F + logf(ls) : -INFINITY;
+      } else {
+        const int64_t at = (int64_t)slot * a.ws.rows_cap + r;
+        *reinterpret_cast<float2*>(a.ws.o + at * DH + d) = make_float2(y0, y1);
+        if (d == 0) a.ws.ml[at] = make_float2(mm, ls);
+      }
+    }
+    if (begins && !ends && tid == 0)
+      a.ws.rec[blockIdx.x] = SplitRec{sp.row0, h * rep, R, (item0 + n_pages - 1) / share - (int)blockIdx.x + 1};
+    __syncthreads();
+    f += i1 - i0;
+  }
+}
+
+}  // namespace rpo

@@ -22,7 +22,9 @@
 #include "kernels.cuh"
 #include "objective.cuh"
 #include "paged_attn.cuh"
+#include "paged_chunk.cuh"
 #include "paged_mass.cuh"
+#include "paged_step.cuh"
 #include "ref_kernels.cuh"
 #include "sampler.cuh"
 
@@ -327,6 +329,11 @@ extern "C" int rpo_create(rpo_ctx** out, const rpo_shape* shape, const rpo_limit
   ALLOC(w.ssq, (size_t)w.R * w.ssq_stride * 4);
   ALLOC(w.ssq_h, (size_t)w.HR * 4);
   ALLOC(w.tile_ctr, (size_t)TC_CTR_CAPACITY * 4);
+  const size_t op_rows = (size_t)2 * c->sm_count * OP_PART_ROWS;   // two parts of OP_PART_ROWS rows per SM
+  ALLOC(w.op_part_o, op_rows * 128 * 4);
+  ALLOC(w.op_part_ml, op_rows * sizeof(float2));
+  ALLOC(w.op_rec, (size_t)2 * c->sm_count * sizeof(SplitRec));
+  ALLOC(w.op_items, (size_t)OP_MAX_ITEMS * sizeof(ChunkItem) + sizeof(ChunkPlan));
   if (rc == RPO_OK && cudaMemsetAsync(w.tile_ctr, 0, (size_t)TC_CTR_CAPACITY * 4, c->stream) != cudaSuccess) { cudaGetLastError(); rc = RPO_ERR_CUDA; }
   if (rc == RPO_OK) rc = tc_create(c);
   // The attention kernels mask keys beyond a segment's end instead of zero-filling them, so the
