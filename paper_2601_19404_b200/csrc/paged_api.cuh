@@ -28,7 +28,7 @@ constexpr int OP_MAX_SEQS = 4096, OP_MAX_REP = 64;
 static int check_chunk(const rpo_ctx* c, const rpo_paged_kv* kv, int n_rows, int hq, int max_chunk, const void* d_q, int64_t q_stride,
                        const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg) {
   RPO_TRY(check_paged(c, kv));
-  if (n_rows < 0 || hq <= 0 || max_chunk <= 0 || !d_q || !d_q_offsets || !cfg || !(cfg->scale > 0.f) || std::isinf(cfg->scale) ||
+  if (n_rows < 0 || hq <= 0 || max_chunk <= 0 || (n_rows > 0 && !d_q) || !d_q_offsets || !cfg || !(cfg->scale > 0.f) || std::isinf(cfg->scale) ||
       cfg->window < 0 || cfg->sinks < 0 || !aligned16(d_q) || (q_stride * (int64_t)c->esz) % 16)
     return RPO_ERR_INVALID_ARG;
   if (hq % kv->n_kv_heads || hq / kv->n_kv_heads > OP_MAX_REP) return RPO_ERR_SHAPE;
@@ -133,8 +133,8 @@ static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs
     LAUNCH_OP(c, (paged_append_kernel<T, DH>), grid_for(n, 256), 256, 0, view, a, (const T*)k_new, (const T*)v_new, new_stride);
   }
   if constexpr (std::is_same<T, bf16>::value) {
-    if (a.max_chunk * (a.hq / kv->n_kv_heads) <= 16) return chunk_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
-    if (a.max_chunk * (a.hq / kv->n_kv_heads) <= 32) return chunk_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
+    if (a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads) <= 16) return chunk_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
+    if (a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads) <= 32) return chunk_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
     return chunk_tiles<DH>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
   }
   LAUNCH_OP(c, (paged_attn_simple_kernel<T, DH>), ceil_div((int64_t)a.n_rows * a.hq, 4), 128, 0, view, a, (const T*)q, q_stride, scale, (T*)out, lse);
@@ -145,7 +145,7 @@ extern "C" int rpo_chunk_attention(rpo_ctx* c, const rpo_paged_kv* kv, int32_t n
                                    int64_t q_stride, const void* d_k_new, const void* d_v_new, int64_t kv_new_stride,
                                    const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg, void* d_out, float* d_lse_out) {
   RPO_TRY(check_chunk(c, kv, n_rows, n_q_heads, max_chunk, d_q, q_stride, d_q_offsets, cfg));
-  if (!d_out || !aligned16(d_out) || !d_k_new != !d_v_new) return RPO_ERR_INVALID_ARG;
+  if ((n_rows > 0 && !d_out) || !aligned16(d_out) || !d_k_new != !d_v_new) return RPO_ERR_INVALID_ARG;
   if (d_k_new && (!aligned16(d_k_new) || !aligned16(d_v_new) || (kv_new_stride * (int64_t)c->esz) % 16 ||
                   (n_rows > 1 && kv_new_stride < (int64_t)kv->n_kv_heads * kv->head_dim)))
     return RPO_ERR_INVALID_ARG;
@@ -159,10 +159,53 @@ extern "C" int rpo_chunk_attention(rpo_ctx* c, const rpo_paged_kv* kv, int32_t n
 #undef CHUNK_ATTN
 }
 
+template <int DH, int MT>
+static int mass_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const float* lse, float scale,
+                      const float* in, float* out, int stride) {
+  using Cfg = MassStepCfg<DH, MT>;
+  static bool attr_done[64] = {};
+  if (tc_first_use_on_device(c, attr_done))
+    CUDA_TRY(cudaFuncSetAttribute(mass_step_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4));
+  MassArgs m;
+  m.kv = view; m.c = a; m.q = q; m.q_stride = q_stride; m.scale_log2 = scale * 1.4426950408889634f; m.lse = lse; m.in = in; m.out = out;
+  m.stride = stride; m.rep = a.hq / view.hkv;
+  LAUNCH_OP(c, (mass_step_kernel<DH, MT>), 3 * c->sm_count, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, m);
+  return RPO_OK;
+}
+
+template <int DH>
+static int mass_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const float* lse, float scale,
+                      const float* in, float* out, int stride) {
+  using Cfg = MassCfg<DH>;
+  static bool attr_done[64] = {};
+  if (tc_first_use_on_device(c, attr_done))
+    CUDA_TRY(cudaFuncSetAttribute(mass_chunk_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+  MassTcArgs m;
+  m.kv = view; m.c = a; m.scale_log2 = scale * 1.4426950408889634f; m.lse = lse; m.in = in; m.out = out; m.stride = stride;
+  m.rep = a.hq / view.hkv; m.tq = MS_ROWS / m.rep;
+  MassItem* items = (MassItem*)c->ws.op_items;
+  ChunkPlan* plan = (ChunkPlan*)(items + OP_MAX_ITEMS);
+  m.items = items; m.plan = plan; m.ws.part = c->ws.op_part_o; m.ws.rec = (SplitRec*)c->ws.op_rec;
+  CUtensorMap qm, km;
+  RPO_TRY(op_map_rows(c, &qm, q, q_stride, a.n_rows, a.hq, DH, m.rep, m.tq));
+  RPO_TRY(op_map_pages(c, &km, view, view.k, DH));
+  LAUNCH_OP(c, mass_plan_kernel, 1, 1024, view.n_seqs * 4, view, a, stride, m.tq, c->sm_count, 2, items, plan);
+  LAUNCH_OP(c, (mass_chunk_kernel<DH>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, m);
+  LAUNCH_OP(c, mass_merge_kernel, c->sm_count, MS_KEYS, 0, m.ws, in, out);
+  return RPO_OK;
+}
+
 template <typename T, int DH>
 static int attention_mass_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs& a, const void* q, int64_t q_stride, const float* lse, float scale,
                             const float* mass_in, float* mass_out, int mass_stride) {
   const PagedView<T> view = paged_view<T>(c, kv);
+  if constexpr (std::is_same<T, bf16>::value) {
+    const int rep = a.hq / kv->n_kv_heads;
+    if (a.n_rows == 0 || a.max_chunk * (int64_t)rep <= 16)
+      return mass_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, lse, scale, mass_in, mass_out, mass_stride);
+    if (a.max_chunk * (int64_t)rep <= 32) return mass_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, lse, scale, mass_in, mass_out, mass_stride);
+    return mass_tiles<DH>(c, view, a, (const bf16*)q, q_stride, lse, scale, mass_in, mass_out, mass_stride);
+  }
   const dim3 grid(ceil_div(std::min((int64_t)mass_stride, (int64_t)view.table_stride * KV_BLOCK), MASS_KEYS), view.hkv, view.n_seqs);
   LAUNCH_OP(c, (paged_mass_simple_kernel<T, DH>), grid, MASS_KEYS, 0, view, a, (const T*)q, q_stride, lse, scale, mass_in, mass_out, mass_stride);
   return RPO_OK;
@@ -172,7 +215,7 @@ extern "C" int rpo_attention_mass(rpo_ctx* c, const rpo_paged_kv* kv, int32_t n_
                                   int64_t q_stride, const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg, const float* d_lse,
                                   const float* d_mass_in, float* d_mass_out, int32_t mass_stride) {
   RPO_TRY(check_chunk(c, kv, n_rows, n_q_heads, max_chunk, d_q, q_stride, d_q_offsets, cfg));
-  if (!d_lse || !d_mass_out || mass_stride <= 0) return RPO_ERR_INVALID_ARG;
+  if ((n_rows > 0 && !d_lse) || !d_mass_out || mass_stride <= 0) return RPO_ERR_INVALID_ARG;
   if (kv->n_kv_heads > 65535) return RPO_ERR_LIMIT;
   RPO_TRY(enter(c));
   ProfScope ps(c, KC_ATTN);

@@ -46,30 +46,33 @@ struct KeyTiles {
   __device__ __forceinline__ int page_end(int t) const { return t < n1 ? kp.n_first : kp.end_page; }
 };
 
+// Sum of the lower threads' values, and of all, of a CTA of 1024.
+__device__ __forceinline__ void plan_scan(int64_t v, int64_t& before, int64_t& all, int64_t* s_warp) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int64_t n = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += n; }
+  __syncthreads();
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  before = incl - v; all = 0;
+  for (int w = 0; w < 32; ++w) { if (w < warp) before += s_warp[w]; all += s_warp[w]; }
+}
+
 // The list of items, summed up: one CTA.  tok: tokens per item; PAGES: pages per key tile.
 template <typename T, int PAGES>
 __global__ void __launch_bounds__(1024) chunk_plan_kernel(PagedView<T> kv, ChunkArgs c, int tok, int n_ctas, int min_share, ChunkItem* items,
                                                           ChunkPlan* plan) {
   extern __shared__ int pl_first[];                    // items of the sequences before s
   __shared__ int64_t s_warp[32];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  auto block_scan = [&](int64_t v, int64_t& before, int64_t& all) {
-    int64_t incl = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const int64_t n = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += n; }
-    __syncthreads();
-    if (lane == 31) s_warp[warp] = incl;
-    __syncthreads();
-    before = incl - v; all = 0;
-    for (int w = 0; w < 32; ++w) { if (w < warp) before += s_warp[w]; all += s_warp[w]; }
-  };
+  const int tid = threadIdx.x;
   // Offsets that go back and forth could name more items than there are rows for: what does not fit is dropped.
   int n_items = 0;
   for (int s0 = 0; s0 < kv.n_seqs; s0 += 1024) {
     const int s = s0 + tid;
     const int n = s < kv.n_seqs ? (chunk_span(kv, c, s).rows + tok - 1) / tok : 0;
     int64_t before, all;
-    block_scan(n, before, all);
+    plan_scan(n, before, all, s_warp);
     if (s < kv.n_seqs) pl_first[s] = (int)min((int64_t)OP_MAX_ITEMS, n_items + before);
     n_items = (int)min((int64_t)OP_MAX_ITEMS, n_items + all);
   }
@@ -80,8 +83,7 @@ __global__ void __launch_bounds__(1024) chunk_plan_kernel(PagedView<T> kv, Chunk
     int64_t n = 0;
     ChunkItem it = {};
     if (i < n_items) {
-      int lo = 0, hi = kv.n_seqs - 1;
-      while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (pl_first[mid] <= i) lo = mid; else hi = mid - 1; }
+      const int lo = page_list_seq(pl_first, kv.n_seqs, i);
       const ChunkSpan sp = chunk_span(kv, c, lo);
       const int t0 = (i - pl_first[lo]) * tok;
       it.seq = lo; it.n_tok = min(tok, sp.rows - t0); it.row0 = sp.row0 + t0; it.p0 = sp.len - sp.rows + t0;
@@ -89,7 +91,7 @@ __global__ void __launch_bounds__(1024) chunk_plan_kernel(PagedView<T> kv, Chunk
       n = (int64_t)it.n_tiles * kv.hkv;
     }
     int64_t before, all;
-    block_scan(n, before, all);
+    plan_scan(n, before, all, s_warp);
     if (total + all > OP_MAX_TILES) {                    // 2^31 tile x head steps: no call of this size ends in a lifetime
       if (tid == 0) atomicOr(kv.status, STATUS_BAD_LENGTH);
       n_items = i0;

@@ -12,7 +12,7 @@
 namespace rpo {
 
 // Workspace of the operators: rows of one part of a split item (two parts per SM), items of one call.
-constexpr int OP_PART_ROWS = 256, OP_MAX_ITEMS = 1 << 17;
+constexpr int OP_PART_ROWS = 256, OP_MAX_ITEMS = 1 << 18;
 constexpr int STATUS_BAD_LENGTH = 8;      // a length, chunk offset or chunk size out of range (clamped)
 
 template <typename T>

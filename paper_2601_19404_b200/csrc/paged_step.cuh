@@ -97,6 +97,31 @@ __device__ __forceinline__ KeyPages key_pages(const ChunkArgs& c, int p0, int p1
   return k;
 }
 
+// The list of all pages: pref[s] = sum of count() over the sequences before s; returns the sum over all.  Called by all
+// THREADS threads of the CTA (thread t: consecutive sequences); ends with a barrier.
+template <int THREADS, typename F>
+__device__ __forceinline__ int page_list(int n_seqs, int* pref, int* scan, F count) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = (n_seqs + THREADS - 1) / THREADS;
+  int sum = 0;
+  for (int s = tid * per; s < min(n_seqs, (tid + 1) * per); ++s) { const int n = count(s); pref[s] = n; sum += n; }
+  int incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int n = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += n; }
+  if (lane == 31) scan[warp] = incl;
+  __syncthreads();
+  int run = incl - sum, total = 0;
+  for (int w = 0; w < THREADS / 32; ++w) { if (w < warp) run += scan[w]; total += scan[w]; }
+  for (int s = tid * per; s < min(n_seqs, (tid + 1) * per); ++s) { const int n = pref[s]; pref[s] = run; run += n; }
+  __syncthreads();
+  return total;
+}
+// The sequence whose pages hold place f of the list (empty sequences hold none).
+__device__ __forceinline__ int page_list_seq(const int* pref, int n_seqs, int f) {
+  int lo = 0, hi = n_seqs - 1;
+  while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (pref[mid] <= f) lo = mid; else hi = mid - 1; }
+  return lo;
+}
+
 template <int DH, int MT>
 struct StepCfg {
   static constexpr int WARPS = 4;
@@ -126,33 +151,10 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, tq = lane & 3;
   const int n_seqs = a.kv.n_seqs, hkv = a.kv.hkv, rep = a.o.rep;
 
-  // ---- the list: pages per sequence, summed up (thread t: `per` consecutive sequences)
-  const int per = (n_seqs + 127) / 128;
-  int sum = 0;
-  for (int i = 0; i < per; ++i) {
-    const int s = tid * per + i;
-    if (s >= n_seqs) break;
+  const int total = page_list<128>(n_seqs, s_pref, s_scan, [&](int s) {
     const ChunkSpan sp = chunk_span(a.kv, a.c, s);
-    const int n = sp.rows > 0 ? max(1, key_pages(a.c, sp.len - sp.rows, sp.len - 1).count()) * hkv : 0;
-    s_pref[s] = n;
-    sum += n;
-  }
-  int incl = sum;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) { const int n = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += n; }
-  if (lane == 31) s_scan[warp] = incl;
-  __syncthreads();
-  int run = incl - sum;
-  for (int w = 0; w < warp; ++w) run += s_scan[w];
-  const int total = s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3];
-  for (int i = 0; i < per; ++i) {
-    const int s = tid * per + i;
-    if (s >= n_seqs) break;
-    const int n = s_pref[s];
-    s_pref[s] = run;
-    run += n;
-  }
-  __syncthreads();
+    return sp.rows > 0 ? max(1, key_pages(a.c, sp.len - sp.rows, sp.len - 1).count()) * hkv : 0;
+  });
   const int share = max(a.min_share, (total + (int)gridDim.x - 1) / (int)gridDim.x);
   const int f_end = (int)min((int64_t)total, (int64_t)(blockIdx.x + 1) * share);
   int f = (int)min((int64_t)total, (int64_t)blockIdx.x * share);
@@ -164,9 +166,7 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
   auto sw = [](int row, int chunk) -> uint32_t { return (uint32_t)(row * (DH * 2) + ((chunk ^ (row & 7)) << 4)); };
 
   while (f < f_end) {
-    int lo = 0, hi = n_seqs - 1;                                       // last sequence that begins at or before f (and is not empty)
-    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (s_pref[mid] <= f) lo = mid; else hi = mid - 1; }
-    const int s = lo;
+    const int s = page_list_seq(s_pref, n_seqs, f);
     const ChunkSpan sp = chunk_span(a.kv, a.c, s);
     const int R = sp.rows * rep, p0 = sp.len - sp.rows, p1 = sp.len - 1;
     const KeyPages kp = key_pages(a.c, p0, p1);
