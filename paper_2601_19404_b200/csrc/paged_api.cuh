@@ -72,7 +72,7 @@ static int chunk_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   s.kv = view; s.c = a; s.q = q; s.q_stride = q_stride; s.scale_log2 = scale * 1.4426950408889634f;
   s.o.out = out; s.o.lse = lse; s.o.hq = a.hq; s.o.rep = a.hq / view.hkv; s.ws = split_ws(c, Cfg::ROWS); s.min_share = 4;
   LAUNCH_OP(c, (paged_step_kernel<DH, MT>), grid, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, s);
-  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(grid, Cfg::ROWS / 4), 128, 0, s.ws, s.o);
+  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(grid, std::min(a.max_chunk * s.o.rep, Cfg::ROWS)), 256, 0, s.ws, s.o);
   return RPO_OK;
 }
 
@@ -120,7 +120,7 @@ static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   RPO_TRY(op_map_pages(c, &vm, view, view.v, DH));
   LAUNCH_OP(c, (chunk_plan_kernel<bf16, CH_BN / KV_BLOCK>), 1, 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4, items, plan);
   LAUNCH_OP(c, (paged_chunk_kernel<DH>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
-  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, 8), 128, 0, t.ws, t.o);
+  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, 16), 256, 0, t.ws, t.o);
   return RPO_OK;
 }
 

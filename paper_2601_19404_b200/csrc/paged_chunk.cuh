@@ -4,19 +4,20 @@
 // An item is up to 2 tq tokens of one sequence x the rep query heads of one KV head, as two sub-tiles of tq rep <= 128
 // packed rows (token-major); its keys come in tiles of 128.  All key tiles of all items form one list, cut into equal
 // pieces for one persistent CTA per SM (plan kernel); an item cut by a piece border leaves unnormalised parts that
-// split_merge_kernel joins.  Per 128-key tile and sub-tile x:
+// split_merge_kernel joins.  A tile is worked on in two halves of 64 keys; per half and sub-tile x:
 //
-//   S_x = Q_x K^T    tcgen05.mma, both operands in shared memory (128-byte swizzle, filled by TMA straight from the
-//                    pages: 16 x 64 boxes), accumulator in tensor memory
+//   S = Q_x K^T      tcgen05.mma, both operands in shared memory (128-byte swizzle, filled by TMA straight from the
+//                    pages: 16 x 64 boxes), accumulator in tensor memory, one buffer per half
 //   softmax          one warpgroup per sub-tile, one thread per row = TMEM lane: no shuffles, no exchange.  P = 2^(s - m)
 //                    goes back to tensor memory as bf16, over the S it came from
-//   O_x += P_x V     tcgen05.mma with A = P from tensor memory; accumulates over all tiles.  m is a reference that moves
-//                    only when the running maximum outgrows it by 2^8: then the row's O is rescaled in place.  (S of
-//                    the next tile is issued after P V of this one, so a softmax thread that holds S knows O is at rest.)
+//   O_x += P V       tcgen05.mma with A = P from tensor memory; accumulates over all tiles.  m is a reference that moves
+//                    only when the running maximum outgrows it by 2^8: then the row's O is rescaled in place.
 //
-// The two sub-tiles alternate: while the softmax of one runs, the tensor cores work for the other.  Rows of V that no
-// row of the item sees (behind the last token, between sinks and window) are zeroed in shared memory before P V, since
-// 0 x NaN is not 0; scores there are masked by selection.
+// S of a half is refilled as soon as P V of the same half of the tile before has been issued, so a softmax warp that
+// hands over one half finds the next one ready: with 128-key halves (S waits for the softmax of the whole tile before)
+// a tile took 4620 clocks, 1900 of them waiting for S.  Rows of V that no row of the item sees (behind the last token,
+// between sinks and window) are zeroed in shared memory before P V, since 0 x NaN is not 0; scores there are masked by
+// selection.
 #pragma once
 #include "attn_tc5.cuh"
 #include "paged_step.cuh"
@@ -25,10 +26,8 @@ namespace rpo {
 
 constexpr int CH_BM = 128, CH_BN = 128;
 constexpr int64_t OP_MAX_TILES = ((int64_t)1 << 31) - (1 << 20);
+constexpr int CH_HALF = CH_BN / 2;
 constexpr float CH_LAZY = 8.0f;                // log2 of the largest P entry tolerated before the reference maximum moves
-// Registers: 384 threads are launched with 168 each (64512); the producer / MMA warpgroup gives some of its own to the
-// softmax warpgroups, whose rows hold 128 scores: 128 x 72 + 256 x 216 = 64512.
-constexpr int CH_REGS_FEW = 72, CH_REGS_MANY = 216;
 
 struct ChunkItem { int first, n_tiles, row0, n_tok; int seq, p0, pad0, pad1; };   // p0: position of the item's first token
 struct ChunkPlan { int n_items, total, share, pad; };                        // `first`, `total`: in (tile, KV head)s
@@ -129,7 +128,7 @@ struct ChunkCfg {
   static constexpr int Q_BYTES = CH_BM * DH * 2;            // one sub-tile
   static constexpr int KV_BYTES = CH_BN * DH * 2;           // one K or V tile
   static constexpr int NSK = 2, NSV = 2;
-  static constexpr int SMEM = 2 * Q_BYTES + (NSK + NSV) * KV_BYTES + 1024 + 512;
+  static constexpr int SMEM = 2 * Q_BYTES + (NSK + NSV) * KV_BYTES + 1024 + 512;      // tiles, alignment, barriers
   static constexpr int THREADS = 384;
 };
 
@@ -170,6 +169,20 @@ __device__ __forceinline__ void tmem_st32_nowait(uint32_t taddr, const uint32_t*
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// The matrix instructions take their descriptors from uniform registers.  Values that went through a shuffle and code
+// under an elected predicate stay there; under `lane == 0` every operand of every instruction is moved across first.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p != 0;
+}
+// Two float32 values in one 64-bit register: one instruction for both.
+__device__ __forceinline__ uint64_t pack2(float x, float y) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y)); return r; }
+__device__ __forceinline__ void unpack2(uint64_t r, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const void* map, int x, int y, int z, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -195,19 +208,21 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
   uint64_t* bars = (uint64_t*)(sm + 2 * Cfg::Q_BYTES + (NSK + NSV) * Cfg::KV_BYTES);
   uint64_t *k_full = bars, *k_empty = bars + NSK, *v_full = bars + 2 * NSK, *v_empty = v_full + NSV;
   uint64_t* b2 = v_empty + NSV;
-  uint64_t *s_full = b2, *p_full = b2 + 2, *o_full = b2 + 4, *q_full = b2 + 6, *q_free = b2 + 7;
-  uint32_t* tmem_slot = (uint32_t*)(b2 + 8);
+  uint64_t *s_full = b2, *p_full = b2 + 4;                    // [sub-tile][half]
+  uint64_t *pv_done = b2 + 8, *o_full = b2 + 10, *q_full = b2 + 12, *q_free = b2 + 13, *v_ready = b2 + 14;
+  uint32_t* tmem_slot = (uint32_t*)(v_ready + NSV);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   int* s_first = (int*)(tmem_slot + 2);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = (int)t5::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int hkv = a.kv.hkv, rep = a.o.rep;
   const ChunkPlan plan = *a.plan;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < NSK; ++i) { tc::mbar_init(&k_full[i], 1); tc::mbar_init(&k_empty[i], 1); }
-    for (int i = 0; i < NSV; ++i) { tc::mbar_init(&v_full[i], 1); tc::mbar_init(&v_empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { tc::mbar_init(&s_full[i], 1); tc::mbar_init(&p_full[i], 4); tc::mbar_init(&o_full[i], 1); }
-    tc::mbar_init(q_full, 1); tc::mbar_init(q_free, 1);
+    for (int i = 0; i < NSK; ++i) { tc::mbar_init(&k_full[i], 1); tc::mbar_init(&k_empty[i], 2); }
+    for (int i = 0; i < NSV; ++i) { tc::mbar_init(&v_full[i], 1); tc::mbar_init(&v_ready[i], 1); tc::mbar_init(&v_empty[i], 2); }
+    for (int i = 0; i < 4; ++i) { tc::mbar_init(&s_full[i], 1); tc::mbar_init(&p_full[i], 4); }
+    for (int i = 0; i < 2; ++i) { tc::mbar_init(&pv_done[i], 1); tc::mbar_init(&o_full[i], 1); }
+    tc::mbar_init(q_full, 1); tc::mbar_init(q_free, 2);
     *abort_flag = 0; *s_first = 0;
     a.ws.rec[blockIdx.x] = SplitRec{0, 0, 0, 0};
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -234,7 +249,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CH_REGS_FEW));   // per role, not before: the register limit holds from here on
     bool ok = true;
     int kt = 0;                                              // tiles sent: ring position of K and V
     for (int seg = 0; ok && walk.next(); ++seg) {
@@ -273,92 +287,119 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         if (hf < HALVES) t5::tma_load_2d(sV + sv * Cfg::KV_BYTES + b * PAGE + hf * 2048, &v_map, hf * 64, y, &v_full[sv]);
       }
     }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer (the warp together; lane 0 issues)
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CH_REGS_FEW));
-    constexpr uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(CH_BN >> 3) << 17) | ((uint32_t)(CH_BM >> 4) << 24);
-    constexpr uint32_t idesc_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(CH_BM >> 4) << 24);
-    const uint32_t dq = t5::desc_lo(sQ, 16), dk = t5::desc_lo(sK, 16), dv = t5::desc_lo(sV, 2048);
+  } else if (warp == 3) {
+    // ------------------------------------------------------------------ rows of V that no row of the item sees: zeros
     bool ok = true;
     int kt = 0;
-    uint32_t p_phase[2] = {0, 0};
-    auto issue_qk = [&](int x, int sk) {
-      const uint32_t q = dq + x * (Cfg::Q_BYTES >> 4), k = dk + sk * (Cfg::KV_BYTES >> 4);
+    while (ok && walk.next()) {
+      const int p1 = walk.it.p0 + walk.it.n_tok - 1;
+      const KeyTiles<CH_BN / KV_BLOCK> kt_of(a.c, walk.it.p0, p1);
+      for (int t = walk.t0; t < walk.t1; ++t, ++kt) {
+        const int sv = kt % NSV;
+        ok = tc::mbar_wait_warp(&v_full[sv], (kt / NSV) & 1, abort_flag);
+        if (!ok) break;
+        const int key0 = kt_of.page0(t) * KV_BLOCK, seen_end = t < kt_of.n1 ? min(a.c.sinks, p1 + 1) : p1 + 1;
+        if (key0 + CH_BN > seen_end || (t >= kt_of.n1 && key0 < kt_of.kp.lo)) {
+          for (int r = lane; r < CH_BN; r += 32) {
+            const int j = key0 + r;
+            if (j < seen_end && (j >= kt_of.kp.lo || j < a.c.sinks)) continue;
+            const uint32_t at = sV + sv * Cfg::KV_BYTES + (r >> 4) * PAGE + (r & 15) * 128;
+#pragma unroll
+            for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+              for (int ch = 0; ch < 8; ++ch) fa::st_zero16(at + hf * 2048 + ch * 16);
+          }
+          t5::fence_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&v_ready[sv]);
+      }
+    }
+  } else if (warp < 3) {
+    // ------------------------------------------------------------------ MMA issuers: warp 1 sub-tile 0, warp 2 sub-tile 1
+    // (One issuer for both left the tensor pipe idle between its waits: an instruction of 64 clocks occupies the thread
+    // that issues it for as long.  Each warp waits together, one lane issues.)
+    constexpr uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(CH_HALF >> 3) << 17) | ((uint32_t)(CH_BM >> 4) << 24);
+    constexpr uint32_t idesc_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(CH_BM >> 4) << 24);
+    const int x = warp - 1;
+    const uint32_t dq = t5::uniform(t5::desc_lo(sQ + x * Cfg::Q_BYTES, 16)), dk = t5::uniform(t5::desc_lo(sK, 16));
+    const uint32_t dv = t5::uniform(t5::desc_lo(sV, 2048)), tm = t5::uniform(tmem);
+    const uint32_t t_s = tm + x * CH_BN, t_o = tm + 2 * CH_BN + x * DH;
+    bool ok = true;
+    int kt = 0;
+    uint32_t p_phase = 0;
+    auto issue_qk = [&](int h, int sk) {
+      const uint32_t k = dk + sk * (Cfg::KV_BYTES >> 4) + h * (CH_HALF * 128 >> 4);
 #pragma unroll
       for (int i = 0; i < DH / 16; ++i) {
         const uint32_t off = (i >> 2) * (CH_BN * 128 >> 4) + (i & 3) * 2;
-        t5::umma_ss(tmem + x * CH_BN, q + off, k + off, idesc_qk, i > 0);
+        t5::umma_ss(t_s + h * CH_HALF, dq + off, k + off, idesc_qk, i > 0);
       }
-      tc::umma_commit(&s_full[x]);
+      tc::umma_commit(&s_full[x * 2 + h]);
     };
-    auto issue_pv = [&](int x, int sv, bool first) {
-      const uint32_t v = dv + sv * (Cfg::KV_BYTES >> 4), o = tmem + 2 * CH_BN + x * DH, p = tmem + x * CH_BN;
+    auto issue_pv = [&](int h, int sv, bool first) {
+      const uint32_t v = dv + sv * (Cfg::KV_BYTES >> 4) + h * (CH_HALF / KV_BLOCK * PAGE >> 4), p = t_s + h * CH_HALF;
 #pragma unroll
-      for (int b = 0; b < CH_BN / KV_BLOCK; ++b) t5::umma_ts(o, p + b * 8, v + b * (PAGE >> 4), idesc_pv, (!first || b > 0) ? 1u : 0u);
+      for (int b = 0; b < CH_HALF / KV_BLOCK; ++b) t5::umma_ts(t_o, p + b * 8, v + b * (PAGE >> 4), idesc_pv, (!first || b > 0) ? 1u : 0u);
+      tc::umma_commit(&pv_done[x]);
     };
     for (int seg = 0; ok && walk.next(); ++seg) {
-      const int p1 = walk.it.p0 + walk.it.n_tok - 1;
-      const KeyTiles<CH_BN / KV_BLOCK> kt_of(a.c, walk.it.p0, p1);
-      const int subs = walk.it.n_tok > a.tq ? 2 : 1;
+      const bool idle = x == 1 && walk.it.n_tok <= a.tq;                 // no second sub-tile: only release what the first uses
       ok = tc::mbar_wait_warp(q_full, seg & 1, abort_flag) && tc::mbar_wait_warp(&k_full[kt % NSK], (kt / NSK) & 1, abort_flag);
       if (!ok) break;
       tc::tmem_fence_after();
-      if (lane == 0) {
-        for (int x = 0; x < subs; ++x) issue_qk(x, kt % NSK);
-        tc::umma_commit(&k_empty[kt % NSK]);
-        if (walk.t1 - walk.t0 == 1) tc::umma_commit(q_free);
+      if (t5::elect_one()) {
+        if (idle) {
+          tc::mbar_arrive(&k_empty[kt % NSK]);
+          tc::mbar_arrive(q_free);
+        } else {
+          issue_qk(0, kt % NSK);
+          issue_qk(1, kt % NSK);
+          tc::umma_commit(&k_empty[kt % NSK]);
+          if (walk.t1 - walk.t0 == 1) tc::umma_commit(q_free);
+        }
       }
       for (int t = walk.t0; t < walk.t1 && ok; ++t, ++kt) {
         const int sv = kt % NSV, sk = (kt + 1) % NSK;
         const bool more = t + 1 < walk.t1;
-        for (int x = 0; x < subs; ++x) {
-          if (x == 0) {
-            ok = tc::mbar_wait_warp(&v_full[sv], (kt / NSV) & 1, abort_flag);
-            if (!ok) break;
-            // rows of V that no row of the item sees
-            const int key0 = kt_of.page0(t) * KV_BLOCK, seen_end = t < kt_of.n1 ? min(a.c.sinks, p1 + 1) : p1 + 1;
-            if (key0 + CH_BN > seen_end || (t >= kt_of.n1 && key0 < kt_of.kp.lo)) {
-              for (int r = lane; r < CH_BN; r += 32) {
-                const int j = key0 + r;
-                if (j < seen_end && (j >= kt_of.kp.lo || j < a.c.sinks)) continue;
-                const uint32_t at = sV + sv * Cfg::KV_BYTES + (r >> 4) * PAGE + (r & 15) * 128;
-#pragma unroll
-                for (int hf = 0; hf < HALVES; ++hf)
-#pragma unroll
-                  for (int ch = 0; ch < 8; ++ch) fa::st_zero16(at + hf * 2048 + ch * 16);
-              }
-              t5::fence_async_smem();
-              __syncwarp();
-            }
+        ok = tc::mbar_wait_warp(&v_ready[sv], (kt / NSV) & 1, abort_flag);
+        if (ok && more) ok = tc::mbar_wait_warp(&k_full[sk], ((kt + 1) / NSK) & 1, abort_flag);
+        if (!ok) break;
+        if (idle) {
+          if (t5::elect_one()) {
+            tc::mbar_arrive(&v_empty[sv]);
+            if (more) tc::mbar_arrive(&k_empty[sk]);
           }
-          ok = tc::mbar_wait_warp(&p_full[x], p_phase[x], abort_flag);
+          continue;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          ok = tc::mbar_wait_warp(&p_full[x * 2 + h], p_phase, abort_flag);
           if (!ok) break;
-          p_phase[x] ^= 1;
           tc::tmem_fence_after();
-          if (lane == 0) {
-            issue_pv(x, sv, t == walk.t0);
-            if (x == subs - 1) tc::umma_commit(&v_empty[sv]);
-            if (!more) tc::umma_commit(&o_full[x]);
-          }
-          if (more) {
-            if (x == 0) { ok = tc::mbar_wait_warp(&k_full[sk], ((kt + 1) / NSK) & 1, abort_flag); if (!ok) break; tc::tmem_fence_after(); }
-            if (lane == 0) {
-              issue_qk(x, sk);
-              if (x == subs - 1) { tc::umma_commit(&k_empty[sk]); if (t + 2 == walk.t1) tc::umma_commit(q_free); }
+          if (t5::elect_one()) {
+            issue_pv(h, sv, t == walk.t0 && h == 0);
+            if (more) issue_qk(h, sk);
+            if (h == 1) {
+              tc::umma_commit(&v_empty[sv]);
+              if (more) tc::umma_commit(&k_empty[sk]);
+              else tc::umma_commit(&o_full[x]);
+              if (t + 2 == walk.t1) tc::umma_commit(q_free);
             }
           }
         }
+        p_phase ^= 1;
       }
     }
   } else if (warp >= 4) {
     // ------------------------------------------------------------------ softmax: warps 4..7 sub-tile 0, 8..11 sub-tile 1
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(CH_REGS_MANY));
     const int x = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
     const uint32_t t_s = tmem + ((uint32_t)(quad * 32) << 16) + x * CH_BN;
     const uint32_t t_o = tmem + ((uint32_t)(quad * 32) << 16) + 2 * CH_BN + x * DH;
     const int tok = r / rep;
     const bool in_tile = tok < a.tq;
     uint32_t s_phase = 0, o_phase = 0;
+    int steps = 0;                                           // halves of this sub-tile so far: phases of pv_done
     bool ok = true;
     for (int seg = 0; ok && walk.next(); ++seg) {
       if (x == 1 && walk.it.n_tok <= a.tq) continue;
@@ -368,33 +409,39 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
       const int p_lo = p_item + x * a.tq, p_hi = min(p1, p_lo + a.tq - 1);     // positions of my sub-tile
       const int p = min(p_lo + tok, p_hi);
       float m = -INFINITY, l = 0.f;
-      for (int t = walk.t0; t < walk.t1; ++t) {
-        const int key0 = kt_of.page0(t) * KV_BLOCK;
-        const bool first_range = t < kt_of.n1;
-        ok = tc::mbar_wait_warp(&s_full[x], s_phase, abort_flag);
+      for (int u = 2 * walk.t0; u < 2 * walk.t1; ++u, ++steps) {
+        const int h = u & 1, key0 = kt_of.page0(u >> 1) * KV_BLOCK + h * CH_HALF;
+        const bool first_range = (u >> 1) < kt_of.n1;
+        const uint32_t ts = t_s + h * CH_HALF;
+        ok = tc::mbar_wait_warp(&s_full[x * 2 + h], s_phase, abort_flag);
         if (!ok) break;
-        s_phase ^= 1;
+        if (h == 1) s_phase ^= 1;
         tc::tmem_fence_after();
-        uint32_t v[CH_BN];
-#pragma unroll
-        for (int c = 0; c < CH_BN; c += 32) tc::tmem_ld32_nowait(t_s + c, v + c);
+        uint32_t v[CH_HALF];
+        tc::tmem_ld32_nowait(ts, v);
+        tc::tmem_ld32_nowait(ts + 32, v + 32);
         tc::tmem_ld_wait();
-        const bool whole = key0 + CH_BN - 1 <= (first_range ? min(p_lo, a.c.sinks - 1) : p_lo) &&
-                           (a.c.window <= 0 || key0 > p_hi - a.c.window || key0 + CH_BN <= a.c.sinks);
+        const bool whole = key0 + CH_HALF - 1 <= (first_range ? min(p_lo, a.c.sinks - 1) : p_lo) &&
+                           (a.c.window <= 0 || key0 > p_hi - a.c.window || key0 + CH_HALF <= a.c.sinks);
         if (!whole) {
           const int hi = (first_range ? min(p, a.c.sinks - 1) : p) - key0;
           const int lo = a.c.window > 0 ? p - a.c.window + 1 - key0 : -key0, sk = a.c.sinks - key0;
 #pragma unroll
-          for (int c = 0; c < CH_BN; ++c) if (c > hi || (c < lo && c >= sk)) v[c] = 0xFF800000u;
+          for (int c = 0; c < CH_HALF; ++c) if (c > hi || (c < lo && c >= sk)) v[c] = 0xFF800000u;
         }
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < CH_BN; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(v[c]));
+        for (int c = 0; c < CH_HALF; c += 2) mx[(c >> 1) & 3] = t5::max3(mx[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
         const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
         const bool move = mt > m + CH_LAZY || (m == -INFINITY && mt > -INFINITY);
         if (__any_sync(0xffffffffu, move)) {
           const float factor = move ? (m == -INFINITY ? 0.f : fa::ex2(m - mt)) : 1.f;
-          if (t > walk.t0) {
+          if (u > 2 * walk.t0) {
+            // O is at rest once P V of the half before is done.  (This half's S was issued behind the P V of two halves
+            // ago, so at most that one phase is outstanding and its parity cannot be taken for an older one.)
+            ok = tc::mbar_wait_warp(&pv_done[x], (steps - 1) & 1, abort_flag);
+            if (!ok) break;
+            tc::tmem_fence_after();
 #pragma unroll
             for (int c = 0; c < DH; c += 32) {
               uint32_t w[32];
@@ -407,21 +454,27 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
           if (move) { l *= factor; m = mt; }
         }
         const float mu = m == -INFINITY ? 0.f : m;
-        float ps[4] = {0.f, 0.f, 0.f, 0.f};
+        // two scores at a time: 2^(s scale - m) as packed multiply-add, two exponentials, packed sum
+        const uint64_t sc2 = t5::pack2(a.scale_log2, a.scale_log2), mu2 = t5::pack2(-mu, -mu);
+        uint64_t ps[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int c = 0; c < CH_BN; c += 2) {
-          const float p0 = fa::ex2(fmaf(__uint_as_float(v[c]), a.scale_log2, -mu));
-          const float pb = fa::ex2(fmaf(__uint_as_float(v[c + 1]), a.scale_log2, -mu));
-          ps[(c >> 1) & 3] += p0 + pb;
+        for (int c = 0; c < CH_HALF; c += 2) {
+          float p0, pb;
+          t5::unpack2(t5::fma2(t5::pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, mu2), p0, pb);
+          p0 = fa::ex2(p0); pb = fa::ex2(pb);
+          ps[(c >> 1) & 3] = t5::add2(ps[(c >> 1) & 3], t5::pack2(p0, pb));
           v[c >> 1] = fa::pack_bf16(p0, pb);
-          if (c == 62) t5::tmem_st32_nowait(t_s, v);
         }
-        t5::tmem_st32_nowait(t_s + 32, v + 32);
-        l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+        t5::tmem_st32_nowait(ts, v);
+        {
+          float x0, x1;
+          t5::unpack2(t5::add2(t5::add2(ps[0], ps[1]), t5::add2(ps[2], ps[3])), x0, x1);
+          l += x0 + x1;
+        }
         t5::tmem_st_wait();
         tc::tmem_fence_before();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&p_full[x]);
+        if (lane == 0) tc::mbar_arrive(&p_full[x * 2 + h]);
       }
       if (!ok) break;
       ok = tc::mbar_wait_warp(&o_full[x], o_phase, abort_flag);
@@ -436,11 +489,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
       for (int c = 0; c < DH; c += 32) {
         uint32_t w[32];
         tc::tmem_ld32(t_o + c, w);                          // the whole warp loads, valid rows store
-        if (!row_valid) continue;
-        if (split) {
+        if (row_valid && split) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(a.ws.o + part * DH + c + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-        } else {
+        } else if (row_valid) {
 #pragma unroll
           for (int i = 0; i < 32; i += 8) {
             uint4 w4;
@@ -451,6 +503,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
             *reinterpret_cast<uint4*>(a.o.out + dst * DH + c + i) = w4;
           }
         }
+        __syncwarp();
       }
       tc::tmem_fence_before();
       if (row_valid) {
@@ -461,8 +514,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         a.ws.rec[blockIdx.x] = SplitRec{walk.it.row0, walk.head * rep, walk.it.n_tok * rep,
                                         (walk.it.first + (walk.head + 1) * walk.it.n_tiles - 1) / plan.share - (int)blockIdx.x + 1};
     }
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CH_REGS_FEW));
   }
   // teardown
   __syncwarp();

@@ -283,6 +283,39 @@ __global__ void __launch_bounds__(MS_KEYS) mass_merge_kernel(MassWs ws, const fl
   out[at] = (in ? in[at] : 0.f) + sum;
 }
 
+// Sum over the 128 columns (rows of the chunk) of this thread's lane (key) of 2^(s scale - lse); MASKED: columns [lo, hi).
+template <bool MASKED, typename F>
+__device__ __forceinline__ float mass_columns(uint32_t ts, uint32_t ls, float scale_log2, int lo, int hi, F release) {
+  const uint64_t sc2 = t5::pack2(scale_log2, scale_log2);
+  uint64_t acc[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int c0 = 0; c0 < MS_ROWS; c0 += 64) {
+    uint32_t v[64];
+    tc::tmem_ld32_nowait(ts + c0, v);
+    tc::tmem_ld32_nowait(ts + c0 + 32, v + 32);
+    tc::tmem_ld_wait();
+    if (c0 + 64 == MS_ROWS) release();
+#pragma unroll
+    for (int c = 0; c < 64; c += 4) {
+      uint64_t l01, l23;                                               // two negated log-sums each
+      asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(l01), "=l"(l23) : "r"(ls + (c0 + c) * 4));
+      float p[4];
+      t5::unpack2(t5::fma2(t5::pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, l01), p[0], p[1]);
+      t5::unpack2(t5::fma2(t5::pack2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc2, l23), p[2], p[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = fa::ex2(p[e]);
+        if (MASKED && (c0 + c + e < lo || c0 + c + e >= hi)) p[e] = 0.f;
+      }
+      acc[(c >> 1) & 2] = t5::add2(acc[(c >> 1) & 2], t5::pack2(p[0], p[1]));
+      acc[((c >> 1) & 2) + 1] = t5::add2(acc[((c >> 1) & 2) + 1], t5::pack2(p[2], p[3]));
+    }
+  }
+  float x, y;
+  t5::unpack2(t5::add2(t5::add2(acc[0], acc[1]), t5::add2(acc[2], acc[3])), x, y);
+  return x + y;
+}
+
 template <int DH>
 __global__ void __launch_bounds__(MassCfg<DH>::THREADS, 1)
 mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, MassTcArgs a) {
@@ -291,14 +324,14 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   extern __shared__ uint8_t mc_raw[];
   uint8_t* sm = (uint8_t*)(((uintptr_t)mc_raw + 1023) & ~(uintptr_t)1023);
   const uint32_t sK = tc::smem_u32(sm), sQ = sK + 2 * Cfg::K_BYTES;
-  float* s_lse = (float*)(sm + 2 * Cfg::K_BYTES + NSQ * Cfg::Q_BYTES);       // [NSQ][128], log2 domain
+  float* s_lse = (float*)(sm + 2 * Cfg::K_BYTES + NSQ * Cfg::Q_BYTES);       // [NSQ][128], negated, log2 domain
   uint64_t* bars = (uint64_t*)(s_lse + NSQ * MS_ROWS);
   uint64_t *q_full = bars, *q_empty = bars + NSQ, *l_full = bars + 2 * NSQ;
   uint64_t *s_full = bars + 3 * NSQ, *s_free = s_full + 4, *k_full = s_full + 8, *k_free = s_full + 9;
   uint32_t* tmem_slot = (uint32_t*)(s_full + 10);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   int* s_first = (int*)(tmem_slot + 2);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hkv = a.kv.hkv, rep = a.rep, cols = a.tq * rep;
+  const int warp = (int)t5::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, hkv = a.kv.hkv, rep = a.rep, cols = a.tq * rep;
   const ChunkPlan plan = *a.plan;
   if (threadIdx.x == 0) {
     for (int i = 0; i < NSQ; ++i) { tc::mbar_init(&q_full[i], 1); tc::mbar_init(&q_empty[i], 1 + 8); tc::mbar_init(&l_full[i], 1); }
@@ -373,12 +406,12 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
           tc::mbar_expect_tx(&q_full[st], HALVES * cols * 128);
           for (int hf = 0; hf < HALVES; ++hf) t5::tma_load_3d(sQ + st * Cfg::Q_BYTES + hf * (MS_ROWS * 128), &q_map, hf * 64, head * rep, min(row, a.c.n_rows - 1), &q_full[st]);
         }
-        // log-sums of the tile's rows; columns without a row (their q is zero) get weight 0 from an infinite one, rows of
+        // log-sums of the tile's rows; columns without a row (their q is zero) get weight 0 from -inf, rows of
         // other chunks are masked later
 #pragma unroll
         for (int c = lane; c < MS_ROWS; c += 32) {
           const int rr = row + c / rep;
-          s_lse[st * MS_ROWS + c] = (c < cols && rr < sp.row0 + sp.rows) ? a.lse[(int64_t)rr * a.c.hq + head * rep + c % rep] * LOG2E_F : INFINITY;
+          s_lse[st * MS_ROWS + c] = (c < cols && rr < sp.row0 + sp.rows) ? a.lse[(int64_t)rr * a.c.hq + head * rep + c % rep] * -LOG2E_F : -INFINITY;
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&l_full[st]);
@@ -387,7 +420,7 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
     constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MS_ROWS >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-    const uint32_t dq = t5::desc_lo(sQ, 16), dk = t5::desc_lo(sK, 16);
+    const uint32_t dq = t5::uniform(t5::desc_lo(sQ, 16)), dk = t5::uniform(t5::desc_lo(sK, 16)), tm = t5::uniform(tmem);
     bool ok = true;
     int qt = 0, used[2] = {0, 0};                            // S buffers filled so far per sub-tile
     for (int seg = 0; ok && next(); ++seg) {
@@ -403,18 +436,18 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
           ok = tc::mbar_wait_warp(&s_free[x * 2 + b], ((used[x] >> 1) & 1) ^ 1, abort_flag);
           if (!ok) break;
           tc::tmem_fence_after();
-          if (lane == 0) {
+          if (t5::elect_one()) {
 #pragma unroll
             for (int i = 0; i < DH / 16; ++i) {
               const uint32_t off = (i >> 2) * (128 * 128 >> 4) + (i & 3) * 2;
-              t5::umma_ss(tmem + (x * 2 + b) * 128, dk + x * (Cfg::K_BYTES >> 4) + off, dq + st * (Cfg::Q_BYTES >> 4) + off, idesc, i > 0);
+              t5::umma_ss(tm + (x * 2 + b) * 128, dk + x * (Cfg::K_BYTES >> 4) + off, dq + st * (Cfg::Q_BYTES >> 4) + off, idesc, i > 0);
             }
             tc::umma_commit(&s_full[x * 2 + b]);
           }
           ++used[x];
         }
         if (!ok) break;
-        if (lane == 0) { tc::umma_commit(&q_empty[st]); if (t + 1 == t1) tc::umma_commit(k_free); }
+        if (t5::elect_one()) { tc::umma_commit(&q_empty[st]); if (t + 1 == t1) tc::umma_commit(k_free); }
       }
     }
   } else if (warp >= 4) {
@@ -444,32 +477,13 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
           int end = max(0, n_tok);
           if (a.c.window > 0 && j >= a.c.sinks) end = (int)max((int64_t)0, min((int64_t)end, (int64_t)j + a.c.window - pt));
           const int hi = end * rep;
-          float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int c0 = 0; c0 < MS_ROWS; c0 += 64) {
-            uint32_t v[64];
-            tc::tmem_ld32_nowait(t_s + b * 128 + c0, v);
-            tc::tmem_ld32_nowait(t_s + b * 128 + c0 + 32, v + 32);
-            tc::tmem_ld_wait();
-            if (c0 + 64 == MS_ROWS) {
-              tc::tmem_fence_before();
-              __syncwarp();
-              if (lane == 0) tc::mbar_arrive(&s_free[x * 2 + b]);
-            }
-            const float4* ls = reinterpret_cast<const float4*>(s_lse + st * MS_ROWS + c0);
-#pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-              const float4 l4 = ls[c >> 2];
-              float p[4] = {fa::ex2(fmaf(__uint_as_float(v[c]), a.scale_log2, -l4.x)), fa::ex2(fmaf(__uint_as_float(v[c + 1]), a.scale_log2, -l4.y)),
-                            fa::ex2(fmaf(__uint_as_float(v[c + 2]), a.scale_log2, -l4.z)), fa::ex2(fmaf(__uint_as_float(v[c + 3]), a.scale_log2, -l4.w))};
-              if (!whole)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) if (c0 + c + e < lo || c0 + c + e >= hi) p[e] = 0.f;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[e] += p[e];
-            }
-          }
-          sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+          const uint32_t ts = t_s + b * 128, ls = tc::smem_u32(s_lse + st * MS_ROWS);
+          auto release = [&]() {
+            tc::tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&s_free[x * 2 + b]);
+          };
+          sum += whole ? mass_columns<false>(ts, ls, a.scale_log2, 0, 0, release) : mass_columns<true>(ts, ls, a.scale_log2, lo, hi, release);
         } else {
           // (the slot's log-sums are not read, but its release counts every warp: wait until it is filled)
           ok = tc::mbar_wait_warp(&l_full[st], (qt / NSQ) & 1, abort_flag);

@@ -32,46 +32,70 @@ struct AttnOut { T* out; float* lse; int hq, rep; };
 
 constexpr float LN2_F = 0.69314718055994531f;
 
-// One warp per row of an item: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p over the item's pieces, in order.
+// o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p over an item's pieces.  A CTA per (item, rows): its eight warps
+// take the pieces in turn (piece p: warp p mod 8), four loads in flight each, and are added up in warp order.
 template <typename T, int DH>
-__global__ void __launch_bounds__(128) split_merge_kernel(SplitWs ws, AttnOut<T> a) {
-  constexpr int DPL = DH / 32;
+__global__ void __launch_bounds__(256) split_merge_kernel(SplitWs ws, AttnOut<T> a) {
+  constexpr int DPL = DH / 32, W = 8;
+  __shared__ float s_o[W][DH];
+  __shared__ float s_l[W];
   const SplitRec rec = ws.rec[blockIdx.x];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.x;
   if (rec.n_parts == 0) return;
-  for (int r = blockIdx.y * 4 + warp; r < rec.rows; r += gridDim.y * 4) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.x;
+  // few pieces: a warp per row.  Many: the warps of the CTA share a row's pieces.
+  const bool shared_row = rec.n_parts > 8;
+  const int step = shared_row ? W : 1;
+  for (int r = shared_row ? blockIdx.y : blockIdx.y * W + warp; r < rec.rows; r += shared_row ? gridDim.y : gridDim.y * W) {
     auto slot = [&](int p) -> int64_t { return (int64_t)(p == 0 ? 2 * b + 1 : 2 * (b + p)) * ws.rows_cap + r; };
     float m = -INFINITY;
     for (int p = lane; p < rec.n_parts; p += 32) m = fmaxf(m, ws.ml[slot(p)].x);
     m = warp_max(m);
     const float mu = m == -INFINITY ? 0.f : m;
     float l = 0.f, acc[DPL];
-  #pragma unroll
+#pragma unroll
     for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
-    for (int p0 = 0; p0 < rec.n_parts; p0 += 32) {
-      const int mine = p0 + lane;
-      float w = 0.f, lp = 0.f;
-      if (mine < rec.n_parts) { const float2 ml = ws.ml[slot(mine)]; w = fa::ex2(ml.x - mu); lp = w * ml.y; }
-      const int n = min(32, rec.n_parts - p0);
-  #pragma unroll 4
-      for (int p = 0; p < n; ++p) {
-        const float wp = __shfl_sync(0xffffffffu, w, p);
-        const float* o = ws.o + slot(p0 + p) * DH + lane * DPL;
-        l += __shfl_sync(0xffffffffu, lp, p);
-        if (DPL == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(o);
-          acc[0] = fmaf(wp, x.x, acc[0]); acc[1] = fmaf(wp, x.y, acc[1]); acc[DPL - 2] = fmaf(wp, x.z, acc[DPL - 2]); acc[DPL - 1] = fmaf(wp, x.w, acc[DPL - 1]);
-        } else {
-          const float2 x = *reinterpret_cast<const float2*>(o);
-          acc[0] = fmaf(wp, x.x, acc[0]); acc[1] = fmaf(wp, x.y, acc[1]);
-        }
+    for (int p0 = shared_row ? warp : 0; p0 < rec.n_parts; p0 += 4 * step) {
+      float x[4][DPL];
+      float2 ml[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bool v = p0 + u * step < rec.n_parts;
+        ml[u] = v ? ws.ml[slot(p0 + u * step)] : make_float2(-INFINITY, 0.f);
+        const float* o = ws.o + slot(v ? p0 + u * step : p0) * DH + lane * DPL;
+#pragma unroll
+        for (int i = 0; i < DPL; i += 2) { const float2 y = *reinterpret_cast<const float2*>(o + i); x[u][i] = y.x; x[u][i + 1] = y.y; }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float w = fa::ex2(ml[u].x - mu);
+        l = fmaf(w, ml[u].y, l);
+#pragma unroll
+        for (int i = 0; i < DPL; ++i) acc[i] = fmaf(w, x[u][i], acc[i]);
       }
     }
     const int64_t dst = (int64_t)(rec.row0 + r / a.rep) * a.hq + rec.head0 + r % a.rep;
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
-  #pragma unroll
-    for (int i = 0; i < DPL; ++i) a.out[dst * DH + lane * DPL + i] = from_f32<T>(acc[i] * inv);
-    if (lane == 0 && a.lse) a.lse[dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
+    if (shared_row) {
+#pragma unroll
+      for (int i = 0; i < DPL; ++i) s_o[warp][lane * DPL + i] = acc[i];
+      if (lane == 0) s_l[warp] = l;
+      __syncthreads();
+      l = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) l += s_l[w];
+      if ((int)threadIdx.x < DH) {
+        float o = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) o += s_o[w][threadIdx.x];
+        a.out[dst * DH + threadIdx.x] = from_f32<T>(l > 0.f ? o / l : 0.f);
+      }
+      if (threadIdx.x == 0 && a.lse) a.lse[dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
+      __syncthreads();
+    } else {
+      const float inv = l > 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+      for (int i = 0; i < DPL; ++i) a.out[dst * DH + lane * DPL + i] = from_f32<T>(acc[i] * inv);
+      if (lane == 0 && a.lse) a.lse[dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
+    }
   }
 }
 
