@@ -10,8 +10,9 @@
 //                    pages: 16 x 64 boxes), accumulator in tensor memory, one buffer per half
 //   softmax          one warpgroup per sub-tile, one thread per row = TMEM lane: no shuffles, no exchange.  P = 2^(s - m)
 //                    goes back to tensor memory as bf16, over the S it came from
-//   O_x += P V       tcgen05.mma with A = P from tensor memory; accumulates over all tiles.  m is a reference that moves
-//                    only when the running maximum outgrows it by 2^8: then the row's O is rescaled in place.
+//   O_x += P V       tcgen05.mma with A = P from tensor memory; accumulates over all tiles.  m is a reference, not
+//                    the running maximum: it moves (and the row's O is rescaled in place) only when a half's sum
+//                    outgrows 10^12, so halves without masked keys take no maximum at all.
 //
 // S of a half is refilled as soon as P V of the same half of the tile before has been issued, so a softmax warp that
 // hands over one half finds the next one ready: with 128-key halves (S waits for the softmax of the whole tile before)
@@ -27,7 +28,7 @@ namespace rpo {
 constexpr int CH_BM = 128, CH_BN = 128;
 constexpr int64_t OP_MAX_TILES = ((int64_t)1 << 31) - (1 << 20);
 constexpr int CH_HALF = CH_BN / 2;
-constexpr float CH_LAZY = 8.0f;                // log2 of the largest P entry tolerated before the reference maximum moves
+constexpr float CH_MOST = 1.0e12f;             // largest sum of a half's P that is taken without moving the reference
 
 struct ChunkItem { int first, n_tiles, row0, n_tok; int seq, p0, pad0, pad1; };   // p0: position of the item's first token
 struct ChunkPlan { int n_items, total, share, pad; };                        // `first`, `total`: in (tile, KV head)s
@@ -182,7 +183,6 @@ __device__ __forceinline__ uint64_t pack2(float x, float y) { uint64_t r; asm("m
 __device__ __forceinline__ void unpack2(uint64_t r, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const void* map, int x, int y, int z, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -194,6 +194,24 @@ __device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const void* map, 
       ::"r"(smem_dst), "l"(map), "r"(tc::smem_u32(bar)), "r"(x), "r"(y) : "memory");
 }
 }  // namespace t5
+
+// P = 2^(s scale - m) of one row's half, packed to 16 bits in v[0 .. 31]; returns the sum of the unrounded values.  Two
+// scores at a time: packed multiply-add, two exponentials, packed sum.
+__device__ __forceinline__ float chunk_exp(uint32_t* v, float scale_log2, float m) {
+  const uint64_t sc2 = t5::pack2(scale_log2, scale_log2), mu2 = t5::pack2(-m, -m);
+  uint64_t ps[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int c = 0; c < CH_HALF; c += 2) {
+    float p0, p1;
+    t5::unpack2(t5::fma2(t5::pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, mu2), p0, p1);
+    p0 = fa::ex2(p0); p1 = fa::ex2(p1);
+    ps[(c >> 1) & 3] = t5::add2(ps[(c >> 1) & 3], t5::pack2(p0, p1));
+    v[c >> 1] = fa::pack_bf16(p0, p1);
+  }
+  float x0, x1;
+  t5::unpack2(t5::add2(t5::add2(ps[0], ps[1]), t5::add2(ps[2], ps[3])), x0, x1);
+  return x0 + x1;
+}
 
 template <int DH>
 __global__ void __launch_bounds__(ChunkCfg<DH>::THREADS, 1)
@@ -409,6 +427,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
       const int p_lo = p_item + x * a.tq, p_hi = min(p1, p_lo + a.tq - 1);     // positions of my sub-tile
       const int p = min(p_lo + tok, p_hi);
       float m = -INFINITY, l = 0.f;
+      bool have_m = false;                                   // every row of the warp has a reference maximum
       for (int u = 2 * walk.t0; u < 2 * walk.t1; ++u, ++steps) {
         const int h = u & 1, key0 = kt_of.page0(u >> 1) * KV_BLOCK + h * CH_HALF;
         const bool first_range = (u >> 1) < kt_of.n1;
@@ -423,54 +442,54 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         tc::tmem_ld_wait();
         const bool whole = key0 + CH_HALF - 1 <= (first_range ? min(p_lo, a.c.sinks - 1) : p_lo) &&
                            (a.c.window <= 0 || key0 > p_hi - a.c.window || key0 + CH_HALF <= a.c.sinks);
-        if (!whole) {
-          const int hi = (first_range ? min(p, a.c.sinks - 1) : p) - key0;
-          const int lo = a.c.window > 0 ? p - a.c.window + 1 - key0 : -key0, sk = a.c.sinks - key0;
-#pragma unroll
-          for (int c = 0; c < CH_HALF; ++c) if (c > hi || (c < lo && c >= sk)) v[c] = 0xFF800000u;
-        }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int c = 0; c < CH_HALF; c += 2) mx[(c >> 1) & 3] = t5::max3(mx[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
-        const bool move = mt > m + CH_LAZY || (m == -INFINITY && mt > -INFINITY);
-        if (__any_sync(0xffffffffu, move)) {
-          const float factor = move ? (m == -INFINITY ? 0.f : fa::ex2(m - mt)) : 1.f;
-          if (u > 2 * walk.t0) {
-            // O is at rest once P V of the half before is done.  (This half's S was issued behind the P V of two halves
-            // ago, so at most that one phase is outstanding and its parity cannot be taken for an older one.)
-            ok = tc::mbar_wait_warp(&pv_done[x], (steps - 1) & 1, abort_flag);
-            if (!ok) break;
-            tc::tmem_fence_after();
-#pragma unroll
-            for (int c = 0; c < DH; c += 32) {
-              uint32_t w[32];
-              tc::tmem_ld32(t_o + c, w);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * factor);
-              t5::tmem_st32_nowait(t_o + c, w);
-            }
+        // All keys seen and every row has a reference: no maximum is needed, any reference is exact as long as nothing
+        // overflows, and the half's sum tells.  (S stays in tensor memory until P is stored over it.)
+        bool done = false;
+        if (whole && have_m) {
+          const float ps = chunk_exp(v, a.scale_log2, m);
+          done = __all_sync(0xffffffffu, ps < CH_MOST || !row_valid);
+          if (done) l += ps;
+          else {
+            tc::tmem_ld32_nowait(ts, v);
+            tc::tmem_ld32_nowait(ts + 32, v + 32);
+            tc::tmem_ld_wait();
           }
-          if (move) { l *= factor; m = mt; }
         }
-        const float mu = m == -INFINITY ? 0.f : m;
-        // two scores at a time: 2^(s scale - m) as packed multiply-add, two exponentials, packed sum
-        const uint64_t sc2 = t5::pack2(a.scale_log2, a.scale_log2), mu2 = t5::pack2(-mu, -mu);
-        uint64_t ps[4] = {0, 0, 0, 0};
+        if (!done) {
+          if (!whole) {
+            const int hi = (first_range ? min(p, a.c.sinks - 1) : p) - key0;
+            const int lo = a.c.window > 0 ? p - a.c.window + 1 - key0 : -key0, sk = a.c.sinks - key0;
 #pragma unroll
-        for (int c = 0; c < CH_HALF; c += 2) {
-          float p0, pb;
-          t5::unpack2(t5::fma2(t5::pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, mu2), p0, pb);
-          p0 = fa::ex2(p0); pb = fa::ex2(pb);
-          ps[(c >> 1) & 3] = t5::add2(ps[(c >> 1) & 3], t5::pack2(p0, pb));
-          v[c >> 1] = fa::pack_bf16(p0, pb);
+            for (int c = 0; c < CH_HALF; ++c) if (c > hi || (c < lo && c >= sk)) v[c] = 0xFF800000u;
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < CH_HALF; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(v[c]));
+          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+          const bool move = mt > m;
+          if (__any_sync(0xffffffffu, move)) {
+            const float factor = move ? (m == -INFINITY ? 0.f : fa::ex2(m - mt)) : 1.f;
+            if (u > 2 * walk.t0) {
+              // O is at rest once P V of the half before is done.  (This half's S was issued behind the P V of two
+              // halves ago, so at most that one phase is outstanding and its parity cannot be taken for an older one.)
+              ok = tc::mbar_wait_warp(&pv_done[x], (steps - 1) & 1, abort_flag);
+              if (!ok) break;
+              tc::tmem_fence_after();
+#pragma unroll
+              for (int c = 0; c < DH; c += 32) {
+                uint32_t w[32];
+                tc::tmem_ld32(t_o + c, w);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * factor);
+                t5::tmem_st32_nowait(t_o + c, w);
+              }
+            }
+            if (move) { l *= factor; m = mt; }
+            have_m = __all_sync(0xffffffffu, m > -INFINITY || !row_valid);
+          }
+          l += chunk_exp(v, a.scale_log2, m == -INFINITY ? 0.f : m);
         }
         t5::tmem_st32_nowait(ts, v);
-        {
-          float x0, x1;
-          t5::unpack2(t5::add2(t5::add2(ps[0], ps[1]), t5::add2(ps[2], ps[3])), x0, x1);
-          l += x0 + x1;
-        }
         t5::tmem_st_wait();
         tc::tmem_fence_before();
         __syncwarp();
