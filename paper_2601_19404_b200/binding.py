@@ -76,14 +76,11 @@ class PagedKV:
         _expect(d_block_table, "d_block_table", "int32", (d_lens.shape[0], d_block_table.shape[-1]))
         _expect(d_lens, "d_lens", "int32", (d_block_table.shape[0],))
         self.d_k, self.d_v, self.d_block_table, self.d_lens = d_k, d_v, d_block_table, d_lens
+        self.dtype = d_k.dtype
         hkv, n_blocks, _, dh = d_k.shape
         self.struct = _PagedKVStruct(_ptr(d_k), _ptr(d_v), _ptr(d_block_table), _ptr(d_lens), n_blocks, d_block_table.shape[0],
                                      d_block_table.shape[1], hkv, dh)
         self.ref = C.byref(self.struct)
-
-    @property
-    def dtype(self):
-        return self.d_k.dtype
 
 
 def load_library(path=None):
@@ -163,19 +160,32 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_DTYPES = {}
+
+
+def _dtype(name):
+    """torch.<name>, looked up once (torch is imported with the first tensor, not with this module)."""
+    if name not in _DTYPES:
+        import torch
+        _DTYPES[name] = getattr(torch, name)
+    return _DTYPES[name]
+
+
 def _expect(t, name, dtype, shape):
     """Refuse a tensor of another type, shape or layout than a call takes."""
-    if str(t.dtype) != "torch." + dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not _dtype(dtype) or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
 def _head_rows(t, name, dtype, heads, dh, n_rows=None):
     """Elements between the rows of a [rows, heads, head_dim] view whose rows are contiguous (a slice of a fused projection is)."""
-    if t.dim() != 3 or t.dtype != dtype or t.shape[1:] != (heads, dh) or (n_rows is not None and t.shape[0] != n_rows):
-        raise ValueError(f"{name} must be {dtype} [{'rows' if n_rows is None else n_rows}, {heads}, {dh}], got {t.dtype} {tuple(t.shape)}")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dh):
+    shape = t.shape
+    if len(shape) != 3 or t.dtype is not dtype or shape[1] != heads or shape[2] != dh or (n_rows is not None and shape[0] != n_rows):
+        raise ValueError(f"{name} must be {dtype} [{'rows' if n_rows is None else n_rows}, {heads}, {dh}], got {t.dtype} {tuple(shape)}")
+    stride = t.stride()
+    if stride[2] != 1 or (heads > 1 and stride[1] != dh):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else heads * dh
+    return stride[0] if shape[0] > 1 else heads * dh
 
 
 def _check(rc, what):
@@ -320,7 +330,7 @@ class Context:
         return ms.value
 
     def _paged_dtype(self, kv):
-        if (str(kv.dtype) == "torch.bfloat16") != (self.shape.dtype == 1) or str(kv.dtype) not in ("torch.bfloat16", "torch.float32"):
+        if kv.dtype is not _dtype("bfloat16" if self.shape.dtype == 1 else "float32"):
             raise ValueError(f"a cache of {kv.dtype} needs a context of that storage type")
         return kv.dtype
 
@@ -341,7 +351,7 @@ class Context:
             if _head_rows(d_v_new, "d_v_new", dt, st.n_kv_heads, st.head_dim, n) != new_stride:
                 raise ValueError("d_k_new and d_v_new must have the same row stride")
         _expect(d_q_offsets, "d_q_offsets", "int32", (st.n_seqs + 1,))
-        if d_out.dtype != dt or d_out.shape != d_q.shape or not d_out.is_contiguous():
+        if d_out.dtype is not dt or d_out.shape != d_q.shape or not d_out.is_contiguous():
             raise ValueError("d_out must be contiguous, of d_q's type and shape")
         if d_lse_out is not None:
             _expect(d_lse_out, "d_lse_out", "float32", (n, hq))

@@ -226,16 +226,23 @@ extern "C" int rpo_attention_mass(rpo_ctx* c, const rpo_paged_kv* kv, int32_t n_
 #undef ATTN_MASS
 }
 
-template <typename T, int DH>
-static int evict_cache_t(rpo_ctx* c, const rpo_paged_kv* kv, const EvictArgs& a) {
-  const size_t smem = evict_smem_bytes(a.mass_stride, a.budget);
+template <int THREADS, int KPT, int C>
+static int evict_launch(rpo_ctx* c, EvictArgs a) {
   static bool attr_done[64] = {};
   if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)evict_smem_bytes(EV_MAX_STRIDE, EV_MAX_STRIDE)));
-  const int n = a.n_seqs * a.hkv;
-  LAUNCH_OP(c, evict_select_kernel, n, EV_THREADS, smem, a);
-  const dim3 grid(std::min(ceil_div(a.budget, 8), std::max(1, 148 * 16 / n)), n);
-  LAUNCH_OP(c, (evict_move_kernel<T, DH>), grid, 256, 0, paged_view<T>(c, kv), a);
+    CUDA_TRY(cudaFuncSetAttribute(evict_kernel<THREADS, KPT, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (EV_MAX_STRIDE / 2 / 8 + 1) * 4));
+  a.list_cap = ceil_div(std::max(1, std::min(a.budget, a.mass_stride / 2 + 1)), C);     // holes: at most half of the slots
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.n_seqs * a.hkv * C); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = (size_t)a.list_cap * 4; cfg.stream = c->stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = C > 1 ? 1 : 0;
+  prof_begin(c, "evict_kernel");
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, evict_kernel<THREADS, KPT, C>, a);
+  prof_end(c);
+  c->launches++;
+  CUDA_TRY(e);
   return RPO_OK;
 }
 
@@ -253,6 +260,15 @@ extern "C" int rpo_evict_cache(rpo_ctx* c, const rpo_paged_kv* kv, const float* 
   a.lens = kv->d_lens; a.mass = d_mass; a.pos = d_positions; a.lens_out = d_lens_out; a.src = d_src_out; a.mass_out = d_mass_out;
   a.pos_out = d_positions_out; a.mass_stride = mass_stride; a.out_stride = out_stride; a.n_seqs = kv->n_seqs; a.hkv = kv->n_kv_heads;
   a.table_stride = kv->table_stride; a.budget = budget; a.sinks = sinks; a.recent = recent; a.status = c->d_status;
-  if (c->bf16) return kv->head_dim == 128 ? evict_cache_t<bf16, 128>(c, kv, a) : evict_cache_t<bf16, 64>(c, kv, a);
-  return kv->head_dim == 128 ? evict_cache_t<float, 128>(c, kv, a) : evict_cache_t<float, 64>(c, kv, a);
+  a.k = (uint8_t*)kv->d_k; a.v = (uint8_t*)kv->d_v; a.table = kv->d_block_table; a.n_blocks = kv->n_blocks;
+  a.row_bytes = kv->head_dim * (int)c->esz; a.head_bytes = (int64_t)kv->n_blocks * KV_BLOCK * a.row_bytes;
+  a.write_lens = d_lens_out != kv->d_lens; a.list_cap = 0;
+  // Registers hold 8 or 16 slots a thread; few slots take a small CTA, so that more (sequence, KV head)s run at once (four
+  // CTAs of 256 or two of 512 threads fit an SM: 256 caches of up to 6144 slots took 90 us with 1024 threads).
+  if (mass_stride <= 2048) RPO_TRY((evict_launch<256, 8, 1>(c, a)));
+  else if (mass_stride <= 8192) RPO_TRY((evict_launch<512, 16, 1>(c, a)));
+  else if (mass_stride <= 8 * 1024 * 16) RPO_TRY((evict_launch<1024, 16, 8>(c, a)));
+  else RPO_TRY((evict_launch<1024, 0, 8>(c, a)));
+  if (!a.write_lens) LAUNCH_OP(c, evict_lens_kernel, ceil_div(a.n_seqs, 256), 256, 0, a);
+  return RPO_OK;
 }
