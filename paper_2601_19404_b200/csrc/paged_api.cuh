@@ -124,6 +124,28 @@ static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   return RPO_OK;
 }
 
+// 32-bit storage: BM rows of an item against tiles of keys on CUDA cores.
+template <int DH, int BM>
+static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& a, const float* q, int64_t q_stride, float scale, float* out, float* lse) {
+  using Cfg = F32Cfg<DH, BM>;
+  static bool attr_done[64] = {};
+  if (tc_first_use_on_device(c, attr_done))
+    CUDA_TRY(cudaFuncSetAttribute(paged_f32_kernel<DH, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+  F32Args f;
+  f.kv = view; f.c = a; f.q = q; f.q_stride = q_stride; f.scale_log2 = scale * 1.4426950408889634f;
+  f.o.out = out; f.o.lse = lse; f.o.hq = a.hq; f.o.rep = a.hq / view.hkv; f.ws = split_ws(c, BM);
+  f.tok = BM / f.o.rep;
+  if ((int64_t)a.n_rows / f.tok + view.n_seqs > OP_MAX_ITEMS) return RPO_ERR_LIMIT;
+  ChunkItem* items = (ChunkItem*)c->ws.op_items;
+  ChunkPlan* plan = (ChunkPlan*)(items + OP_MAX_ITEMS);
+  f.items = items; f.plan = plan;
+  const int grid = std::min(Cfg::CTAS * c->sm_count, OP_GRID * c->sm_count);
+  LAUNCH_OP(c, (chunk_plan_kernel<float, Cfg::BN / KV_BLOCK>), 1, 1024, view.n_seqs * 4, view, a, f.tok, grid, 2, items, plan);
+  LAUNCH_OP(c, (paged_f32_kernel<DH, BM>), grid, 256, Cfg::SMEM, f);
+  LAUNCH_OP(c, (split_merge_kernel<float, DH>), dim3(grid, BM == 64 ? 8 : std::min(a.max_chunk * f.o.rep, BM)), 256, 0, f.ws, f.o);
+  return RPO_OK;
+}
+
 template <typename T, int DH>
 static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs& a, const void* q, int64_t q_stride, const void* k_new,
                              const void* v_new, int64_t new_stride, float scale, void* out, float* lse) {
@@ -132,13 +154,15 @@ static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs
     const int64_t n = (int64_t)a.n_rows * view.hkv * 2 * (DH * sizeof(T) / 16);
     LAUNCH_OP(c, (paged_append_kernel<T, DH>), grid_for(n, 256), 256, 0, view, a, (const T*)k_new, (const T*)v_new, new_stride);
   }
+  const int64_t rows = a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads);           // of the longest chunk, per KV head
   if constexpr (std::is_same<T, bf16>::value) {
-    if (a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads) <= 16) return chunk_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
-    if (a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads) <= 32) return chunk_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
+    if (rows <= 16) return chunk_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
+    if (rows <= 32) return chunk_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
     return chunk_tiles<DH>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
+  } else {
+    if (rows <= 16) return chunk_f32<DH, 16>(c, view, a, (const float*)q, q_stride, scale, (float*)out, lse);
+    return chunk_f32<DH, 64>(c, view, a, (const float*)q, q_stride, scale, (float*)out, lse);
   }
-  LAUNCH_OP(c, (paged_attn_simple_kernel<T, DH>), ceil_div((int64_t)a.n_rows * a.hq, 4), 128, 0, view, a, (const T*)q, q_stride, scale, (T*)out, lse);
-  return RPO_OK;
 }
 
 extern "C" int rpo_chunk_attention(rpo_ctx* c, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_chunk, const void* d_q,
@@ -195,20 +219,34 @@ static int mass_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& 
   return RPO_OK;
 }
 
+template <int DH, int BM>
+static int mass_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& a, const float* q, int64_t q_stride, const float* lse, float scale,
+                    const float* in, float* out, int stride) {
+  constexpr int smem = ((MF_KEYS + BM) * (DH + 4) + BM) * 4;
+  static bool attr_done[64] = {};
+  if (tc_first_use_on_device(c, attr_done))
+    CUDA_TRY(cudaFuncSetAttribute(mass_f32_kernel<DH, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  MassF32Args m;
+  m.kv = view; m.c = a; m.q = q; m.q_stride = q_stride; m.scale_log2 = scale * 1.4426950408889634f; m.lse = lse; m.in = in; m.out = out;
+  m.stride = stride; m.rep = a.hq / view.hkv;
+  const dim3 grid(ceil_div(std::min((int64_t)stride, (int64_t)view.table_stride * KV_BLOCK), MF_KEYS), view.hkv, view.n_seqs);
+  LAUNCH_OP(c, (mass_f32_kernel<DH, BM>), grid, 256, smem, m);
+  return RPO_OK;
+}
+
 template <typename T, int DH>
 static int attention_mass_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs& a, const void* q, int64_t q_stride, const float* lse, float scale,
-                            const float* mass_in, float* mass_out, int mass_stride) {
+                            const float* in, float* out, int stride) {
   const PagedView<T> view = paged_view<T>(c, kv);
+  const int64_t rows = a.n_rows == 0 ? 0 : a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads);
   if constexpr (std::is_same<T, bf16>::value) {
-    const int rep = a.hq / kv->n_kv_heads;
-    if (a.n_rows == 0 || a.max_chunk * (int64_t)rep <= 16)
-      return mass_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, lse, scale, mass_in, mass_out, mass_stride);
-    if (a.max_chunk * (int64_t)rep <= 32) return mass_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, lse, scale, mass_in, mass_out, mass_stride);
-    return mass_tiles<DH>(c, view, a, (const bf16*)q, q_stride, lse, scale, mass_in, mass_out, mass_stride);
+    if (rows <= 16) return mass_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, lse, scale, in, out, stride);
+    if (rows <= 32) return mass_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, lse, scale, in, out, stride);
+    return mass_tiles<DH>(c, view, a, (const bf16*)q, q_stride, lse, scale, in, out, stride);
+  } else {
+    if (rows <= 16) return mass_f32<DH, 16>(c, view, a, (const float*)q, q_stride, lse, scale, in, out, stride);
+    return mass_f32<DH, 64>(c, view, a, (const float*)q, q_stride, lse, scale, in, out, stride);
   }
-  const dim3 grid(ceil_div(std::min((int64_t)mass_stride, (int64_t)view.table_stride * KV_BLOCK), MASS_KEYS), view.hkv, view.n_seqs);
-  LAUNCH_OP(c, (paged_mass_simple_kernel<T, DH>), grid, MASS_KEYS, 0, view, a, (const T*)q, q_stride, lse, scale, mass_in, mass_out, mass_stride);
-  return RPO_OK;
 }
 
 extern "C" int rpo_attention_mass(rpo_ctx* c, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_chunk, const void* d_q,

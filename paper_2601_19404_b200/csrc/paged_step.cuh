@@ -30,7 +30,7 @@ struct SplitWs {
 template <typename T>
 struct AttnOut { T* out; float* lse; int hq, rep; };
 
-constexpr float LN2_F = 0.69314718055994531f;
+constexpr float LN2_F = 0.69314718055994531f, LOG2E_F = 1.44269504088896341f;
 
 // o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p over an item's pieces.  A CTA per (item, rows): its eight warps
 // take the pieces in turn (piece p: warp p mod 8), four loads in flight each, and are added up in warp order.

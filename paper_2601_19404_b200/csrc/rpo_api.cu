@@ -21,8 +21,8 @@
 #include "gemm_tc2.cuh"
 #include "kernels.cuh"
 #include "objective.cuh"
-#include "paged_attn.cuh"
 #include "paged_chunk.cuh"
+#include "paged_f32.cuh"
 #include "paged_mass.cuh"
 #include "paged_step.cuh"
 #include "ref_kernels.cuh"
@@ -332,7 +332,7 @@ extern "C" int rpo_create(rpo_ctx** out, const rpo_shape* shape, const rpo_limit
   const size_t op_rows = (size_t)2 * c->sm_count * OP_PART_ROWS;   // two parts of OP_PART_ROWS rows per SM
   ALLOC(w.op_part_o, op_rows * 128 * 4);
   ALLOC(w.op_part_ml, op_rows * sizeof(float2));
-  ALLOC(w.op_rec, (size_t)2 * c->sm_count * sizeof(SplitRec));
+  ALLOC(w.op_rec, (size_t)OP_GRID * c->sm_count * sizeof(SplitRec));
   ALLOC(w.op_items, (size_t)OP_MAX_ITEMS * sizeof(ChunkItem) + sizeof(ChunkPlan));
   if (rc == RPO_OK && cudaMemsetAsync(w.tile_ctr, 0, (size_t)TC_CTR_CAPACITY * 4, c->stream) != cudaSuccess) { cudaGetLastError(); rc = RPO_ERR_CUDA; }
   if (rc == RPO_OK) rc = tc_create(c);
