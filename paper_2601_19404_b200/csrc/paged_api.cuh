@@ -62,17 +62,18 @@ static SplitWs split_ws(rpo_ctx* c, int rows_cap) {
 
 // Few rows per sequence (decode steps): one CTA pair per SM over an equal share of all pages.
 template <int DH, int MT>
-static int chunk_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, float scale, bf16* out, float* lse) {
+static int chunk_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const bf16* k_new, const bf16* v_new,
+                       int64_t new_stride, float scale, bf16* out, float* lse) {
   using Cfg = StepCfg<DH, MT>;
   static bool attr_done[64] = {};
   if (tc_first_use_on_device(c, attr_done))
     CUDA_TRY(cudaFuncSetAttribute(paged_step_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4));
   const int grid = 2 * c->sm_count;
   StepArgs s;
-  s.kv = view; s.c = a; s.q = q; s.q_stride = q_stride; s.scale_log2 = scale * 1.4426950408889634f;
+  s.kv = view; s.c = a; s.q = q; s.q_stride = q_stride; s.k_new = k_new; s.v_new = v_new; s.new_stride = new_stride; s.scale_log2 = scale * 1.4426950408889634f;
   s.o.out = out; s.o.lse = lse; s.o.hq = a.hq; s.o.rep = a.hq / view.hkv; s.ws = split_ws(c, Cfg::ROWS); s.min_share = 4;
   LAUNCH_OP(c, (paged_step_kernel<DH, MT>), grid, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, s);
-  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(grid, std::min(a.max_chunk * s.o.rep, Cfg::ROWS)), 256, 0, s.ws, s.o);
+  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(grid, std::min(a.max_chunk * s.o.rep, Cfg::ROWS)), MERGE_WARPS * 32, 0, s.ws, s.o);
   return RPO_OK;
 }
 
@@ -120,7 +121,7 @@ static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   RPO_TRY(op_map_pages(c, &vm, view, view.v, DH));
   LAUNCH_OP(c, (chunk_plan_kernel<bf16, CH_BN / KV_BLOCK>), 1, 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4, items, plan);
   LAUNCH_OP(c, (paged_chunk_kernel<DH>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
-  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, 16), 256, 0, t.ws, t.o);
+  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, 16), MERGE_WARPS * 32, 0, t.ws, t.o);
   return RPO_OK;
 }
 
@@ -142,7 +143,7 @@ static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& 
   const int grid = std::min(Cfg::CTAS * c->sm_count, OP_GRID * c->sm_count);
   LAUNCH_OP(c, (chunk_plan_kernel<float, Cfg::BN / KV_BLOCK>), 1, 1024, view.n_seqs * 4, view, a, f.tok, grid, 2, items, plan);
   LAUNCH_OP(c, (paged_f32_kernel<DH, BM>), grid, 256, Cfg::SMEM, f);
-  LAUNCH_OP(c, (split_merge_kernel<float, DH>), dim3(grid, BM == 64 ? 8 : std::min(a.max_chunk * f.o.rep, BM)), 256, 0, f.ws, f.o);
+  LAUNCH_OP(c, (split_merge_kernel<float, DH>), dim3(grid, BM == 64 ? 8 : std::min(a.max_chunk * f.o.rep, BM)), MERGE_WARPS * 32, 0, f.ws, f.o);
   return RPO_OK;
 }
 
@@ -150,14 +151,16 @@ template <typename T, int DH>
 static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs& a, const void* q, int64_t q_stride, const void* k_new,
                              const void* v_new, int64_t new_stride, float scale, void* out, float* lse) {
   const PagedView<T> view = paged_view<T>(c, kv);
-  if (k_new) {
+  const int64_t rows = a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads);           // of the longest chunk, per KV head
+  const bool steps = c->bf16 && rows <= 32;
+  if (k_new && !steps) {                                     // (the kernel of decode steps writes them itself)
     const int64_t n = (int64_t)a.n_rows * view.hkv * 2 * (DH * sizeof(T) / 16);
     LAUNCH_OP(c, (paged_append_kernel<T, DH>), grid_for(n, 256), 256, 0, view, a, (const T*)k_new, (const T*)v_new, new_stride);
   }
-  const int64_t rows = a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads);           // of the longest chunk, per KV head
   if constexpr (std::is_same<T, bf16>::value) {
-    if (rows <= 16) return chunk_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
-    if (rows <= 32) return chunk_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
+    if (steps)
+      return rows <= 16 ? chunk_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse)
+                        : chunk_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
     return chunk_tiles<DH>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
   } else {
     if (rows <= 16) return chunk_f32<DH, 16>(c, view, a, (const float*)q, q_stride, scale, (float*)out, lse);
@@ -193,7 +196,7 @@ static int mass_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& 
   MassArgs m;
   m.kv = view; m.c = a; m.q = q; m.q_stride = q_stride; m.scale_log2 = scale * 1.4426950408889634f; m.lse = lse; m.in = in; m.out = out;
   m.stride = stride; m.rep = a.hq / view.hkv;
-  LAUNCH_OP(c, (mass_step_kernel<DH, MT>), 3 * c->sm_count, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, m);
+  LAUNCH_OP(c, (mass_step_kernel<DH, MT>), 4 * c->sm_count, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, m);
   return RPO_OK;
 }
 

@@ -19,7 +19,7 @@ struct MassArgs {
 // every warp takes an equal share of the pages of all (sequence, KV head)s, with a ring of pages of its own.
 template <int DH, int MT>
 struct MassStepCfg {
-  static constexpr int STAGES = 4, PAGE_BYTES = KV_BLOCK * DH * 2;
+  static constexpr int STAGES = 3, PAGE_BYTES = KV_BLOCK * DH * 2;
   static constexpr int SMEM = 4 * STAGES * PAGE_BYTES;                 // + (n_seqs + 1) ints
 };
 
@@ -105,6 +105,14 @@ __global__ void __launch_bounds__(128) mass_step_kernel(MassArgs a) {
       }
       fa::cp_commit();
       const int key0 = (i0 + it) * KV_BLOCK;
+      // lane (g < 2, tq) hands over keys 8 g + 2 tq, + 1: what they had is on its way while the scores are computed
+      const int j = key0 + g * 8 + tq * 2;
+      const int64_t at = ((int64_t)s * hkv + h) * a.stride + j;
+      float had0 = 0.f, had1 = 0.f;
+      if (a.in && g < 2) {
+        if (j < n_live) had0 = a.in[at];
+        if (j + 1 < n_live) had1 = a.in[at + 1];
+      }
       float w[4] = {0.f, 0.f, 0.f, 0.f};                               // keys 2 tq, 2 tq + 1, and 8 further
       if ((have >> (it & 31)) & 1) {
         fa::cp_wait<STAGES - 1>();
@@ -137,12 +145,9 @@ __global__ void __launch_bounds__(128) mass_step_kernel(MassArgs a) {
           for (int e = 0; e < 4; ++e) w[e] += __shfl_xor_sync(0xffffffffu, w[e], o);
         __syncwarp();
       }
-      if (g < 2) {                                                     // lane (g, tq): keys 8 g + 2 tq, + 1
-        const int j = key0 + g * 8 + tq * 2;
-        const int64_t at = ((int64_t)s * hkv + h) * a.stride + j;
-        const float x0 = g ? w[2] : w[0], x1 = g ? w[3] : w[1];
-        if (j < n_live) a.out[at] = (a.in ? a.in[at] : 0.f) + x0;
-        if (j + 1 < n_live) a.out[at + 1] = (a.in ? a.in[at + 1] : 0.f) + x1;
+      if (g < 2) {
+        if (j < n_live) a.out[at] = had0 + (g ? w[2] : w[0]);
+        if (j + 1 < n_live) a.out[at + 1] = had1 + (g ? w[3] : w[1]);
       }
     }
     fa::cp_wait<0>();

@@ -32,11 +32,12 @@ struct AttnOut { T* out; float* lse; int hq, rep; };
 
 constexpr float LN2_F = 0.69314718055994531f, LOG2E_F = 1.44269504088896341f;
 
-// o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p over an item's pieces.  A CTA per (item, rows): its eight warps
-// take the pieces in turn (piece p: warp p mod 8), four loads in flight each, and are added up in warp order.
+// o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p over an item's pieces.  A CTA per (item, rows): where many pieces
+// meet its eight warps take them in turn (piece p: warp p mod 8), eight loads in flight each, and are added up in warp order.
+constexpr int MERGE_WARPS = 8, MERGE_LOADS = 8;
 template <typename T, int DH>
-__global__ void __launch_bounds__(256) split_merge_kernel(SplitWs ws, AttnOut<T> a) {
-  constexpr int DPL = DH / 32, W = 8;
+__global__ void __launch_bounds__(MERGE_WARPS * 32) split_merge_kernel(SplitWs ws, AttnOut<T> a) {
+  constexpr int DPL = DH / 32, W = MERGE_WARPS;
   __shared__ float s_o[W][DH];
   __shared__ float s_l[W];
   const SplitRec rec = ws.rec[blockIdx.x];
@@ -54,11 +55,11 @@ __global__ void __launch_bounds__(256) split_merge_kernel(SplitWs ws, AttnOut<T>
     float l = 0.f, acc[DPL];
 #pragma unroll
     for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
-    for (int p0 = shared_row ? warp : 0; p0 < rec.n_parts; p0 += 4 * step) {
-      float x[4][DPL];
-      float2 ml[4];
+    for (int p0 = shared_row ? warp : 0; p0 < rec.n_parts; p0 += MERGE_LOADS * step) {
+      float x[MERGE_LOADS][DPL];
+      float2 ml[MERGE_LOADS];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < MERGE_LOADS; ++u) {
         const bool v = p0 + u * step < rec.n_parts;
         ml[u] = v ? ws.ml[slot(p0 + u * step)] : make_float2(-INFINITY, 0.f);
         const float* o = ws.o + slot(v ? p0 + u * step : p0) * DH + lane * DPL;
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(256) split_merge_kernel(SplitWs ws, AttnOut<T>
         for (int i = 0; i < DPL; i += 2) { const float2 y = *reinterpret_cast<const float2*>(o + i); x[u][i] = y.x; x[u][i + 1] = y.y; }
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < MERGE_LOADS; ++u) {
         const float w = fa::ex2(ml[u].x - mu);
         l = fmaf(w, ml[u].y, l);
 #pragma unroll
@@ -161,6 +162,7 @@ struct StepCfg {
 struct StepArgs {
   PagedView<bf16> kv; ChunkArgs c;
   const bf16* q; int64_t q_stride; float scale_log2;
+  const bf16 *k_new, *v_new; int64_t new_stride;             // NULL: the chunk's K and V are in the cache
   AttnOut<bf16> o; SplitWs ws;
   int min_share;
 };
@@ -196,8 +198,8 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
     const KeyPages kp = key_pages(a.c, p0, p1);
     const int n_pages = max(1, kp.count()), in_seq = f - s_pref[s], h = in_seq / n_pages, i0 = in_seq % n_pages;
     const int i1 = min(n_pages, i0 + (f_end - f)), item0 = f - i0;     // my pages of the item, its place in the list
-    const bf16* kb = a.kv.k + h * a.kv.head_stride;
-    const bf16* vb = a.kv.v + h * a.kv.head_stride;
+    bf16* kb = a.kv.k + h * a.kv.head_stride;
+    bf16* vb = a.kv.v + h * a.kv.head_stride;
     const int32_t* tbl = a.kv.table + (int64_t)s * a.kv.table_stride;
 
     // ---- queries as A fragments: rows g, g + 8 of every 16
@@ -239,14 +241,28 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
       const int blk = __shfl_sync(0xffffffffu, ids, it & 31);
       const int key0 = kp.page(i0 + warp + 4 * it) * KV_BLOCK;
       const uint32_t dst = ring + (it % STAGES) * (2 * PB);
-#pragma unroll
-      for (int e = 0; e < KV_BLOCK * CPR / 32; ++e) {
+      auto piece = [&](int e, bool fresh) {
         const int x = e * 32 + lane, row = x / CPR, ch = x % CPR, j = key0 + row;
         // rows that none of the queries sees become zeros: whatever the cache holds there, 0 x NaN included
         const int bytes = (blk >= 0 && j <= p1 && (j >= kp.lo || j < a.c.sinks)) ? 16 : 0;
         const int64_t at = ((int64_t)max(blk, 0) * KV_BLOCK + row) * DH + ch * 8;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + sw(row, ch)), "l"(kb + at), "r"(bytes) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + PB + sw(row, ch)), "l"(vb + at), "r"(bytes) : "memory");
+        const bf16 *ks = kb + at, *vs = vb + at;
+        if (fresh && j >= p0 && bytes) {
+          // a row of the chunk: read where it is, and written to its page on the way (this page is nobody else's)
+          const int64_t n = (int64_t)(sp.row0 + j - p0) * a.new_stride + h * DH + ch * 8;
+          ks = a.k_new + n; vs = a.v_new + n;
+          *reinterpret_cast<uint4*>(kb + at) = *reinterpret_cast<const uint4*>(ks);
+          *reinterpret_cast<uint4*>(vb + at) = *reinterpret_cast<const uint4*>(vs);
+        }
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + sw(row, ch)), "l"(ks), "r"(bytes) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + PB + sw(row, ch)), "l"(vs), "r"(bytes) : "memory");
+      };
+      if (a.k_new && key0 + KV_BLOCK > p0) {
+#pragma unroll 1
+        for (int e = 0; e < KV_BLOCK * CPR / 32; ++e) piece(e, true);
+      } else {
+#pragma unroll
+        for (int e = 0; e < KV_BLOCK * CPR / 32; ++e) piece(e, false);
       }
     };
     if (n_mine > 0) fetch_ids(0);
