@@ -221,8 +221,8 @@ struct MassCfg {
   static constexpr int K_BYTES = 128 * DH * 2;              // one sub-tile of keys
   static constexpr int Q_BYTES = MS_ROWS * DH * 2;          // one tile of rows
   static constexpr int NSQ = 3;
-  static constexpr int SMEM = 2 * K_BYTES + NSQ * Q_BYTES + 1024 + 512 + NSQ * MS_ROWS * 4;
-  static constexpr int THREADS = 384;
+  static constexpr int SMEM = 2 * K_BYTES + NSQ * Q_BYTES + 1024 + 512 + NSQ * MS_ROWS * 4 + MS_KEYS * 4;
+  static constexpr int THREADS = 640;                       // producer, issuer, two warps for the log-sums; four warpgroups of sums
 };
 
 struct MassTcArgs {
@@ -243,19 +243,16 @@ __global__ void __launch_bounds__(MS_KEYS) mass_merge_kernel(MassWs ws, const fl
 }
 
 // Sum over the 128 columns (rows of the chunk) of this thread's lane (key) of 2^(s scale - lse); MASKED: columns [lo, hi).
-template <bool MASKED, typename F>
-__device__ __forceinline__ float mass_columns(uint32_t ts, uint32_t ls, float scale_log2, int lo, int hi, F release) {
+template <bool MASKED>
+__device__ __forceinline__ float mass_columns(uint32_t ts, uint32_t ls, float scale_log2, int lo, int hi) {
   const uint64_t sc2 = t5::pack2(scale_log2, scale_log2);
   uint64_t acc[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int c0 = 0; c0 < MS_ROWS; c0 += 64) {
-    uint32_t v[64];
-    tc::tmem_ld32_nowait(ts + c0, v);
-    tc::tmem_ld32_nowait(ts + c0 + 32, v + 32);
-    tc::tmem_ld_wait();
-    if (c0 + 64 == MS_ROWS) release();
+  for (int c0 = 0; c0 < MS_ROWS; c0 += 32) {
+    uint32_t v[32];
+    tc::tmem_ld32(ts + c0, v);
 #pragma unroll
-    for (int c = 0; c < 64; c += 4) {
+    for (int c = 0; c < 32; c += 4) {
       uint64_t l01, l23;                                               // two negated log-sums each
       asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(l01), "=l"(l23) : "r"(ls + (c0 + c) * 4));
       float p[4];
@@ -284,10 +281,12 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   uint8_t* sm = (uint8_t*)(((uintptr_t)mc_raw + 1023) & ~(uintptr_t)1023);
   const uint32_t sK = tc::smem_u32(sm), sQ = sK + 2 * Cfg::K_BYTES;
   float* s_lse = (float*)(sm + 2 * Cfg::K_BYTES + NSQ * Cfg::Q_BYTES);       // [NSQ][128], negated, log2 domain
-  uint64_t* bars = (uint64_t*)(s_lse + NSQ * MS_ROWS);
+  float* s_sum = s_lse + NSQ * MS_ROWS;                                      // [2][128]: the odd steps' sums
+  uint64_t* bars = (uint64_t*)(s_sum + MS_KEYS);
   uint64_t *q_full = bars, *q_empty = bars + NSQ, *l_full = bars + 2 * NSQ;
   uint64_t *s_full = bars + 3 * NSQ, *s_free = s_full + 4, *k_full = s_full + 8, *k_free = s_full + 9;
-  uint32_t* tmem_slot = (uint32_t*)(s_full + 10);
+  uint64_t *x_full = s_full + 10, *x_free = s_full + 12;                     // hand-over of the odd steps' sums, per sub-tile
+  uint32_t* tmem_slot = (uint32_t*)(s_full + 14);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   int* s_first = (int*)(tmem_slot + 2);
   const int warp = (int)t5::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, hkv = a.kv.hkv, rep = a.rep, cols = a.tq * rep;
@@ -295,6 +294,7 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   if (threadIdx.x == 0) {
     for (int i = 0; i < NSQ; ++i) { tc::mbar_init(&q_full[i], 1); tc::mbar_init(&q_empty[i], 1 + 8); tc::mbar_init(&l_full[i], 1); }
     for (int i = 0; i < 4; ++i) { tc::mbar_init(&s_full[i], 1); tc::mbar_init(&s_free[i], 4); }
+    for (int i = 0; i < 2; ++i) { tc::mbar_init(&x_full[i], 4); tc::mbar_init(&x_free[i], 4); }
     tc::mbar_init(k_full, 1); tc::mbar_init(k_free, 1);
     *abort_flag = 0; *s_first = 0;
     a.ws.rec[blockIdx.x] = SplitRec{0, 0, 0, 0};
@@ -365,13 +365,28 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
           tc::mbar_expect_tx(&q_full[st], HALVES * cols * 128);
           for (int hf = 0; hf < HALVES; ++hf) t5::tma_load_3d(sQ + st * Cfg::Q_BYTES + hf * (MS_ROWS * 128), &q_map, hf * 64, head * rep, min(row, a.c.n_rows - 1), &q_full[st]);
         }
-        // log-sums of the tile's rows; columns without a row (their q is zero) get weight 0 from -inf, rows of
-        // other chunks are masked later
+      }
+    }
+  } else if (warp == 2 || warp == 3) {
+    // ------------------------------------------------------------------ log-sums of the rows: warp 2 even steps, 3 odd ones
+    // Columns without a row (their q is zero) get weight 0 from -inf, rows of other chunks are masked later.
+    bool ok = true;
+    int qt = 0, tok[4], at[4];
 #pragma unroll
-        for (int c = lane; c < MS_ROWS; c += 32) {
-          const int rr = row + c / rep;
-          s_lse[st * MS_ROWS + c] = (c < cols && rr < sp.row0 + sp.rows) ? a.lse[(int64_t)rr * a.c.hq + head * rep + c % rep] * -LOG2E_F : -INFINITY;
-        }
+    for (int i = 0; i < 4; ++i) { const int c = lane + 32 * i; tok[i] = c < cols ? c / rep : 1 << 30; at[i] = c < cols ? c / rep * a.c.hq + c % rep : 0; }
+    while (ok && next()) {
+      const ChunkSpan sp = chunk_span(a.kv, a.c, it.seq);
+      for (int t = t0; t < t1; ++t, ++qt) {
+        if ((qt & 1) != (warp & 1)) continue;
+        const int st = qt % NSQ, first = it.tok0 + t * a.tq;
+        const float* l = a.lse + (int64_t)(sp.row0 + first) * a.c.hq + head * rep;
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = tok[i] < sp.rows - first ? l[at[i]] * -LOG2E_F : -INFINITY;
+        ok = tc::mbar_wait_warp(&q_empty[st], ((qt / NSQ) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_lse[st * MS_ROWS + lane + 32 * i] = x[i];
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&l_full[st]);
       }
@@ -381,7 +396,8 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MS_ROWS >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     const uint32_t dq = t5::uniform(t5::desc_lo(sQ, 16)), dk = t5::uniform(t5::desc_lo(sK, 16)), tm = t5::uniform(tmem);
     bool ok = true;
-    int qt = 0, used[2] = {0, 0};                            // S buffers filled so far per sub-tile
+    int qt = 0;
+    uint32_t free_phase = 0;                                 // bit 2 x + b: phase of S buffer b of sub-tile x
     for (int seg = 0; ok && next(); ++seg) {
       const int live = min(paged_len(a.kv.lens, it.seq, a.kv.table_stride, a.kv.status), a.stride) - it.key0, subs = live > 128 ? 2 : 1;
       ok = tc::mbar_wait_warp(k_full, seg & 1, abort_flag);
@@ -391,9 +407,10 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         ok = tc::mbar_wait_warp(&q_full[st], (qt / NSQ) & 1, abort_flag);
         if (!ok) break;
         for (int x = 0; x < subs; ++x) {
-          const int b = used[x] & 1;
-          ok = tc::mbar_wait_warp(&s_free[x * 2 + b], ((used[x] >> 1) & 1) ^ 1, abort_flag);
+          const int b = qt & 1;
+          ok = tc::mbar_wait_warp(&s_free[x * 2 + b], ((free_phase >> (x * 2 + b)) & 1) ^ 1, abort_flag);
           if (!ok) break;
+          free_phase ^= 1u << (x * 2 + b);
           tc::tmem_fence_after();
           if (t5::elect_one()) {
 #pragma unroll
@@ -403,30 +420,34 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
             }
             tc::umma_commit(&s_full[x * 2 + b]);
           }
-          ++used[x];
         }
         if (!ok) break;
         if (t5::elect_one()) { tc::umma_commit(&q_empty[st]); if (t + 1 == t1) tc::umma_commit(k_free); }
       }
     }
   } else if (warp >= 4) {
-    // ------------------------------------------------------------------ sums: warps 4..7 keys 0..127, 8..11 keys 128..255
-    const int x = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
-    const uint32_t t_s = tmem + ((uint32_t)(quad * 32) << 16) + x * 256;
+    // ------------------------------------------------------------------ sums: a warpgroup per (sub-tile x, step parity b)
+    // (With one warpgroup per sub-tile, two warps per scheduler, the exponential unit was half idle: 103 us against ... )
+    const int x = ((warp - 4) >> 2) & 1, b = (warp - 4) >> 3, quad = warp & 3, r = quad * 32 + lane;
+    const uint32_t ts = tmem + ((uint32_t)(quad * 32) << 16) + x * 256 + b * 128;
     bool ok = true;
-    int qt = 0, used = 0;
+    int qt = 0;
+    uint32_t s_phase = 0, x_phase = 0;
     for (int seg = 0; ok && next(); ++seg) {
       const ChunkSpan sp = chunk_span(a.kv, a.c, it.seq);
       const int live = min(sp.len, a.stride) - it.key0, j = it.key0 + x * 128 + r, p0 = sp.len - sp.rows;
       const bool active = x == 0 || live > 128;
       float sum = 0.f;
       for (int t = t0; t < t1; ++t, ++qt) {
+        if ((qt & 1) != b) continue;
         const int st = qt % NSQ;
+        ok = tc::mbar_wait_warp(&l_full[st], (qt / NSQ) & 1, abort_flag);
+        if (ok && active) {
+          ok = tc::mbar_wait_warp(&s_full[x * 2 + b], s_phase, abort_flag);
+          s_phase ^= 1;
+        }
+        if (!ok) break;
         if (active) {
-          const int b = used & 1;
-          ok = tc::mbar_wait_warp(&s_full[x * 2 + b], (used >> 1) & 1, abort_flag) && tc::mbar_wait_warp(&l_full[st], (qt / NSQ) & 1, abort_flag);
-          if (!ok) break;
-          ++used;
           tc::tmem_fence_after();
           const int tok0 = it.tok0 + t * a.tq, n_tok = min(a.tq, sp.rows - tok0), pt = p0 + tok0;
           const int k_lo = it.key0 + x * 128, k_hi = k_lo + 127;
@@ -436,22 +457,33 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
           int end = max(0, n_tok);
           if (a.c.window > 0 && j >= a.c.sinks) end = (int)max((int64_t)0, min((int64_t)end, (int64_t)j + a.c.window - pt));
           const int hi = end * rep;
-          const uint32_t ts = t_s + b * 128, ls = tc::smem_u32(s_lse + st * MS_ROWS);
-          auto release = [&]() {
-            tc::tmem_fence_before();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&s_free[x * 2 + b]);
-          };
-          sum += whole ? mass_columns<false>(ts, ls, a.scale_log2, 0, 0, release) : mass_columns<true>(ts, ls, a.scale_log2, lo, hi, release);
-        } else {
-          // (the slot's log-sums are not read, but its release counts every warp: wait until it is filled)
-          ok = tc::mbar_wait_warp(&l_full[st], (qt / NSQ) & 1, abort_flag);
-          if (!ok) break;
+          const uint32_t ls = tc::smem_u32(s_lse + st * MS_ROWS);
+          sum += whole ? mass_columns<false>(ts, ls, a.scale_log2, 0, 0) : mass_columns<true>(ts, ls, a.scale_log2, lo, hi);
+          tc::tmem_fence_before();
         }
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&q_empty[st]);
+        if (lane == 0) {
+          if (active) tc::mbar_arrive(&s_free[x * 2 + b]);
+          tc::mbar_arrive(&q_empty[st]);
+        }
       }
       if (!ok) break;
+      // the odd steps' sums join the even ones'
+      if (b == 1) {
+        ok = tc::mbar_wait_warp(&x_free[x], x_phase ^ 1, abort_flag);
+        if (!ok) break;
+        s_sum[x * 128 + r] = sum;
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&x_full[x]);
+        x_phase ^= 1;
+        continue;
+      }
+      ok = tc::mbar_wait_warp(&x_full[x], x_phase, abort_flag);
+      if (!ok) break;
+      sum += s_sum[x * 128 + r];
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&x_free[x]);
+      x_phase ^= 1;
       const bool begins = t0 == 0, ends = t1 == it.steps;
       const int64_t at = ((int64_t)it.seq * hkv + head) * a.stride + j;
       if (begins && ends) {
