@@ -450,15 +450,18 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         if (active) {
           tc::tmem_fence_after();
           const int tok0 = it.tok0 + t * a.tq, n_tok = min(a.tq, sp.rows - tok0), pt = p0 + tok0;
-          const int k_lo = it.key0 + x * 128, k_hi = k_lo + 127;
+          // of this warp's 32 keys: all seen by all rows of the tile, or none by any?
+          const int k_lo = it.key0 + x * 128 + quad * 32, k_hi = k_lo + 31;
           const bool whole = n_tok == a.tq && k_hi <= pt && (a.c.window <= 0 || k_lo > pt + n_tok - 1 - a.c.window || k_hi < a.c.sinks);
+          const bool none = k_lo > pt + n_tok - 1 || (a.c.window > 0 && k_hi <= pt - a.c.window && k_lo >= a.c.sinks);
           // columns [lo, hi) of my key
           const int lo = min(max(0, j - pt), MS_ROWS) * rep;
           int end = max(0, n_tok);
           if (a.c.window > 0 && j >= a.c.sinks) end = (int)max((int64_t)0, min((int64_t)end, (int64_t)j + a.c.window - pt));
           const int hi = end * rep;
           const uint32_t ls = tc::smem_u32(s_lse + st * MS_ROWS);
-          sum += whole ? mass_columns<false>(ts, ls, a.scale_log2, 0, 0) : mass_columns<true>(ts, ls, a.scale_log2, lo, hi);
+          if (whole) sum += mass_columns<false>(ts, ls, a.scale_log2, 0, 0);
+          else if (!none) sum += mass_columns<true>(ts, ls, a.scale_log2, lo, hi);
           tc::tmem_fence_before();
         }
         __syncwarp();
