@@ -67,6 +67,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
   constexpr int WARPS = THREADS / 32, BPT = EV_BINS / THREADS;
   extern __shared__ int ev_list[];                            // slots of the holes this CTA lists
   __shared__ int hist[EV_BINS];
+  __shared__ int totals[2][C > 1 ? EV_BINS / C : 1];          // cluster: counts of the bins this CTA owns, of this round and the next
   __shared__ uint32_t mask[KPT ? WARPS * KPT : EV_MAX_WORDS];
   __shared__ int s_warp[2][32], s_cta[2], s_max;
   __shared__ int s_bin, s_above;
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     }
     return;
   }
-  const int kpt = KPT ? KPT : (a.mass_stride + C * THREADS - 1) / (C * THREADS);
+  const int kpt = (a.mass_stride + C * THREADS - 1) / (C * THREADS);       // at most KPT: the slots are spread over all threads
   const int slot0 = (rank * WARPS + warp) * 32 * kpt + lane;
 
   auto sync_all = [&]() { if (C > 1) fa::cluster_sync(); else __syncthreads(); };
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     if (KPT) {
 #pragma unroll
       for (int k = 0; k < KPT; ++k) {
-        const int i = slot0 + 32 * k;
+        const int i = k < kpt ? slot0 + 32 * k : len;
         key[k] = i < len ? evict_key(mass[i]) : 0u;
         p[k] = i < len ? pos[i] : INT_MIN;
         newest = max(newest, p[k]);
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     if (KPT)
 #pragma unroll
       for (int k = 0; k < KPT; ++k)
-        if (slot0 + 32 * k < len && (p[k] < a.sinks || (int64_t)p[k] > (int64_t)newest - a.recent)) safe_bits |= 1u << k;
+        if (k < kpt && slot0 + 32 * k < len && (p[k] < a.sinks || (int64_t)p[k] > (int64_t)newest - a.recent)) safe_bits |= 1u << k;
   }
   auto is_safe = [&](int k) -> bool {                         // (newest - recent may not fit 32 bits)
     if (KPT) return (safe_bits >> k) & 1;
@@ -159,7 +160,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
   auto each = [&](auto f) {                                   // f(k) for my slots that hold a token
     if (KPT) {
 #pragma unroll
-      for (int k = 0; k < KPT; ++k) if (slot0 + 32 * k < len) f(k);
+      for (int k = 0; k < KPT; ++k) if (k < kpt && slot0 + 32 * k < len) f(k);
     } else {
       for (int k = 0; k < kpt; ++k) if (slot0 + 32 * k < len) f(k);
     }
@@ -199,21 +200,28 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     for (int round = 0; round < 3; ++round) {
       const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
       for (int i = tid; i < EV_BINS; i += THREADS) hist[i] = 0;
-      __syncthreads();
+      if (C > 1) for (int i = tid; i < EV_BINS / C; i += THREADS) { totals[(round + 1) & 1][i] = 0; if (round == 0) totals[0][i] = 0; }
+      if (C > 1 && round == 0) sync_all(); else __syncthreads();
       each([&](int k) {
         const uint32_t x = get_key(k);
         if (is_safe(k) == cls && (round == 0 || (x >> (shift + bits)) == prefix)) atomicAdd(&hist[(x >> shift) & ((1 << bits) - 1)], 1);
       });
+      if (C > 1) {
+        // every bin has an owner in the cluster; only bins that hold something are sent there
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < BPT; ++i) {
+          const int bin = i * THREADS + tid, n = hist[bin];
+          if (n) asm volatile("red.relaxed.cluster.shared::cluster.add.s32 [%0], %1;" ::"r"(peer(&totals[round & 1][bin % (EV_BINS / C)], bin / (EV_BINS / C))), "r"(n) : "memory");
+        }
+      }
       sync_all();
       // thread t owns BPT bins from the top: counts from the top
       int c[BPT], sum = 0;
 #pragma unroll
       for (int i = 0; i < BPT; ++i) {
         const int bin = EV_BINS - 1 - tid * BPT - i;
-        c[i] = C > 1 ? 0 : hist[bin];
-        if (C > 1)
-#pragma unroll
-          for (int r = 0; r < C; ++r) c[i] += ld_cluster_s32(peer(&hist[bin], r));
+        c[i] = C > 1 ? ld_cluster_s32(peer(&totals[round & 1][bin % (EV_BINS / C)], bin / (EV_BINS / C))) : hist[bin];
         sum += c[i];
       }
       int incl = sum;
@@ -236,6 +244,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
   int n_eq = 0, n_hole = 0, n_mover = 0, eq_rank, hole, mover, n_moves;
 #pragma unroll
   for (int k = 0; k < (KPT ? KPT : kpt); ++k) {
+    if (k >= kpt) break;
     bool kept = false, eq = false;
     if (slot0 + 32 * k < len) {
       const bool sf = is_safe(k);
@@ -252,6 +261,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
   else __syncwarp();
 #pragma unroll
   for (int k = 0; k < (KPT ? KPT : kpt); ++k) {
+    if (k >= kpt) break;
     const bool eq = !few && slot0 + 32 * k < len && is_safe(k) == cls && get_key(k) == last;
     const uint32_t e = __ballot_sync(0xffffffffu, eq);
     const bool take = eq && eq_rank + __popc(e & ((1u << lane) - 1)) < need;
