@@ -100,9 +100,16 @@ static int op_map_rows(rpo_ctx* c, CUtensorMap* m, const bf16* q, int64_t q_stri
   return op_map(c, m, q, 3, dims, strides, box);
 }
 
+// One CTA for the list of items, up to two per SM for the chunk's K and V.
+template <typename T, int DH>
+static int prepare_grid(const PagedView<T>& view, const ChunkArgs& a, const T* k_new) {
+  return 1 + (k_new ? grid_for((int64_t)a.n_rows * view.hkv * 2 * (DH * sizeof(T) / 16), 1024, 2 * 148) : 0);
+}
+
 // Many rows per sequence: tensor-core tiles of 2 x (tokens x heads of a KV head <= 128) rows against 128 keys.
 template <int DH>
-static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, float scale, bf16* out, float* lse) {
+static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const bf16* k_new, const bf16* v_new,
+                      int64_t new_stride, float scale, bf16* out, float* lse) {
   using Cfg = ChunkCfg<DH>;
   static bool attr_done[64] = {};
   if (tc_first_use_on_device(c, attr_done))
@@ -119,15 +126,17 @@ static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   RPO_TRY(op_map_rows(c, &qm, q, q_stride, a.n_rows, a.hq, DH, t.o.rep, t.tq));
   RPO_TRY(op_map_pages(c, &km, view, view.k, DH));
   RPO_TRY(op_map_pages(c, &vm, view, view.v, DH));
-  LAUNCH_OP(c, (chunk_plan_kernel<bf16, CH_BN / KV_BLOCK>), 1, 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4, items, plan);
+  LAUNCH_OP(c, (chunk_prepare_kernel<bf16, DH, CH_BN / KV_BLOCK>), (prepare_grid<bf16, DH>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4,
+            items, plan, k_new, v_new, new_stride);
   LAUNCH_OP(c, (paged_chunk_kernel<DH>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
-  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, 16), MERGE_WARPS * 32, 0, t.ws, t.o);
+  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, OP_PART_ROWS / (MERGE_WARPS * MERGE_ROWS)), MERGE_WARPS * 32, 0, t.ws, t.o);
   return RPO_OK;
 }
 
 // 32-bit storage: BM rows of an item against tiles of keys on CUDA cores.
 template <int DH, int BM>
-static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& a, const float* q, int64_t q_stride, float scale, float* out, float* lse) {
+static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& a, const float* q, int64_t q_stride, const float* k_new, const float* v_new,
+                      int64_t new_stride, float scale, float* out, float* lse) {
   using Cfg = F32Cfg<DH, BM>;
   static bool attr_done[64] = {};
   if (tc_first_use_on_device(c, attr_done))
@@ -141,9 +150,10 @@ static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& 
   ChunkPlan* plan = (ChunkPlan*)(items + OP_MAX_ITEMS);
   f.items = items; f.plan = plan;
   const int grid = std::min(Cfg::CTAS * c->sm_count, OP_GRID * c->sm_count);
-  LAUNCH_OP(c, (chunk_plan_kernel<float, Cfg::BN / KV_BLOCK>), 1, 1024, view.n_seqs * 4, view, a, f.tok, grid, 2, items, plan);
+  LAUNCH_OP(c, (chunk_prepare_kernel<float, DH, Cfg::BN / KV_BLOCK>), (prepare_grid<float, DH>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, f.tok, grid, 2, items,
+            plan, k_new, v_new, new_stride);
   LAUNCH_OP(c, (paged_f32_kernel<DH, BM>), grid, 256, Cfg::SMEM, f);
-  LAUNCH_OP(c, (split_merge_kernel<float, DH>), dim3(grid, BM == 64 ? 8 : std::min(a.max_chunk * f.o.rep, BM)), MERGE_WARPS * 32, 0, f.ws, f.o);
+  LAUNCH_OP(c, (split_merge_kernel<float, DH>), dim3(grid, BM == 64 ? BM / (MERGE_WARPS * MERGE_ROWS) : std::min(a.max_chunk * f.o.rep, BM)), MERGE_WARPS * 32, 0, f.ws, f.o);
   return RPO_OK;
 }
 
@@ -152,19 +162,14 @@ static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs
                              const void* v_new, int64_t new_stride, float scale, void* out, float* lse) {
   const PagedView<T> view = paged_view<T>(c, kv);
   const int64_t rows = a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads);           // of the longest chunk, per KV head
-  const bool steps = c->bf16 && rows <= 32;
-  if (k_new && !steps) {                                     // (the kernel of decode steps writes them itself)
-    const int64_t n = (int64_t)a.n_rows * view.hkv * 2 * (DH * sizeof(T) / 16);
-    LAUNCH_OP(c, (paged_append_kernel<T, DH>), grid_for(n, 256), 256, 0, view, a, (const T*)k_new, (const T*)v_new, new_stride);
-  }
   if constexpr (std::is_same<T, bf16>::value) {
-    if (steps)
+    if (rows <= 32)
       return rows <= 16 ? chunk_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse)
                         : chunk_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
-    return chunk_tiles<DH>(c, view, a, (const bf16*)q, q_stride, scale, (bf16*)out, lse);
+    return chunk_tiles<DH>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
   } else {
-    if (rows <= 16) return chunk_f32<DH, 16>(c, view, a, (const float*)q, q_stride, scale, (float*)out, lse);
-    return chunk_f32<DH, 64>(c, view, a, (const float*)q, q_stride, scale, (float*)out, lse);
+    if (rows <= 16) return chunk_f32<DH, 16>(c, view, a, (const float*)q, q_stride, (const float*)k_new, (const float*)v_new, new_stride, scale, (float*)out, lse);
+    return chunk_f32<DH, 64>(c, view, a, (const float*)q, q_stride, (const float*)k_new, (const float*)v_new, new_stride, scale, (float*)out, lse);
   }
 }
 

@@ -59,10 +59,16 @@ __device__ __forceinline__ void plan_scan(int64_t v, int64_t& before, int64_t& a
   for (int w = 0; w < 32; ++w) { if (w < warp) before += s_warp[w]; all += s_warp[w]; }
 }
 
-// The list of items, summed up: one CTA.  tok: tokens per item; PAGES: pages per key tile.
-template <typename T, int PAGES>
-__global__ void __launch_bounds__(1024) chunk_plan_kernel(PagedView<T> kv, ChunkArgs c, int tok, int n_ctas, int min_share, ChunkItem* items,
-                                                          ChunkPlan* plan) {
+// What a call needs before its main kernel: CTA 0 sums up the list of items (tok: tokens per item; PAGES: pages per key
+// tile), the others write the chunk's K and V to their pages.
+template <typename T, int DH, int PAGES>
+__global__ void __launch_bounds__(1024) chunk_prepare_kernel(PagedView<T> kv, ChunkArgs c, int tok, int n_ctas, int min_share, ChunkItem* items,
+                                                             ChunkPlan* plan, const T* __restrict__ k_new, const T* __restrict__ v_new,
+                                                             int64_t new_stride) {
+  if (blockIdx.x > 0) {
+    paged_append<T, DH>(kv, c, k_new, v_new, new_stride, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
   extern __shared__ int pl_first[];                    // items of the sequences before s
   __shared__ int64_t s_warp[32];
   const int tid = threadIdx.x;
@@ -428,9 +434,14 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
       const int p = min(p_lo + tok, p_hi);
       float m = -INFINITY, l = 0.f;
       bool have_m = false;                                   // every row of the warp has a reference maximum
+      // Halves [u_whole0, u_whole1) hold only keys that every row of the sub-tile sees (of the window's tiles; halves of
+      // the sinks' tiles are masked one by one).
+      const int first_key = kt_of.page0(kt_of.n1) * KV_BLOCK;
+      const int from = a.c.window > 0 ? max(0, p_hi - a.c.window + 1 - first_key) : 0;
+      const int u_whole0 = 2 * kt_of.n1 + (from + CH_HALF - 1) / CH_HALF;
+      const int u_whole1 = 2 * kt_of.n1 + max(0, p_lo + 1 - first_key) / CH_HALF;
       for (int u = 2 * walk.t0; u < 2 * walk.t1; ++u, ++steps) {
-        const int h = u & 1, key0 = kt_of.page0(u >> 1) * KV_BLOCK + h * CH_HALF;
-        const bool first_range = (u >> 1) < kt_of.n1;
+        const int h = u & 1;
         const uint32_t ts = t_s + h * CH_HALF;
         ok = tc::mbar_wait_warp(&s_full[x * 2 + h], s_phase, abort_flag);
         if (!ok) break;
@@ -440,8 +451,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         tc::tmem_ld32_nowait(ts, v);
         tc::tmem_ld32_nowait(ts + 32, v + 32);
         tc::tmem_ld_wait();
-        const bool whole = key0 + CH_HALF - 1 <= (first_range ? min(p_lo, a.c.sinks - 1) : p_lo) &&
-                           (a.c.window <= 0 || key0 > p_hi - a.c.window || key0 + CH_HALF <= a.c.sinks);
+        const bool whole = u >= u_whole0 && u < u_whole1;
         // All keys seen and every row has a reference: no maximum is needed, any reference is exact as long as nothing
         // overflows, and the half's sum tells.  (S stays in tensor memory until P is stored over it.)
         bool done = false;
@@ -457,6 +467,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         }
         if (!done) {
           if (!whole) {
+            const int key0 = kt_of.page0(u >> 1) * KV_BLOCK + h * CH_HALF;
+            const bool first_range = (u >> 1) < kt_of.n1;
             const int hi = (first_range ? min(p, a.c.sinks - 1) : p) - key0;
             const int lo = a.c.window > 0 ? p - a.c.window + 1 - key0 : -key0, sk = a.c.sinks - key0;
 #pragma unroll

@@ -72,11 +72,11 @@ __device__ __forceinline__ int64_t paged_row(const PagedView<T>& kv, int s, int 
 // The chunk's K and V rows into their pages; 16 bytes per thread.  Token i of a chunk of n rows in a cache of len
 // tokens lands at position len - n + i (rows whose position would be negative are dropped).
 template <typename T, int DH>
-__global__ void __launch_bounds__(256) paged_append_kernel(PagedView<T> kv, ChunkArgs c, const T* __restrict__ k_new,
-                                                           const T* __restrict__ v_new, int64_t new_stride) {
+__device__ __forceinline__ void paged_append(const PagedView<T>& kv, const ChunkArgs& c, const T* __restrict__ k_new, const T* __restrict__ v_new,
+                                             int64_t new_stride, int block, int n_blocks) {
   constexpr int EPC = 16 / sizeof(T), CPR = DH / EPC;        // elements per copy, copies per row
   const int64_t n = (int64_t)c.n_rows * kv.hkv * 2 * CPR;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+  for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < n; i += (int64_t)n_blocks * blockDim.x) {
     const int ch = (int)(i % CPR);
     const int64_t j = i / CPR;
     const int h = (int)(j % kv.hkv), which = (int)((j / kv.hkv) & 1), row = (int)(j / (2 * kv.hkv));

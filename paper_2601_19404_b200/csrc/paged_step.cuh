@@ -32,9 +32,21 @@ struct AttnOut { T* out; float* lse; int hq, rep; };
 
 constexpr float LN2_F = 0.69314718055994531f, LOG2E_F = 1.44269504088896341f;
 
-// o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p over an item's pieces.  A CTA per (item, rows): where many pieces
-// meet its eight warps take them in turn (piece p: warp p mod 8), eight loads in flight each, and are added up in warp order.
-constexpr int MERGE_WARPS = 8, MERGE_LOADS = 8;
+// o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p over an item's pieces, added up in piece order.  Few pieces: a warp
+// takes MERGE_ROWS rows at once, all of their loads in flight together.  Many (one long sequence): the warps of the CTA share a row's pieces, eight loads
+// in flight each.
+constexpr int MERGE_WARPS = 8, MERGE_LOADS = 8, MERGE_ROWS = 2, MERGE_FEW = 4;
+
+template <typename T, int N>
+__device__ __forceinline__ void merge_store(T* dst, const float (&x)[N], float scale) {
+  T y[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) y[i] = from_f32<T>(x[i] * scale);
+  if (sizeof(y) == 16) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(y);
+  else if (sizeof(y) == 8) *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(y);
+  else *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(y);
+}
+
 template <typename T, int DH>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) split_merge_kernel(SplitWs ws, AttnOut<T> a) {
   constexpr int DPL = DH / 32, W = MERGE_WARPS;
@@ -43,28 +55,69 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) split_merge_kernel(SplitWs w
   const SplitRec rec = ws.rec[blockIdx.x];
   if (rec.n_parts == 0) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.x;
-  // few pieces: a warp per row.  Many: the warps of the CTA share a row's pieces.
-  const bool shared_row = rec.n_parts > 8;
-  const int step = shared_row ? W : 1;
-  for (int r = shared_row ? blockIdx.y : blockIdx.y * W + warp; r < rec.rows; r += shared_row ? gridDim.y : gridDim.y * W) {
-    auto slot = [&](int p) -> int64_t { return (int64_t)(p == 0 ? 2 * b + 1 : 2 * (b + p)) * ws.rows_cap + r; };
+  auto slot = [&](int p, int r) -> int64_t { return (int64_t)(p == 0 ? 2 * b + 1 : 2 * (b + p)) * ws.rows_cap + r; };
+  auto load = [&](int64_t at, float (&x)[DPL]) {
+#pragma unroll
+    for (int i = 0; i < DPL; i += 2) { const float2 y = *reinterpret_cast<const float2*>(ws.o + at * DH + lane * DPL + i); x[i] = y.x; x[i + 1] = y.y; }
+  };
+  auto place = [&](int r) -> int64_t { return (int64_t)(rec.row0 + r / a.rep) * a.hq + rec.head0 + r % a.rep; };
+  if (rec.n_parts <= MERGE_FEW) {
+    for (int r0 = (blockIdx.y * W + warp) * MERGE_ROWS; r0 < rec.rows; r0 += gridDim.y * W * MERGE_ROWS) {
+      float2 ml[MERGE_ROWS][MERGE_FEW];
+      float x[MERGE_ROWS][MERGE_FEW][DPL];
+#pragma unroll
+      for (int p = 0; p < MERGE_FEW; ++p)
+#pragma unroll
+        for (int u = 0; u < MERGE_ROWS; ++u) {
+          ml[u][p] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+          for (int i = 0; i < DPL; ++i) x[u][p][i] = 0.f;
+          if (p < rec.n_parts) {
+            const int64_t at = slot(p, min(r0 + u, rec.rows - 1));
+            ml[u][p] = ws.ml[at];
+            load(at, x[u][p]);
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < MERGE_ROWS; ++u) {
+        if (r0 + u >= rec.rows) break;
+        float m = -INFINITY, l = 0.f, acc[DPL];
+#pragma unroll
+        for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
+#pragma unroll
+        for (int p = 0; p < MERGE_FEW; ++p) m = fmaxf(m, ml[u][p].x);
+        const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int p = 0; p < MERGE_FEW; ++p) {
+          const float w = fa::ex2(ml[u][p].x - mu);
+          l = fmaf(w, ml[u][p].y, l);
+#pragma unroll
+          for (int i = 0; i < DPL; ++i) acc[i] = fmaf(w, x[u][p][i], acc[i]);
+        }
+        const int64_t dst = place(r0 + u);
+        merge_store(a.out + dst * DH + lane * DPL, acc, l > 0.f ? 1.0f / l : 0.f);
+        if (lane == 0 && a.lse) a.lse[dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
+      }
+    }
+    return;
+  }
+  for (int r = blockIdx.y; r < rec.rows; r += gridDim.y) {
     float m = -INFINITY;
-    for (int p = lane; p < rec.n_parts; p += 32) m = fmaxf(m, ws.ml[slot(p)].x);
+    for (int p = lane; p < rec.n_parts; p += 32) m = fmaxf(m, ws.ml[slot(p, r)].x);
     m = warp_max(m);
     const float mu = m == -INFINITY ? 0.f : m;
     float l = 0.f, acc[DPL];
 #pragma unroll
     for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
-    for (int p0 = shared_row ? warp : 0; p0 < rec.n_parts; p0 += MERGE_LOADS * step) {
+    for (int p0 = warp; p0 < rec.n_parts; p0 += MERGE_LOADS * W) {
       float x[MERGE_LOADS][DPL];
       float2 ml[MERGE_LOADS];
 #pragma unroll
       for (int u = 0; u < MERGE_LOADS; ++u) {
-        const bool v = p0 + u * step < rec.n_parts;
-        ml[u] = v ? ws.ml[slot(p0 + u * step)] : make_float2(-INFINITY, 0.f);
-        const float* o = ws.o + slot(v ? p0 + u * step : p0) * DH + lane * DPL;
-#pragma unroll
-        for (int i = 0; i < DPL; i += 2) { const float2 y = *reinterpret_cast<const float2*>(o + i); x[u][i] = y.x; x[u][i + 1] = y.y; }
+        const bool v = p0 + u * W < rec.n_parts;
+        const int64_t at = slot(v ? p0 + u * W : p0, r);
+        ml[u] = v ? ws.ml[at] : make_float2(-INFINITY, 0.f);
+        load(at, x[u]);
       }
 #pragma unroll
       for (int u = 0; u < MERGE_LOADS; ++u) {
@@ -74,29 +127,22 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) split_merge_kernel(SplitWs w
         for (int i = 0; i < DPL; ++i) acc[i] = fmaf(w, x[u][i], acc[i]);
       }
     }
-    const int64_t dst = (int64_t)(rec.row0 + r / a.rep) * a.hq + rec.head0 + r % a.rep;
-    if (shared_row) {
 #pragma unroll
-      for (int i = 0; i < DPL; ++i) s_o[warp][lane * DPL + i] = acc[i];
-      if (lane == 0) s_l[warp] = l;
-      __syncthreads();
-      l = 0.f;
+    for (int i = 0; i < DPL; ++i) s_o[warp][lane * DPL + i] = acc[i];
+    if (lane == 0) s_l[warp] = l;
+    __syncthreads();
+    const int64_t dst = place(r);
+    l = 0.f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) l += s_l[w];
-      if ((int)threadIdx.x < DH) {
-        float o = 0.f;
+    for (int w = 0; w < W; ++w) l += s_l[w];
+    if ((int)threadIdx.x < DH) {
+      float o = 0.f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) o += s_o[w][threadIdx.x];
-        a.out[dst * DH + threadIdx.x] = from_f32<T>(l > 0.f ? o / l : 0.f);
-      }
-      if (threadIdx.x == 0 && a.lse) a.lse[dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
-      __syncthreads();
-    } else {
-      const float inv = l > 0.f ? 1.0f / l : 0.f;
-#pragma unroll
-      for (int i = 0; i < DPL; ++i) a.out[dst * DH + lane * DPL + i] = from_f32<T>(acc[i] * inv);
-      if (lane == 0 && a.lse) a.lse[dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
+      for (int w = 0; w < W; ++w) o += s_o[w][threadIdx.x];
+      a.out[dst * DH + threadIdx.x] = from_f32<T>(l > 0.f ? o / l : 0.f);
     }
+    if (threadIdx.x == 0 && a.lse) a.lse[dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
+    __syncthreads();
   }
 }
 
