@@ -220,7 +220,9 @@ struct MassCfg {
   static constexpr int HALVES = DH / 64;
   static constexpr int K_BYTES = 128 * DH * 2;              // one sub-tile of keys
   static constexpr int Q_BYTES = MS_ROWS * DH * 2;          // one tile of rows
-  static constexpr int NSQ = 3;
+  // An even number of slots: whoever serves every second step then serves the same slots every time and follows their
+  // barriers phase by phase (a parity wait says nothing to a waiter two phases behind).
+  static constexpr int NSQ = 4;
   static constexpr int SMEM = 2 * K_BYTES + NSQ * Q_BYTES + 1024 + 512 + NSQ * MS_ROWS * 4 + MS_KEYS * 4;
   static constexpr int THREADS = 640;                       // producer, issuer, two warps for the log-sums; four warpgroups of sums
 };
@@ -427,7 +429,7 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
     }
   } else if (warp >= 4) {
     // ------------------------------------------------------------------ sums: a warpgroup per (sub-tile x, step parity b)
-    // (With one warpgroup per sub-tile, two warps per scheduler, the exponential unit was half idle: 103 us against ... )
+    // (one warpgroup per sub-tile, two warps per scheduler, left the exponential unit idle for a third of the time)
     const int x = ((warp - 4) >> 2) & 1, b = (warp - 4) >> 3, quad = warp & 3, r = quad * 32 + lane;
     const uint32_t ts = tmem + ((uint32_t)(quad * 32) << 16) + x * 256 + b * 128;
     bool ok = true;
