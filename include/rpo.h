@@ -271,15 +271,18 @@ int rpo_sample_rows_noalloc(int32_t n_rows, int32_t vocab, const float* d_logits
  * keep every key.)
  *
  * The calls enqueue work on the context's stream, allocate nothing, do not synchronise and can be
- * captured into a CUDA graph; split work goes through workspaces of the context, so calls on one
- * context (replays of graphs that hold them included) must not overlap on the GPU.
+ * captured into a CUDA graph; split work goes through workspaces of the context (48 MB, taken at
+ * rpo_create), so calls on one context (replays of graphs that hold them included) must not overlap
+ * on the GPU.  Outputs must not overlap inputs except where said.  Results do not depend on the
+ * order in which the GPU finishes things: the same call gives the same bits.
  *
  * Device arrays are checked on the device: a length beyond the block table, a chunk offset out of
  * range, a chunk longer than max_chunk or a slot beyond the mass array is clamped and sets bit 3
  * of rpo_device_status; a block id outside the pool sets bit 2, nothing is written through it and
- * it reads as some block of the pool.  Block-table entries of tokens that no row can see are not
- * used.  Memory behind a sequence's last token, in its last block or elsewhere, may hold anything,
- * NaN included; keys and values that some row of the same sequence sees must be finite. */
+ * its tokens read as zeros or as some block of the pool.  Block-table entries of tokens that no row
+ * can see are not used.  Memory behind a sequence's last token, in its last block or elsewhere, may
+ * hold anything, NaN included; keys and values that some row of the same sequence sees must be
+ * finite.  An expired device-side wait sets bit 0, as everywhere. */
 typedef struct rpo_paged_kv {
   void* d_k;                     /* [n_kv_heads][n_blocks][16][head_dim], 16-byte aligned               */
   void* d_v;
@@ -310,7 +313,8 @@ typedef struct rpo_chunk_cfg {
  * unnormalised weights (as the rollout's own attention does) and the output.
  * Errors: RPO_ERR_INVALID_ARG (NULL, misaligned, scale <= 0, negative sizes), RPO_ERR_SHAPE (head_dim,
  * n_q_heads not a multiple of n_kv_heads or more than 64 query heads per KV head), RPO_ERR_LIMIT (more
- * than 4096 sequences, 2^30 rows x heads or 2^31 tokens x KV heads in the pool). */
+ * than 4096 sequences, 2^30 rows x heads, 2^31 tokens x KV heads in the pool, 2^31 table entries x KV
+ * heads, or 2^18 tiles of rows: at least 2^18 rows fit). */
 int rpo_chunk_attention(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_chunk,
                         const void* d_q, int64_t q_stride, const void* d_k_new, const void* d_v_new,
                         int64_t kv_new_stride, const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg, void* d_out,
@@ -322,7 +326,8 @@ int rpo_chunk_attention(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, in
  * for j < len; entries behind are left as they are.  The chunk's K must be in the cache, d_lse as
  * rpo_chunk_attention wrote it.  d_mass_in NULL: zeros; d_mass_out may be d_mass_in (accumulation
  * over steps).  Both float [n_seqs][n_kv_heads][mass_stride].  Sums are float32 in a fixed order.
- * Errors as in rpo_chunk_attention. */
+ * Errors as in rpo_chunk_attention; more than 2^18 x 256 cached tokens in a call with chunks of many
+ * rows are cut off and set bit 3 of the status word. */
 int rpo_attention_mass(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_chunk,
                        const void* d_q, int64_t q_stride, const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg,
                        const float* d_lse, const float* d_mass_in, float* d_mass_out, int32_t mass_stride);

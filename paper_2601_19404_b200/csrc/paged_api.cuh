@@ -28,7 +28,7 @@ constexpr int OP_MAX_SEQS = 4096, OP_MAX_REP = 64;
 static int check_chunk(const rpo_ctx* c, const rpo_paged_kv* kv, int n_rows, int hq, int max_chunk, const void* d_q, int64_t q_stride,
                        const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg) {
   RPO_TRY(check_paged(c, kv));
-  if (n_rows < 0 || hq <= 0 || max_chunk <= 0 || (n_rows > 0 && !d_q) || !d_q_offsets || !cfg || !(cfg->scale > 0.f) || std::isinf(cfg->scale) ||
+  if (n_rows < 0 || hq <= 0 || max_chunk <= 0 || (n_rows > 0 && !d_q) || !d_q_offsets || !cfg || !(cfg->scale > 0.f) || std::isinf(cfg->scale * 1.5f) ||
       cfg->window < 0 || cfg->sinks < 0 || !aligned16(d_q) || (q_stride * (int64_t)c->esz) % 16)
     return RPO_ERR_INVALID_ARG;
   if (hq % kv->n_kv_heads || hq / kv->n_kv_heads > OP_MAX_REP) return RPO_ERR_SHAPE;
@@ -50,7 +50,9 @@ static PagedView<T> paged_view(rpo_ctx* c, const rpo_paged_kv* kv) {
 
 static ChunkArgs chunk_args(int n_rows, int hq, int max_chunk, const int32_t* offsets, const rpo_chunk_cfg* cfg) {
   ChunkArgs a;
-  a.offsets = offsets; a.n_rows = n_rows; a.max_chunk = max_chunk; a.window = cfg->window; a.sinks = cfg->sinks; a.hq = hq;
+  // positions lie in (-2^30, 2^30): a longer window or more sinks see no more, and sums with them stay in 32 bits
+  constexpr int32_t most = 1 << 30;
+  a.offsets = offsets; a.n_rows = n_rows; a.max_chunk = max_chunk; a.window = std::min(cfg->window, most); a.sinks = std::min(cfg->sinks, most); a.hq = hq;
   return a;
 }
 
@@ -237,7 +239,9 @@ static int mass_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& a
   MassF32Args m;
   m.kv = view; m.c = a; m.q = q; m.q_stride = q_stride; m.scale_log2 = scale * 1.4426950408889634f; m.lse = lse; m.in = in; m.out = out;
   m.stride = stride; m.rep = a.hq / view.hkv;
-  const dim3 grid(ceil_div(std::min((int64_t)stride, (int64_t)view.table_stride * KV_BLOCK), MF_KEYS), view.hkv, view.n_seqs);
+  // every (sequence, KV head) has its CTAs, 16 per SM in all; they walk the key tiles there are, not those the table could hold
+  const int tiles = ceil_div(std::min((int64_t)stride, (int64_t)view.table_stride * KV_BLOCK), MF_KEYS);
+  const dim3 grid(std::min(tiles, ceil_div(16 * c->sm_count, (int64_t)view.hkv * view.n_seqs)), view.hkv, view.n_seqs);
   LAUNCH_OP(c, (mass_f32_kernel<DH, BM>), grid, 256, smem, m);
   return RPO_OK;
 }

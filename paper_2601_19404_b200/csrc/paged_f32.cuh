@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
   }
 }
 
-// Attention mass, 32-bit: a CTA owns 64 keys of one (sequence, KV head) and walks the rows that see any of them.  Thread
+// Attention mass, 32-bit: a CTA takes 64 keys of one (sequence, KV head) at a time and walks the rows that see any of them.  Thread
 // (ty, tx) sums its rows' weights for its keys; the sixteen ty of a key are added up in order at the end.
 struct MassF32Args {
   PagedView<float> kv; ChunkArgs c;
@@ -232,69 +232,71 @@ __global__ void __launch_bounds__(256) mass_f32_kernel(MassF32Args a) {
   constexpr int TM = BM / 16, KPT = MF_KEYS / 16, S = DH + 4, CPR = DH / 4;
   extern __shared__ __align__(16) float mf_smem[];
   float *sk = mf_smem, *sq = sk + MF_KEYS * S, *s_lse = sq + BM * S;
-  const int s = blockIdx.z, h = blockIdx.y, key0 = blockIdx.x * MF_KEYS, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, rep = a.rep;
+  const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, rep = a.rep;
   const ChunkSpan sp = chunk_span(a.kv, a.c, s);
   const int live = min(sp.len, a.stride);
   if (sp.len > a.stride && tid == 0) atomicOr(a.kv.status, STATUS_BAD_LENGTH);
-  if (key0 >= live) return;
   const int p0 = sp.len - sp.rows, p1 = sp.len - 1;
   const KeyPages kp = key_pages(a.c, p0, p1);
   const int32_t* tbl = a.kv.table + (int64_t)s * a.kv.table_stride;
-  for (int x = tid; x < MF_KEYS * CPR; x += 256) {
-    const int row = x / CPR, ch = x % CPR, page = key0 / KV_BLOCK + row / KV_BLOCK;
-    int blk = -1;
-    if (sp.rows > 0 && (page < kp.n_first || (page >= kp.lo_page && page < kp.end_page))) {
-      blk = tbl[page];
-      if (blk < 0 || blk >= a.kv.n_blocks) { atomicOr(a.kv.status, STATUS_BAD_BLOCK); blk = -1; }
-    }
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (blk >= 0) y = *reinterpret_cast<const float4*>(a.kv.k + h * a.kv.head_stride + ((int64_t)blk * KV_BLOCK + row % KV_BLOCK) * DH + ch * 4);
-    *reinterpret_cast<float4*>(sk + row * S + ch * 4) = y;
-  }
-  // tokens that see any of the keys
-  const int tok0 = max(0, key0 - p0);
-  int tok1 = sp.rows;
-  if (a.c.window > 0 && key0 >= a.c.sinks) tok1 = (int)min((int64_t)tok1, max((int64_t)0, (int64_t)key0 + MF_KEYS - 1 + a.c.window - p0));
-  float sum[KPT];
-#pragma unroll
-  for (int j = 0; j < KPT; ++j) sum[j] = 0.f;
-  for (int base = tok0 * rep; base < tok1 * rep; base += BM) {
-    __syncthreads();
-    for (int x = tid; x < BM * CPR; x += 256) {
-      const int r = base + x / CPR, ch = x % CPR;
+  for (int key0 = blockIdx.x * MF_KEYS; key0 < live; key0 += gridDim.x * MF_KEYS) {
+    __syncthreads();                                         // the last tile's keys and sums are read
+    for (int x = tid; x < MF_KEYS * CPR; x += 256) {
+      const int row = x / CPR, ch = x % CPR, page = key0 / KV_BLOCK + row / KV_BLOCK;
+      int blk = -1;
+      if (sp.rows > 0 && (page < kp.n_first || (page >= kp.lo_page && page < kp.end_page))) {
+        blk = tbl[page];
+        if (blk < 0 || blk >= a.kv.n_blocks) { atomicOr(a.kv.status, STATUS_BAD_BLOCK); blk = -1; }
+      }
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < tok1 * rep) y = *reinterpret_cast<const float4*>(a.q + (int64_t)(sp.row0 + r / rep) * a.q_stride + (h * rep + r % rep) * DH + ch * 4);
-      *reinterpret_cast<float4*>(sq + (x / CPR) * S + ch * 4) = y;
+      if (blk >= 0) y = *reinterpret_cast<const float4*>(a.kv.k + h * a.kv.head_stride + ((int64_t)blk * KV_BLOCK + row % KV_BLOCK) * DH + ch * 4);
+      *reinterpret_cast<float4*>(sk + row * S + ch * 4) = y;
     }
-    if (tid < BM) {
-      const int r = base + tid;
-      s_lse[tid] = r < tok1 * rep ? a.lse[(int64_t)(sp.row0 + r / rep) * a.c.hq + h * rep + r % rep] * LOG2E_F : 0.f;
-    }
-    __syncthreads();
-    float acc[TM][KPT];
-    f32_scores<DH, TM, KPT>(sq, sk, ty * TM, tx, acc);
+    // tokens that see any of the keys
+    const int tok0 = max(0, key0 - p0);
+    int tok1 = sp.rows;
+    if (a.c.window > 0 && key0 >= a.c.sinks) tok1 = (int)min((int64_t)tok1, max((int64_t)0, (int64_t)key0 + MF_KEYS - 1 + a.c.window - p0));
+    float sum[KPT];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int r = base + ty * TM + i, p = r < tok1 * rep ? p0 + r / rep : -1;
-      const float ls = s_lse[ty * TM + i];
+    for (int j = 0; j < KPT; ++j) sum[j] = 0.f;
+    for (int base = tok0 * rep; base < tok1 * rep; base += BM) {
+      __syncthreads();
+      for (int x = tid; x < BM * CPR; x += 256) {
+        const int r = base + x / CPR, ch = x % CPR;
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < tok1 * rep) y = *reinterpret_cast<const float4*>(a.q + (int64_t)(sp.row0 + r / rep) * a.q_stride + (h * rep + r % rep) * DH + ch * 4);
+        *reinterpret_cast<float4*>(sq + (x / CPR) * S + ch * 4) = y;
+      }
+      if (tid < BM) {
+        const int r = base + tid;
+        s_lse[tid] = r < tok1 * rep ? a.lse[(int64_t)(sp.row0 + r / rep) * a.c.hq + h * rep + r % rep] * LOG2E_F : 0.f;
+      }
+      __syncthreads();
+      float acc[TM][KPT];
+      f32_scores<DH, TM, KPT>(sq, sk, ty * TM, tx, acc);
 #pragma unroll
-      for (int j = 0; j < KPT; ++j) {
-        const float w = fa::ex2(fmaf(acc[i][j], a.scale_log2, -ls));
-        sum[j] += chunk_visible(a.c, key0 + tx + 16 * j, p) ? w : 0.f;
+      for (int i = 0; i < TM; ++i) {
+        const int r = base + ty * TM + i, p = r < tok1 * rep ? p0 + r / rep : -1;
+        const float ls = s_lse[ty * TM + i];
+#pragma unroll
+        for (int j = 0; j < KPT; ++j) {
+          const float w = fa::ex2(fmaf(acc[i][j], a.scale_log2, -ls));
+          sum[j] += chunk_visible(a.c, key0 + tx + 16 * j, p) ? w : 0.f;
+        }
       }
     }
-  }
-  __syncthreads();
-  float* part = sq;                                          // [16][64]
+    __syncthreads();
+    float* part = sq;                                          // [16][64]
 #pragma unroll
-  for (int j = 0; j < KPT; ++j) part[ty * MF_KEYS + tx + 16 * j] = sum[j];
-  __syncthreads();
-  if (tid < MF_KEYS && key0 + tid < live) {
-    float x = 0.f;
+    for (int j = 0; j < KPT; ++j) part[ty * MF_KEYS + tx + 16 * j] = sum[j];
+    __syncthreads();
+    if (tid < MF_KEYS && key0 + tid < live) {
+      float x = 0.f;
 #pragma unroll
-    for (int y = 0; y < 16; ++y) x += part[y * MF_KEYS + tid];
-    const int64_t at = ((int64_t)s * a.kv.hkv + h) * a.stride + key0 + tid;
-    a.out[at] = (a.in ? a.in[at] : 0.f) + x;
+      for (int y = 0; y < 16; ++y) x += part[y * MF_KEYS + tid];
+      const int64_t at = ((int64_t)s * a.kv.hkv + h) * a.stride + key0 + tid;
+      a.out[at] = (a.in ? a.in[at] : 0.f) + x;
+    }
   }
 }
 
