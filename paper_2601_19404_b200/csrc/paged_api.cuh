@@ -232,7 +232,7 @@ static int mass_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& 
 template <int DH, int BM>
 static int mass_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& a, const float* q, int64_t q_stride, const float* lse, float scale,
                     const float* in, float* out, int stride) {
-  constexpr int smem = ((MF_KEYS + BM) * (DH + 4) + BM) * 4;
+  constexpr int smem = ((MF_KEYS + 2 * BM) * (DH + 4) + 2 * BM) * 4;
   static bool attr_done[64] = {};
   if (tc_first_use_on_device(c, attr_done))
     CUDA_TRY(cudaFuncSetAttribute(mass_f32_kernel<DH, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));

@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
     }
   __syncthreads();
   walk.idx = s_first;
-  const uint32_t uk = (uint32_t)__cvta_generic_to_shared(sk), uv = (uint32_t)__cvta_generic_to_shared(sv);
+  const uint32_t uq = (uint32_t)__cvta_generic_to_shared(sq), uk = (uint32_t)__cvta_generic_to_shared(sk), uv = (uint32_t)__cvta_generic_to_shared(sv);
 
   while (walk.next()) {
     const int R = walk.it.n_tok * rep, p0 = walk.it.p0, p1 = p0 + walk.it.n_tok - 1;
@@ -111,15 +111,14 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
       }
       fa::cp_commit();
     };
-    lookup(walk.t0, blk);
-    load(uk, QS, kb, walk.t0, blk);
-    load(uv, DH, vb, walk.t0, blk);
     for (int x = tid; x < BM * CPR; x += 256) {
       const int r = x / CPR, ch = x % CPR;
-      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < R) y = *reinterpret_cast<const float4*>(a.q + (int64_t)(walk.it.row0 + r / rep) * a.q_stride + (walk.head * rep + r % rep) * DH + ch * 4);
-      *reinterpret_cast<float4*>(sq + r * QS + ch * 4) = y;
+      const bool live = r < R;
+      cp_async16_zfill(uq + (r * QS + ch * 4) * 4, a.q + (int64_t)(walk.it.row0 + (live ? r / rep : 0)) * a.q_stride + (walk.head * rep + (live ? r % rep : 0)) * DH + ch * 4, live);
     }
+    lookup(walk.t0, blk);
+    load(uk, QS, kb, walk.t0, blk);                          // (one group with the queries)
+    load(uv, DH, vb, walk.t0, blk);
     float o[TM][DG][4], m[TM], l[TM];
     int prow[TM];
 #pragma unroll
@@ -231,7 +230,7 @@ template <int DH, int BM>
 __global__ void __launch_bounds__(256) mass_f32_kernel(MassF32Args a) {
   constexpr int TM = BM / 16, KPT = MF_KEYS / 16, S = DH + 4, CPR = DH / 4;
   extern __shared__ __align__(16) float mf_smem[];
-  float *sk = mf_smem, *sq = sk + MF_KEYS * S, *s_lse = sq + BM * S;
+  float *sk = mf_smem, *sq = sk + MF_KEYS * S, *s_lse = sq + 2 * BM * S;      // two buffers of rows and log-sums
   const int s = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, rep = a.rep;
   const ChunkSpan sp = chunk_span(a.kv, a.c, s);
   const int live = min(sp.len, a.stride);
@@ -239,52 +238,67 @@ __global__ void __launch_bounds__(256) mass_f32_kernel(MassF32Args a) {
   const int p0 = sp.len - sp.rows, p1 = sp.len - 1;
   const KeyPages kp = key_pages(a.c, p0, p1);
   const int32_t* tbl = a.kv.table + (int64_t)s * a.kv.table_stride;
+  const uint32_t uk = (uint32_t)__cvta_generic_to_shared(sk), uq = (uint32_t)__cvta_generic_to_shared(sq), ul = (uint32_t)__cvta_generic_to_shared(s_lse);
   for (int key0 = blockIdx.x * MF_KEYS; key0 < live; key0 += gridDim.x * MF_KEYS) {
-    __syncthreads();                                         // the last tile's keys and sums are read
-    for (int x = tid; x < MF_KEYS * CPR; x += 256) {
-      const int row = x / CPR, ch = x % CPR, page = key0 / KV_BLOCK + row / KV_BLOCK;
-      int blk = -1;
-      if (sp.rows > 0 && (page < kp.n_first || (page >= kp.lo_page && page < kp.end_page))) {
-        blk = tbl[page];
-        if (blk < 0 || blk >= a.kv.n_blocks) { atomicOr(a.kv.status, STATUS_BAD_BLOCK); blk = -1; }
-      }
-      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (blk >= 0) y = *reinterpret_cast<const float4*>(a.kv.k + h * a.kv.head_stride + ((int64_t)blk * KV_BLOCK + row % KV_BLOCK) * DH + ch * 4);
-      *reinterpret_cast<float4*>(sk + row * S + ch * 4) = y;
-    }
     // tokens that see any of the keys
     const int tok0 = max(0, key0 - p0);
     int tok1 = sp.rows;
     if (a.c.window > 0 && key0 >= a.c.sinks) tok1 = (int)min((int64_t)tok1, max((int64_t)0, (int64_t)key0 + MF_KEYS - 1 + a.c.window - p0));
+    const int r_end = tok1 * rep;
+    auto load_rows = [&](int base, int buf) {                  // BM rows and their log-sums
+#pragma unroll
+      for (int e = 0; e < BM * CPR / 256; ++e) {
+        const int x = e * 256 + tid, r = base + x / CPR, ch = x % CPR;
+        const bool there = r < r_end;
+        cp_async16_zfill(uq + (buf * BM * S + (x / CPR) * S + ch * 4) * 4,
+                         a.q + (int64_t)(sp.row0 + (there ? r / rep : 0)) * a.q_stride + (h * rep + (there ? r % rep : 0)) * DH + ch * 4, there);
+      }
+      if (tid < BM && base + tid < r_end) {
+        const int r = base + tid;
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ul + (buf * BM + tid) * 4), "l"(a.lse + (int64_t)(sp.row0 + r / rep) * a.c.hq + h * rep + r % rep) : "memory");
+      }
+      fa::cp_commit();
+    };
+    __syncthreads();                                           // the last tile's keys and sums are read
+    int blk[MF_KEYS / KV_BLOCK];
+#pragma unroll
+    for (int i = 0; i < MF_KEYS / KV_BLOCK; ++i) {
+      const int page = key0 / KV_BLOCK + i;
+      blk[i] = -1;
+      if (sp.rows > 0 && (page < kp.n_first || (page >= kp.lo_page && page < kp.end_page))) {
+        blk[i] = tbl[page];
+        if (blk[i] < 0 || blk[i] >= a.kv.n_blocks) { if (tid == 0) atomicOr(a.kv.status, STATUS_BAD_BLOCK); blk[i] = -1; }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < MF_KEYS * CPR / 256; ++e) {
+      const int x = e * 256 + tid, row = x / CPR, ch = x % CPR, bk = blk[e * 256 / CPR / KV_BLOCK];
+      cp_async16_zfill(uk + (row * S + ch * 4) * 4, a.kv.k + h * a.kv.head_stride + ((int64_t)max(bk, 0) * KV_BLOCK + row % KV_BLOCK) * DH + ch * 4, bk >= 0);
+    }
     float sum[KPT];
 #pragma unroll
     for (int j = 0; j < KPT; ++j) sum[j] = 0.f;
-    for (int base = tok0 * rep; base < tok1 * rep; base += BM) {
-      __syncthreads();
-      for (int x = tid; x < BM * CPR; x += 256) {
-        const int r = base + x / CPR, ch = x % CPR;
-        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r < tok1 * rep) y = *reinterpret_cast<const float4*>(a.q + (int64_t)(sp.row0 + r / rep) * a.q_stride + (h * rep + r % rep) * DH + ch * 4);
-        *reinterpret_cast<float4*>(sq + (x / CPR) * S + ch * 4) = y;
-      }
-      if (tid < BM) {
-        const int r = base + tid;
-        s_lse[tid] = r < tok1 * rep ? a.lse[(int64_t)(sp.row0 + r / rep) * a.c.hq + h * rep + r % rep] * LOG2E_F : 0.f;
-      }
+    int buf = 0;
+    if (tok0 * rep < r_end) load_rows(tok0 * rep, 0);          // (one group with the keys)
+    for (int base = tok0 * rep; base < r_end; base += BM, buf ^= 1) {
+      if (base + BM < r_end) load_rows(base + BM, buf ^ 1); else fa::cp_commit();
+      fa::cp_wait<1>();
       __syncthreads();
       float acc[TM][KPT];
-      f32_scores<DH, TM, KPT>(sq, sk, ty * TM, tx, acc);
+      f32_scores<DH, TM, KPT>(sq + buf * BM * S, sk, ty * TM, tx, acc);
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        const int r = base + ty * TM + i, p = r < tok1 * rep ? p0 + r / rep : -1;
-        const float ls = s_lse[ty * TM + i];
+        const int r = base + ty * TM + i, p = r < r_end ? p0 + r / rep : -1;
+        const float ls = s_lse[buf * BM + ty * TM + i] * LOG2E_F;
 #pragma unroll
         for (int j = 0; j < KPT; ++j) {
           const float w = fa::ex2(fmaf(acc[i][j], a.scale_log2, -ls));
           sum[j] += chunk_visible(a.c, key0 + tx + 16 * j, p) ? w : 0.f;
         }
       }
+      __syncthreads();                                         // the buffer may be filled again
     }
+    fa::cp_wait<0>();
     __syncthreads();
     float* part = sq;                                          // [16][64]
 #pragma unroll

@@ -82,6 +82,9 @@ class Case:
         torch.cuda.synchronize()
         return out, d_lse
 
+    def attend_into(self, ctx, out):
+        ctx.chunk_attention(self.q, self.kv, self.d_off, self.max_chunk, out, window=self.window, sinks=self.sinks)
+
     def errors(self):
         """Per row and head: (relative error of a weight, error of the log-sum, sum of |w v|) by the header's bounds."""
         q, k, v = self.np(self.q), np.nan_to_num(self.np(self.k)), np.nan_to_num(self.np(self.v))
@@ -213,6 +216,46 @@ def test_attention_on_another_stream_and_in_a_graph():
             c.check(out, lse)
             del graph
         assert ctx.device_status() == 0
+
+
+FIRST_CALL = """
+import torch, paper_2601_19404_b200 as rpo
+s = torch.cuda.Stream()
+for dt, code in ((torch.bfloat16, 1), (torch.float32, 0)):
+    ctx = rpo.Context(rpo.shape_preset("tiny", dtype=code), kv_pool_blocks=8, max_groups=1, max_seqs=1, max_chunk_tokens=16, max_positions=32, stream=s)
+    for n in (1, 90):
+        k = torch.randn(2, 40, 16, 64, device="cuda").to(dt); v = torch.randn_like(k)
+        lens = torch.full((2,), 300, dtype=torch.int32, device="cuda")
+        kv = rpo.PagedKV(k, v, torch.arange(38, dtype=torch.int32, device="cuda").reshape(2, 19), lens)
+        q = torch.randn(2 * n, 4, 64, device="cuda").to(dt); off = torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda")
+        out = torch.zeros_like(q); lse = torch.zeros(2 * n, 4, device="cuda"); mass = torch.zeros(2, 2, 304, device="cuda")
+        pos = torch.arange(304, dtype=torch.int32, device="cuda").expand(2, 2, 304).contiguous()
+        src = torch.zeros(2, 2, 64, dtype=torch.int32, device="cuda"); n_out = torch.zeros(2, dtype=torch.int32, device="cuda")
+        m_out, p_out = torch.zeros(2, 2, 64, device="cuda"), torch.zeros(2, 2, 64, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            ctx.chunk_attention(q, kv, off, n, out, lse)
+            ctx.attention_mass(q, kv, off, n, lse, mass)
+            ctx.evict_cache(kv, mass, pos, 64, n_out, src, m_out, p_out)
+        with torch.cuda.stream(s):
+            g.replay()
+        torch.cuda.synchronize()
+        assert abs(mass.double().sum().item() - 8 * n) < 1e-3 * n and n_out.tolist() == [64, 64]
+        assert ctx.device_status() == 0
+        del g
+    ctx.close()
+print("captured")
+"""
+
+
+def test_a_process_may_capture_its_first_calls():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
@@ -475,8 +518,46 @@ def test_refusals(contexts):
     q32 = torch.zeros(4, 4, 32, dtype=torch.bfloat16, device=DEV)
     assert code(att, q32, kv32, c.d_off, 3, q32.clone()) == -2
     assert code(ctx.attention_mass, q32, kv32, c.d_off, 3, lse, mass) == -2
-    # no rows: nothing to do
-    none = torch.zeros(0, 4, 64, dtype=torch.bfloat16, device=DEV)
+    # no rows at all: nothing to attend, every weight stays
+    none, zero = torch.zeros(0, 4, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    att(none, c.kv, zero, 3, none.clone(), lse[:0])
+    start, got = torch.rand(2, 2, 40, device=DEV), torch.full((2, 2, 40), 5.0, device=DEV)
+    ctx.attention_mass(none, c.kv, zero, 3, lse[:0], got, d_mass_in=start)
     torch.cuda.synchronize()
+    assert torch.equal(got[0, :, :20], start[0, :, :20]) and torch.equal(got[1, :, :30], start[1, :, :30])
+    assert torch.all(got[0, :, 20:] == 5.0) and torch.all(got[1, :, 30:] == 5.0)
     assert ctx.device_status() == 0
-    del none
+
+
+def test_windows_and_sinks_beyond_every_position(contexts):
+    """Far beyond the cache they change nothing."""
+    for rows in (STEPS, CHUNKS):
+        c = Case("bf16", 4, 2, 64, *rows, seed=14)
+        _, lse = c.attend(contexts["bf16"])
+        for c.window, c.sinks in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 2 ** 31 - 1)):
+            c.check(*c.attend(contexts["bf16"]))
+            mass, same = torch.zeros(7, 2, 400, device=DEV), torch.zeros(7, 2, 400, device=DEV)
+            contexts["bf16"].attention_mass(c.q, c.kv, c.d_off, c.max_chunk, lse, mass, window=c.window, sinks=c.sinks)
+            contexts["bf16"].attention_mass(c.q, c.kv, c.d_off, c.max_chunk, lse, same)
+            # (the same weights, added up in the same tiles)
+            assert torch.allclose(mass, same, rtol=1e-5, atol=1e-30)
+    assert contexts["bf16"].device_status() == 0
+
+
+def test_two_contexts_at_once():
+    """Contexts own their workspaces: calls on two of them may overlap on the GPU."""
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    ctx = [rpo.Context(rpo.shape_preset("tiny", dtype=1), kv_pool_blocks=8, max_groups=1, max_seqs=1, max_chunk_tokens=16, max_positions=32, stream=s)
+           for s in streams]
+    cases = [Case("bf16", 12, 2, 128, [200, 3], [3000, 900], seed=31), Case("bf16", 12, 2, 128, [150, 90], [1000, 4000], seed=32)]
+    want = [c.attend(ctx[0])[0] for c in cases]
+    out = [[torch.zeros_like(w) for _ in range(10)] for w in want]
+    torch.cuda.synchronize()
+    for i in range(10):
+        for k in (0, 1):
+            cases[k].attend_into(ctx[k], out[k][i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[k]) for k in (0, 1) for o in out[k])
+    for x in ctx:
+        assert x.device_status() == 0
+        x.close()
