@@ -129,7 +129,7 @@ static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   RPO_TRY(op_map_pages(c, &km, view, view.k, DH));
   RPO_TRY(op_map_pages(c, &vm, view, view.v, DH));
   LAUNCH_OP(c, (chunk_prepare_kernel<bf16, DH, CH_BN / KV_BLOCK>), (prepare_grid<bf16, DH>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4,
-            items, plan, k_new, v_new, new_stride);
+            2, items, plan, k_new, v_new, new_stride);
   LAUNCH_OP(c, (paged_chunk_kernel<DH>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
   LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, OP_PART_ROWS / (MERGE_WARPS * MERGE_ROWS)), MERGE_WARPS * 32, 0, t.ws, t.o);
   return RPO_OK;
@@ -152,7 +152,7 @@ static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& 
   ChunkPlan* plan = (ChunkPlan*)(items + OP_MAX_ITEMS);
   f.items = items; f.plan = plan;
   const int grid = std::min(Cfg::CTAS * c->sm_count, OP_GRID * c->sm_count);
-  LAUNCH_OP(c, (chunk_prepare_kernel<float, DH, Cfg::BN / KV_BLOCK>), (prepare_grid<float, DH>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, f.tok, grid, 2, items,
+  LAUNCH_OP(c, (chunk_prepare_kernel<float, DH, Cfg::BN / KV_BLOCK>), (prepare_grid<float, DH>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, f.tok, grid, 2, 1, items,
             plan, k_new, v_new, new_stride);
   LAUNCH_OP(c, (paged_f32_kernel<DH, BM>), grid, 256, Cfg::SMEM, f);
   LAUNCH_OP(c, (split_merge_kernel<float, DH>), dim3(grid, BM == 64 ? BM / (MERGE_WARPS * MERGE_ROWS) : std::min(a.max_chunk * f.o.rep, BM)), MERGE_WARPS * 32, 0, f.ws, f.o);
@@ -223,7 +223,7 @@ static int mass_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& 
   CUtensorMap qm, km;
   RPO_TRY(op_map_rows(c, &qm, q, q_stride, a.n_rows, a.hq, DH, m.rep, m.tq));
   RPO_TRY(op_map_pages(c, &km, view, view.k, DH));
-  LAUNCH_OP(c, mass_plan_kernel, 1, 1024, view.n_seqs * 4, view, a, stride, m.tq, c->sm_count, 2, items, plan);
+  LAUNCH_OP(c, mass_plan_kernel, 1, 1024, view.n_seqs * 4, view, a, stride, m.tq, c->sm_count, 4, 2, items, plan);
   LAUNCH_OP(c, (mass_chunk_kernel<DH>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, m);
   LAUNCH_OP(c, mass_merge_kernel, c->sm_count, MS_KEYS, 0, m.ws, in, out);
   return RPO_OK;

@@ -31,7 +31,9 @@ constexpr int CH_HALF = CH_BN / 2;
 constexpr float CH_MOST = 1.0e12f;             // largest sum of a half's P that is taken without moving the reference
 
 struct ChunkItem { int first, n_tiles, row0, n_tok; int seq, p0, pad0, pad1; };   // p0: position of the item's first token
-struct ChunkPlan { int n_items, total, share, pad; };                        // `first`, `total`: in (tile, KV head)s
+// `first`, `total`, `share` count (tile, KV head)s, and `over` more for every (item, KV head): what filling the pipeline for
+// it and writing its result costs, in tiles, so that CTAs with many short pieces get fewer tiles.
+struct ChunkPlan { int n_items, total, share, over; };
 
 // Key tiles of an item: the sinks' pages, then the window's, each padded to whole tiles.
 template <int PAGES>
@@ -62,8 +64,8 @@ __device__ __forceinline__ void plan_scan(int64_t v, int64_t& before, int64_t& a
 // What a call needs before its main kernel: CTA 0 sums up the list of items (tok: tokens per item; PAGES: pages per key
 // tile), the others write the chunk's K and V to their pages.
 template <typename T, int DH, int PAGES>
-__global__ void __launch_bounds__(1024) chunk_prepare_kernel(PagedView<T> kv, ChunkArgs c, int tok, int n_ctas, int min_share, ChunkItem* items,
-                                                             ChunkPlan* plan, const T* __restrict__ k_new, const T* __restrict__ v_new,
+__global__ void __launch_bounds__(1024) chunk_prepare_kernel(PagedView<T> kv, ChunkArgs c, int tok, int n_ctas, int min_share, int over,
+                                                             ChunkItem* items, ChunkPlan* plan, const T* __restrict__ k_new, const T* __restrict__ v_new,
                                                              int64_t new_stride) {
   if (blockIdx.x > 0) {
     paged_append<T, DH>(kv, c, k_new, v_new, new_stride, blockIdx.x - 1, gridDim.x - 1);
@@ -94,7 +96,7 @@ __global__ void __launch_bounds__(1024) chunk_prepare_kernel(PagedView<T> kv, Ch
       const int t0 = (i - pl_first[lo]) * tok;
       it.seq = lo; it.n_tok = min(tok, sp.rows - t0); it.row0 = sp.row0 + t0; it.p0 = sp.len - sp.rows + t0;
       it.n_tiles = KeyTiles<PAGES>(c, it.p0, it.p0 + it.n_tok - 1).n;
-      n = (int64_t)it.n_tiles * kv.hkv;
+      n = (int64_t)(it.n_tiles + over) * kv.hkv;
     }
     int64_t before, all;
     plan_scan(n, before, all, s_warp);
@@ -107,26 +109,30 @@ __global__ void __launch_bounds__(1024) chunk_prepare_kernel(PagedView<T> kv, Ch
     if (i < n_items) items[i] = it;
     total += all;
   }
-  if (tid == 0) *plan = ChunkPlan{n_items, (int)total, max(min_share, (int)((total + n_ctas - 1) / n_ctas)), 0};
+  if (tid == 0) *plan = ChunkPlan{n_items, (int)total, max(min_share, (int)((total + n_ctas - 1) / n_ctas)), over};
 }
 
 // The pieces of one CTA, in order: every role of the CTA walks the same ones.
 struct PieceWalk {
   const ChunkItem* items;
-  int f, f_end, idx, hkv;
+  int f, f_end, idx, hkv, over;
   // of the current piece
   ChunkItem it; int head, t0, t1;
   __device__ __forceinline__ bool next() {
-    if (f >= f_end) return false;
-    it = items[idx];
-    if (f >= it.first + it.n_tiles * hkv) it = items[++idx];           // items hold at least one tile
-    const int in_item = f - it.first;
-    head = in_item / it.n_tiles;
-    t0 = in_item % it.n_tiles;
-    t1 = min(it.n_tiles, t0 + (f_end - f));
-    f += t1 - t0;
-    return true;
+    while (f < f_end) {
+      it = items[idx];
+      if (f >= it.first + (it.n_tiles + over) * hkv) it = items[++idx];  // items hold at least one tile
+      const int w = it.n_tiles + over, in_item = f - it.first, v0 = in_item % w, v1 = min(w, v0 + (f_end - f));
+      head = in_item / w;
+      t0 = max(0, v0 - over);                                        // the first `over` places of an item hold no tile
+      t1 = v1 - over;
+      f += v1 - v0;
+      if (t0 < t1) return true;
+    }
+    return false;
   }
+  // CTAs that work on the current (item, KV head), when it begins in CTA b.
+  __device__ __forceinline__ int parts(int share, int b) const { return (it.first + (head + 1) * (it.n_tiles + over) - 1) / share - b + 1; }
 };
 
 template <int DH>
@@ -260,13 +266,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
   tc::tmem_fence_after();
   const uint32_t tmem = *tmem_slot;
   PieceWalk walk;
-  walk.items = a.items; walk.hkv = hkv;
+  walk.items = a.items; walk.hkv = hkv; walk.over = plan.over;
   walk.f = (int)min((int64_t)plan.total, (int64_t)blockIdx.x * plan.share);
   walk.f_end = (int)min((int64_t)plan.total, (int64_t)(blockIdx.x + 1) * plan.share);
   if (walk.f < walk.f_end)
     for (int i = threadIdx.x; i < plan.n_items; i += Cfg::THREADS) {
       const int2 x = *reinterpret_cast<const int2*>(a.items + i);      // (first, n_tiles)
-      if (x.x <= walk.f && walk.f < x.x + x.y * hkv) *s_first = i;
+      if (x.x <= walk.f && walk.f < x.x + (x.y + plan.over) * hkv) *s_first = i;
     }
   __syncthreads();
   walk.idx = *s_first;
@@ -542,8 +548,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         else if (a.o.lse) a.o.lse[dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
       }
       if (begins && !ends && x == 0 && quad == 2 && lane == 0)
-        a.ws.rec[blockIdx.x] = SplitRec{walk.it.row0, walk.head * rep, walk.it.n_tok * rep,
-                                        (walk.it.first + (walk.head + 1) * walk.it.n_tiles - 1) / plan.share - (int)blockIdx.x + 1};
+        a.ws.rec[blockIdx.x] = SplitRec{walk.it.row0, walk.head * rep, walk.it.n_tok * rep, walk.parts(plan.share, blockIdx.x)};
     }
   }
   // teardown

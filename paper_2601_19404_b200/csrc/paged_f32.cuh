@@ -70,14 +70,14 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
   const ChunkPlan plan = *a.plan;
   if (tid == 0) { a.ws.rec[blockIdx.x] = SplitRec{0, 0, 0, 0}; s_first = 0; }
   PieceWalk walk;
-  walk.items = a.items; walk.hkv = hkv;
+  walk.items = a.items; walk.hkv = hkv; walk.over = plan.over;
   walk.f = (int)min((int64_t)plan.total, (int64_t)blockIdx.x * plan.share);
   walk.f_end = (int)min((int64_t)plan.total, (int64_t)(blockIdx.x + 1) * plan.share);
   __syncthreads();
   if (walk.f < walk.f_end)
     for (int i = tid; i < plan.n_items; i += 256) {
       const int2 x = *reinterpret_cast<const int2*>(a.items + i);
-      if (x.x <= walk.f && walk.f < x.x + x.y * hkv) s_first = i;
+      if (x.x <= walk.f && walk.f < x.x + (x.y + plan.over) * hkv) s_first = i;
     }
   __syncthreads();
   walk.idx = s_first;
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
       }
     }
     if (begins && !ends && tid == 0)
-      a.ws.rec[blockIdx.x] = SplitRec{walk.it.row0, walk.head * rep, R, (walk.it.first + (walk.head + 1) * walk.it.n_tiles - 1) / plan.share - (int)blockIdx.x + 1};
+      a.ws.rec[blockIdx.x] = SplitRec{walk.it.row0, walk.head * rep, R, walk.parts(plan.share, blockIdx.x)};
     __syncthreads();                                         // the next piece overwrites Q, K and V
   }
 }

@@ -168,7 +168,7 @@ struct MassWs { float* part; SplitRec* rec; };                                  
 
 constexpr int MS_KEYS = 256, MS_ROWS = 128;
 
-__global__ void __launch_bounds__(1024) mass_plan_kernel(PagedView<bf16> kv, ChunkArgs c, int stride, int tq, int n_ctas, int min_share,
+__global__ void __launch_bounds__(1024) mass_plan_kernel(PagedView<bf16> kv, ChunkArgs c, int stride, int tq, int n_ctas, int min_share, int over,
                                                          MassItem* items, ChunkPlan* plan) {
   extern __shared__ int pl_first[];                    // items of the sequences before s
   __shared__ int64_t s_warp[32];
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(1024) mass_plan_kernel(PagedView<bf16> kv, Chu
       int end = sp.rows;
       if (c.window > 0 && it.key0 >= c.sinks) end = (int)min((int64_t)end, (int64_t)it.key0 + MS_KEYS - 1 + c.window - p0);
       it.steps = max(1, (end - it.tok0 + tq - 1) / tq);                // (none: one step in which nothing is seen)
-      n = (int64_t)it.steps * kv.hkv;
+      n = (int64_t)(it.steps + over) * kv.hkv;
       if (sp.len > stride) atomicOr(kv.status, STATUS_BAD_LENGTH);
     }
     int64_t before, all;
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(1024) mass_plan_kernel(PagedView<bf16> kv, Chu
     if (i < n_items) items[i] = it;
     total += all;
   }
-  if (tid == 0) *plan = ChunkPlan{n_items, (int)total, max(min_share, (int)((total + n_ctas - 1) / n_ctas)), 0};
+  if (tid == 0) *plan = ChunkPlan{n_items, (int)total, max(min_share, (int)((total + n_ctas - 1) / n_ctas)), over};
 }
 
 template <int DH>
@@ -318,19 +318,23 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
   if (f < f_end)
     for (int i = threadIdx.x; i < plan.n_items; i += Cfg::THREADS) {
       const int2 x = *reinterpret_cast<const int2*>(a.items + i);
-      if (x.x <= f && f < x.x + x.y * hkv) *s_first = i;
+      if (x.x <= f && f < x.x + (x.y + plan.over) * hkv) *s_first = i;
     }
   __syncthreads();
   int idx = *s_first, head = 0, t0 = 0, t1 = 0;
   MassItem it = {};
   auto next = [&]() {                                        // the next piece: every role walks the same ones
-    if (f >= f_end) return false;
-    it = a.items[idx];
-    if (f >= it.first + it.steps * hkv) it = a.items[++idx];
-    head = (f - it.first) / it.steps; t0 = (f - it.first) % it.steps;
-    t1 = min(it.steps, t0 + (f_end - f));
-    f += t1 - t0;
-    return true;
+    while (f < f_end) {
+      it = a.items[idx];
+      if (f >= it.first + (it.steps + plan.over) * hkv) it = a.items[++idx];
+      const int w = it.steps + plan.over, v0 = (f - it.first) % w, v1 = min(w, v0 + (f_end - f));
+      head = (f - it.first) / w;
+      t0 = max(0, v0 - plan.over);                           // the first `over` places of an item hold no step
+      t1 = v1 - plan.over;
+      f += v1 - v0;
+      if (t0 < t1) return true;
+    }
+    return false;
   };
 
   if (warp == 0) {
@@ -497,7 +501,7 @@ mass_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_consta
         a.ws.part[(int64_t)(2 * blockIdx.x + (begins ? 1 : 0)) * MS_KEYS + x * 128 + r] = sum;
         if (begins && x == 0 && quad == 0 && lane == 0)
           a.ws.rec[blockIdx.x] = SplitRec{(int)(at & 0x7FFFFFFF), (int)(at >> 31), min(live, MS_KEYS),
-                                          (it.first + (head + 1) * it.steps - 1) / plan.share - (int)blockIdx.x + 1};
+                                          (it.first + (head + 1) * (it.steps + plan.over) - 1) / plan.share - (int)blockIdx.x + 1};
       }
     }
   }
