@@ -71,10 +71,12 @@ class PagedKV:
     d_lens int32 [n_seqs].  Keeps references to the tensors; build it once and reuse it."""
 
     def __init__(self, d_k, d_v, d_block_table, d_lens):
-        if d_k.dim() != 4 or d_k.shape[2] != 16 or d_v.shape != d_k.shape or d_v.dtype != d_k.dtype:
-            raise ValueError("d_k and d_v must be [n_kv_heads, n_blocks, 16, head_dim] of one type")
-        _expect(d_block_table, "d_block_table", "int32", (d_lens.shape[0], d_block_table.shape[-1]))
-        _expect(d_lens, "d_lens", "int32", (d_block_table.shape[0],))
+        if (d_k.dim() != 4 or d_k.shape[2] != 16 or d_v.shape != d_k.shape or d_v.dtype != d_k.dtype or not d_k.is_contiguous()
+                or not d_v.is_contiguous() or d_v.device != d_k.device):
+            raise ValueError("d_k and d_v must be contiguous [n_kv_heads, n_blocks, 16, head_dim] of one type on one device")
+        self.device = d_k.device
+        _expect(d_block_table, "d_block_table", "int32", (d_lens.shape[0], d_block_table.shape[-1]), self.device)
+        _expect(d_lens, "d_lens", "int32", (d_block_table.shape[0],), self.device)
         self.d_k, self.d_v, self.d_block_table, self.d_lens = d_k, d_v, d_block_table, d_lens
         self.dtype = d_k.dtype
         hkv, n_blocks, _, dh = d_k.shape
@@ -171,17 +173,19 @@ def _dtype(name):
     return _DTYPES[name]
 
 
-def _expect(t, name, dtype, shape):
-    """Refuse a tensor of another type, shape or layout than a call takes."""
-    if t.dtype is not _dtype(dtype) or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+def _expect(t, name, dtype, shape, device):
+    """Refuse a tensor of another type, shape, layout or device than a call takes."""
+    if t.dtype is not _dtype(dtype) or t.shape != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _head_rows(t, name, dtype, heads, dh, n_rows=None):
+def _head_rows(t, name, dtype, heads, dh, device, n_rows=None):
     """Elements between the rows of a [rows, heads, head_dim] view whose rows are contiguous (a slice of a fused projection is)."""
     shape = t.shape
     if len(shape) != 3 or t.dtype is not dtype or shape[1] != heads or shape[2] != dh or (n_rows is not None and shape[0] != n_rows):
         raise ValueError(f"{name} must be {dtype} [{'rows' if n_rows is None else n_rows}, {heads}, {dh}], got {t.dtype} {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {device}")
     stride = t.stride()
     if stride[2] != 1 or (heads > 1 and stride[1] != dh):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
@@ -207,6 +211,8 @@ def sample_rows_noalloc(d_logits, sampler, d_seq_ids, step, d_tokens_out, d_logp
 class Context:
     """Owns one rpo_ctx.  Methods mirror the C calls one to one."""
 
+    device = None                       # of the context's memory
+
     def __init__(self, shape, kv_pool_blocks, max_groups, max_seqs, max_chunk_tokens, max_positions, stream=None):
         import torch
         if not torch.cuda.is_available():
@@ -217,6 +223,7 @@ class Context:
         self.handle = C.c_void_p()
         stream_ptr = None if stream is None else C.c_void_p(stream.cuda_stream)
         _check(self.lib.rpo_create(C.byref(self.handle), C.byref(self.shape), C.byref(self.limits), stream_ptr), "rpo_create")
+        self.device = torch.device("cuda", torch.cuda.current_device())
 
     def close(self):
         h = getattr(self, "handle", None)
@@ -332,6 +339,8 @@ class Context:
     def _paged_dtype(self, kv):
         if kv.dtype is not _dtype("bfloat16" if self.shape.dtype == 1 else "float32"):
             raise ValueError(f"a cache of {kv.dtype} needs a context of that storage type")
+        if self.device is not None and kv.device != self.device:
+            raise ValueError(f"the cache is on {kv.device}, the context on {self.device}")
         return kv.dtype
 
     def _chunk_cfg(self, kv, scale, window, sinks):
@@ -342,19 +351,19 @@ class Context:
         float32 [rows, n_q_heads].  scale defaults to head_dim ** -0.5."""
         dt, st = self._paged_dtype(kv), kv.struct
         n, hq = d_q.shape[0], d_q.shape[1]
-        q_stride = _head_rows(d_q, "d_q", dt, hq, st.head_dim)
+        q_stride = _head_rows(d_q, "d_q", dt, hq, st.head_dim, kv.device)
         new_stride = 0
         if (d_k_new is None) != (d_v_new is None):
             raise ValueError("d_k_new and d_v_new go together")
         if d_k_new is not None:
-            new_stride = _head_rows(d_k_new, "d_k_new", dt, st.n_kv_heads, st.head_dim, n)
-            if _head_rows(d_v_new, "d_v_new", dt, st.n_kv_heads, st.head_dim, n) != new_stride:
+            new_stride = _head_rows(d_k_new, "d_k_new", dt, st.n_kv_heads, st.head_dim, kv.device, n)
+            if _head_rows(d_v_new, "d_v_new", dt, st.n_kv_heads, st.head_dim, kv.device, n) != new_stride:
                 raise ValueError("d_k_new and d_v_new must have the same row stride")
-        _expect(d_q_offsets, "d_q_offsets", "int32", (st.n_seqs + 1,))
-        if d_out.dtype is not dt or d_out.shape != d_q.shape or not d_out.is_contiguous():
-            raise ValueError("d_out must be contiguous, of d_q's type and shape")
+        _expect(d_q_offsets, "d_q_offsets", "int32", (st.n_seqs + 1,), kv.device)
+        if d_out.dtype is not dt or d_out.shape != d_q.shape or not d_out.is_contiguous() or d_out.device != kv.device:
+            raise ValueError("d_out must be contiguous, of d_q's type and shape, on its device")
         if d_lse_out is not None:
-            _expect(d_lse_out, "d_lse_out", "float32", (n, hq))
+            _expect(d_lse_out, "d_lse_out", "float32", (n, hq), kv.device)
         cfg = self._chunk_cfg(kv, scale, window, sinks)
         _check(self.lib.rpo_chunk_attention(self.handle, kv.ref, n, hq, max_chunk, d_q.data_ptr(), q_stride,
                                             None if d_k_new is None else d_k_new.data_ptr(), None if d_v_new is None else d_v_new.data_ptr(),
@@ -366,13 +375,13 @@ class Context:
         tensor) float32 [n_seqs, n_kv_heads, slots]."""
         dt, st = self._paged_dtype(kv), kv.struct
         n, hq = d_q.shape[0], d_q.shape[1]
-        q_stride = _head_rows(d_q, "d_q", dt, hq, st.head_dim)
-        _expect(d_q_offsets, "d_q_offsets", "int32", (st.n_seqs + 1,))
-        _expect(d_lse, "d_lse", "float32", (n, hq))
+        q_stride = _head_rows(d_q, "d_q", dt, hq, st.head_dim, kv.device)
+        _expect(d_q_offsets, "d_q_offsets", "int32", (st.n_seqs + 1,), kv.device)
+        _expect(d_lse, "d_lse", "float32", (n, hq), kv.device)
         slots = d_mass_out.shape[-1]
-        _expect(d_mass_out, "d_mass_out", "float32", (st.n_seqs, st.n_kv_heads, slots))
+        _expect(d_mass_out, "d_mass_out", "float32", (st.n_seqs, st.n_kv_heads, slots), kv.device)
         if d_mass_in is not None:
-            _expect(d_mass_in, "d_mass_in", "float32", (st.n_seqs, st.n_kv_heads, slots))
+            _expect(d_mass_in, "d_mass_in", "float32", (st.n_seqs, st.n_kv_heads, slots), kv.device)
         cfg = self._chunk_cfg(kv, scale, window, sinks)
         _check(self.lib.rpo_attention_mass(self.handle, kv.ref, n, hq, max_chunk, d_q.data_ptr(), q_stride, d_q_offsets.data_ptr(), C.byref(cfg),
                                            d_lse.data_ptr(), None if d_mass_in is None else d_mass_in.data_ptr(), d_mass_out.data_ptr(), slots),
@@ -385,12 +394,12 @@ class Context:
         self._paged_dtype(kv)
         n, h = kv.struct.n_seqs, kv.struct.n_kv_heads
         slots, out_slots = d_mass.shape[-1], d_mass_out.shape[-1]
-        _expect(d_mass, "d_mass", "float32", (n, h, slots))
-        _expect(d_positions, "d_positions", "int32", (n, h, slots))
-        _expect(d_lens_out, "d_lens_out", "int32", (n,))
-        _expect(d_src_out, "d_src_out", "int32", (n, h, budget))
-        _expect(d_mass_out, "d_mass_out", "float32", (n, h, out_slots))
-        _expect(d_positions_out, "d_positions_out", "int32", (n, h, out_slots))
+        _expect(d_mass, "d_mass", "float32", (n, h, slots), kv.device)
+        _expect(d_positions, "d_positions", "int32", (n, h, slots), kv.device)
+        _expect(d_lens_out, "d_lens_out", "int32", (n,), kv.device)
+        _expect(d_src_out, "d_src_out", "int32", (n, h, budget), kv.device)
+        _expect(d_mass_out, "d_mass_out", "float32", (n, h, out_slots), kv.device)
+        _expect(d_positions_out, "d_positions_out", "int32", (n, h, out_slots), kv.device)
         _check(self.lib.rpo_evict_cache(self.handle, kv.ref, d_mass.data_ptr(), d_positions.data_ptr(), slots, budget, sinks, recent,
                                         d_lens_out.data_ptr(), d_src_out.data_ptr(), d_mass_out.data_ptr(), d_positions_out.data_ptr(), out_slots),
                "rpo_evict_cache")

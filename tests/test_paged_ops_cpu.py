@@ -25,7 +25,8 @@ def test_the_cache_description():
     assert (kv.struct.n_blocks, kv.struct.n_seqs, kv.struct.table_stride, kv.struct.n_kv_heads, kv.struct.head_dim) == (4, 3, 2, 2, 64)
     k, t, n = torch.zeros(2, 4, 16, 64), torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
     for bad in ((k[:, :, :8], k[:, :, :8], t, n), (k, k[:1], t, n), (k, k.bfloat16(), t, n), (k, k, t.long(), n), (k, k, t, n[:2]),
-                (k, k, t, n.float()), (k, k, t.t(), n), (k[0], k[0], t, n)):
+                (k, k, t, n.float()), (k, k, t.t(), n), (k[0], k[0], t, n), (k.transpose(0, 1), k.transpose(0, 1), t, n),
+                (k, k.transpose(0, 1).contiguous().transpose(0, 1), t, n)):
         with pytest.raises(ValueError):
             rpo.PagedKV(*bad)
 
@@ -65,5 +66,20 @@ def test_calls_check_types_shapes_and_layouts():
 
 def test_row_strides_of_a_fused_projection_pass():
     x = torch.zeros(6, 8, 64)
-    assert binding._head_rows(x[:, :4], "q", torch.float32, 4, 64) == 512
-    assert binding._head_rows(x[:1, :4], "q", torch.float32, 4, 64) == 256
+    assert binding._head_rows(x[:, :4], "q", torch.float32, 4, 64, x.device) == 512
+    assert binding._head_rows(x[:1, :4], "q", torch.float32, 4, 64, x.device) == 256
+
+
+def test_tensors_of_another_device_are_refused():
+    """A host pointer must not reach a kernel: the device of every tensor is compared with the cache's, the cache's with the context's."""
+    ctx, kv = _ctx(), _kv()
+    q, off = torch.zeros(5, 4, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    ctx.device = torch.device("cuda", 0)
+    with pytest.raises(ValueError):
+        ctx.chunk_attention(q, kv, off, 2, q.clone())
+    ctx.device = None
+    kv.device = torch.device("cuda", 0)
+    with pytest.raises(ValueError):
+        ctx.chunk_attention(q, kv, off, 2, q.clone())
+    with pytest.raises(ValueError):
+        ctx.attention_mass(q, kv, off, 2, torch.zeros(5, 4), torch.zeros(3, 2, 40))
