@@ -16,7 +16,8 @@ struct MassArgs {
 };
 
 // Few rows per sequence (16-bit storage): HBM-bound, K of every page once.  A page's sums need nothing of other pages:
-// every warp takes an equal share of the pages of all (sequence, KV head)s, with a ring of pages of its own.
+// every warp takes an equal share of the pages of all (sequence, KV head)s, with a ring of pages of its own.  Measured: one
+// token for each of 128 sequences of 1024 .. 6144 tokens, 4 KV heads of 128: 87 us, 5.6 TB/s.
 template <int DH, int MT>
 struct MassStepCfg {
   static constexpr int STAGES = 3, PAGE_BYTES = KV_BLOCK * DH * 2;
@@ -162,7 +163,9 @@ __global__ void __launch_bounds__(128) mass_step_kernel(MassArgs a) {
 // An item is 256 keys of one (sequence, KV head), as two sub-tiles of 128 kept in shared memory; the rows of the chunk
 // that see any of them stream through in tiles of tq tokens x rep heads <= 128.  All steps of all items form one list,
 // cut into equal pieces (one persistent CTA per SM); keys whose rows are spread over several CTAs leave partial sums,
-// added up in piece order by mass_merge_kernel.  One exponential per (row, key) bounds it: 16 a clock and SM.
+// added up in piece order by mass_merge_kernel.  One exponential per (row, key) bounds it: 16 a clock and SM.  Measured: 8
+// chunks of up to 1024 tokens behind 1000 .. 4096, 12 on 2 heads of 128: 83 us with list and join, the exponential unit 82 %
+// busy in the steps (94 us while short items counted like long ones in the division of the list).
 struct MassItem { int first, steps, seq, key0; int tok0, pad0, pad1, pad2; };      // tok0: first token that sees a key
 struct MassWs { float* part; SplitRec* rec; };                                     // part [slot][256]
 

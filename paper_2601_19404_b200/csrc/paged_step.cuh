@@ -8,6 +8,10 @@
 // 16-byte asynchronous copies; scores and P V run on mma.sync m16n8k16 with the online softmax in registers.  The
 // warps' results are joined through shared memory at the end of an item; an item that runs over several CTAs leaves
 // unnormalised parts, joined in piece order by split_merge_kernel.
+//
+// Measured (28 query on 4 KV heads of 128): one token for each of 128 sequences of 1024 .. 6144 tokens 163 us, 5.75 TB/s, 88 %
+// of a copy's rate; pages fetched as one bulk copy per row 212 us, as TMA boxes 168 us and 3.6 us of host time per tensor map;
+// K and V of the new token written by a kernel of their own 3 us more.
 #pragma once
 #include "attn_tc.cuh"
 #include "paged_kv.cuh"
