@@ -7,7 +7,7 @@
 // depend on their order, so only the movers' rows are touched, and since sources lie at or above `budget` and
 // destinations below it, all moves are independent and in place.
 //
-// One launch does all of it: a CTA, or a cluster of eight for long caches, per (sequence, KV head).  Weights are mapped to
+// One launch does all of it: a CTA, or a cluster of up to eight for long caches, per (sequence, KV head).  Weights are mapped to
 // an unsigned order and kept in registers (one read of weights and positions); a radix select (11 + 11 + 10 bits, shared-
 // memory counts, added up through the cluster) finds the last weight that stays; prefix sums in slot order settle ties
 // and number the holes; holes leave their slots in a shared list that the movers read; the rows are copied

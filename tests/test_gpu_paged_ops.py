@@ -318,16 +318,18 @@ def test_calls_of_many_steps_repeat_bit_for_bit(contexts, heads, new, lens):
 
 
 EVICT = [([40, 9, 0, 33, 34, 100], 33, 2, 5, 41), ([1000, 1025, 1024, 31], 1024, 4, 200, 1030), ([5000, 2], 64, 3, 10, 5000), ([17, 40], 1, 0, 1, 64),
-         ([200, 300], 16, 8, 8, 301), ([70000], 8191, 16, 500, 70001)]
+         ([200, 300], 16, 8, 8, 301), ([70000], 8191, 16, 500, 70001),
+         ([1700, 300, 5] * 20, 600, 4, 60, 1701), ([3000] * 9 + [100] * 21, 1000, 2, 30, 3001), ([9000, 16000, 70] * 20, 41, 4, 20, 16001),
+         ([20000] * 3 + [50] * 20, 3000, 8, 900, 20001)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("dh", [64, 128])
-@pytest.mark.parametrize("case", EVICT, ids=lambda c: str(c[1]))
+@pytest.mark.parametrize("case", EVICT, ids=lambda c: f"{len(c[0])}x{max(c[0])}to{c[1]}")
 @pytest.mark.parametrize("in_place", [False, True])
 def test_evict(contexts, dtype, dh, case, in_place):
     lens, budget, sinks, recent, slots = case
-    hkv = 1 if max(lens) > 10000 else 3
+    hkv = 1 if max(lens) > 5000 or len(lens) > 10 else 3
     rng = np.random.default_rng(budget)
     c = Case(dtype, hkv, hkv, dh, [0] * len(lens), lens, seed=1, bad=0.5)
     mass = (np.round(rng.exponential(size=(len(lens), hkv, slots)) * 8) / 8).astype(np.float32)       # many ties
