@@ -277,11 +277,12 @@ __global__ void __launch_bounds__(256) mass_f32_kernel(MassF32Args a) {
       const int x = e * 256 + tid, row = x / CPR, ch = x % CPR, bk = blk[e * 256 / CPR / KV_BLOCK];
       cp_async16_zfill(uk + (row * S + ch * 4) * 4, a.kv.k + h * a.kv.head_stride + ((int64_t)max(bk, 0) * KV_BLOCK + row % KV_BLOCK) * DH + ch * 4, bk >= 0);
     }
+    fa::cp_commit();                                           // a group of their own: waited for even if no row follows
     float sum[KPT];
 #pragma unroll
     for (int j = 0; j < KPT; ++j) sum[j] = 0.f;
     int buf = 0;
-    if (tok0 * rep < r_end) load_rows(tok0 * rep, 0);          // (one group with the keys)
+    if (tok0 * rep < r_end) load_rows(tok0 * rep, 0);
     for (int base = tok0 * rep; base < r_end; base += BM, buf ^= 1) {
       if (base + BM < r_end) load_rows(base + BM, buf ^ 1); else fa::cp_commit();
       fa::cp_wait<1>();

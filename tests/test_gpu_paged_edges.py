@@ -1,0 +1,43 @@
+"""The operators on a caller-owned paged cache at the edges of what the header allows; tolerances as derived in
+test_gpu_paged_ops.py."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import DEV
+from oracle import paged
+from test_gpu_paged_ops import U, Case, contexts  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def check_mass(ctx, c, slots, in_place=False):
+    """attention_mass of a Case against the definition, on log-sums of the definition; entries behind a sequence stay."""
+    q, k = c.np(c.q), np.nan_to_num(c.np(c.k))
+    mask = (c.window, c.sinks)
+    want = paged.attention_mass(q, k, c.table, c.lens, c.off, c.scale, slots, *mask)
+    lse = paged.chunk_attention(q, k, k, c.table, c.lens, c.off, c.scale, *mask)[1]
+    ew, _, _ = c.errors()
+    start = torch.rand(len(c.lens), c.hkv, slots, generator=torch.Generator().manual_seed(1)).to(DEV)
+    base = c.np(start)
+    live = np.broadcast_to(np.arange(slots)[None, None] < np.array(c.lens)[:, None, None], base.shape)
+    out = start.clone() if in_place else torch.full_like(start, 9.0)
+    ctx.attention_mass(c.q, c.kv, c.d_off, c.max_chunk, torch.from_numpy(lse.astype(np.float32)).to(DEV), out,
+                       d_mass_in=out if in_place else start, window=c.window, sinks=c.sinks)
+    torch.cuda.synchronize()
+    got, full = c.np(out), want + base
+    n = max(c.new) * (c.hq // c.hkv)
+    finite = lse[np.isfinite(lse)]
+    rel = ew.max() + U * (np.abs(finite).max() if finite.size else 0.0) + 2.0 ** -20 + (n + 2) * U
+    assert np.all(np.abs(got - full)[live] <= (rel * full + 1e-35)[live])
+    assert np.array_equal(got[~live], base[~live] if in_place else np.full_like(got[~live], 9.0))
+    assert ctx.device_status() == 0
+
+
+@pytest.mark.parametrize("new,sinks", [([1] * 64, 3), ([2] * 32 + [0] * 32, 70), ([0] * 40 + [9] * 24, 0)], ids=["steps", "sinks", "empty"])
+def test_32_bit_mass_goes_from_unseen_to_seen_keys(contexts, new, sinks):  # noqa: F811
+    """More tiles of keys than CTAs per (sequence, KV head): a CTA takes tiles that no row sees (between sinks and window, or
+    of a sequence without rows) before tiles that some row sees, in the same shared memory."""
+    c = Case("fp32", 8, 8, 64, new, [1200 + 13 * (s % 7) for s in range(64)], seed=41, window=150, sinks=sinks)
+    c.hide_pages()
+    check_mass(contexts["fp32"], c, 1300)
