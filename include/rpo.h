@@ -282,7 +282,8 @@ int rpo_sample_rows_noalloc(int32_t n_rows, int32_t vocab, const float* d_logits
  * its tokens read as zeros or as some block of the pool.  Block-table entries of tokens that no row
  * can see are not used.  Memory behind a sequence's last token, in its last block or elsewhere, may
  * hold anything, NaN included; keys and values that some row of the same sequence sees must be
- * finite.  An expired device-side wait sets bit 0, as everywhere. */
+ * finite, the values below 2^127 / length (unnormalised sums are float32).  An expired device-side
+ * wait sets bit 0, as everywhere. */
 typedef struct rpo_paged_kv {
   void* d_k;                     /* [n_kv_heads][n_blocks][16][head_dim], 16-byte aligned               */
   void* d_v;

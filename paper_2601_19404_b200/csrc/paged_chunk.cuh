@@ -11,8 +11,11 @@
 //   softmax          one warpgroup per sub-tile, one thread per row = TMEM lane: no shuffles, no exchange.  P = 2^(s - m)
 //                    goes back to tensor memory as bf16, over the S it came from
 //   O_x += P V       tcgen05.mma with A = P from tensor memory; accumulates over all tiles.  m is a reference, not
-//                    the running maximum: it moves (and the row's O is rescaled in place) only when a half's sum
-//                    outgrows 10^12, so halves without masked keys take no maximum at all.
+//                    the running maximum.  Halves with masked keys, and all halves until every row of a warp has a
+//                    reference, take the maximum and move m (rescaling the row's O in place) where it grows; later
+//                    halves take none and move m only where the half's sum exceeds CH_MOST, two per key: the sums
+//                    then stay within twice what weights of at most 1 would give (with a bound of 10^12 O left the
+//                    range of float32 for values above 3e26).
 //
 // S of a half is refilled as soon as P V of the same half of the tile before has been issued, so a softmax warp that
 // hands over one half finds the next one ready: with 128-key halves (S waits for the softmax of the whole tile before)
@@ -32,7 +35,7 @@ namespace rpo {
 constexpr int CH_BM = 128, CH_BN = 128;
 constexpr int64_t OP_MAX_TILES = ((int64_t)1 << 31) - (1 << 20);
 constexpr int CH_HALF = CH_BN / 2;
-constexpr float CH_MOST = 1.0e12f;             // largest sum of a half's P that is taken without moving the reference
+constexpr float CH_MOST = 2.0f * CH_HALF;      // largest sum of a half's P that is taken without moving the reference
 
 struct ChunkItem { int first, n_tiles, row0, n_tok; int seq, p0, pad0, pad1; };   // p0: position of the item's first token
 // `first`, `total`, `share` count (tile, KV head)s, and `over` more for every (item, KV head): what filling the pipeline for

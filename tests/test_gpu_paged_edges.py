@@ -41,3 +41,20 @@ def test_32_bit_mass_goes_from_unseen_to_seen_keys(contexts, new, sinks):  # noq
     c = Case("fp32", 8, 8, 64, new, [1200 + 13 * (s % 7) for s in range(64)], seed=41, window=150, sinks=sinks)
     c.hide_pages()
     check_mass(contexts["fp32"], c, 1300)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [1, 100], ids=["step", "chunk"])
+def test_large_values_behind_growing_scores(contexts, dtype, new):  # noqa: F811
+    """Values of 1e33 whose scores are 22 higher than those of the first keys, and than each other's 64 keys on: the sums stay
+    within what weights of about 1 give."""
+    c = Case(dtype, 4, 2, 64, [new, new], [1100, 801], seed=43)
+    c.q.mul_(0.02)
+    c.q[..., 0] = 8.0                                                     # a score is about the key's first element
+    c.v.mul_(1e33)
+    for s, n in enumerate(c.lens):
+        at = torch.arange(n, device=DEV)
+        page = torch.from_numpy(c.table[s]).to(DEV).long()[at // 16]
+        c.k[:, page, at % 16, 0] = torch.where(at < 300, 0.0, torch.where(at < 700, 22.0, 22.0 + (at - 700) // 64)).to(c.dtype)
+    c.check(*c.attend(contexts[dtype]))
+    assert contexts[dtype].device_status() == 0
