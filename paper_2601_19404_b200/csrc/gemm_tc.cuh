@@ -22,6 +22,7 @@
 #include "common.cuh"
 #include "context.h"
 #include "gemm_epi.cuh"
+#include "once_per_device.h"
 
 namespace rpo {
 
@@ -426,12 +427,11 @@ struct TcFuse {
 
 constexpr int TC_CTR_CAPACITY = 1 << 16;     // arrival counters of a split-K launch (ints)
 
-// cudaFuncSetAttribute has to be made once per device, not once per process.
-inline bool tc_first_use_on_device(rpo_ctx* c, bool (&done)[64]) {
-  const int d = (c->device >= 0 && c->device < 64) ? c->device : 0;
-  if (done[d]) return false;
-  done[d] = true;
-  return true;
+// More than 48 KB of dynamic shared memory for a kernel (always the same amount).
+template <auto KERNEL>
+inline cudaError_t allow_smem(rpo_ctx* c, int bytes) {
+  static OncePerDevice once;
+  return once.run(c->device, [&] { return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
 }
 
 inline void tc_fill_fuse(rpo_ctx* c, TcParams& p, const TcFuse* f) {
@@ -446,11 +446,7 @@ inline void tc_fill_fuse(rpo_ctx* c, TcParams& p, const TcFuse* f) {
 template <int BN, int EPI>
 inline int tc_launch(rpo_ctx* c, const CUtensorMap* ma, const CUtensorMap* mw, const TcParams& p, int grid) {
   using Cfg = TcCfg<BN>;
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done)) {
-    if (cudaFuncSetAttribute(gemm_tc_kernel<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM_BYTES) != cudaSuccess)
-      return RPO_ERR_CUDA;
-  }
+  if (allow_smem<gemm_tc_kernel<BN, EPI>>(c, Cfg::SMEM_BYTES) != cudaSuccess) return RPO_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid); cfg.blockDim = dim3(192); cfg.dynamicSmemBytes = Cfg::SMEM_BYTES; cfg.stream = c->stream;
   cudaLaunchAttribute attr[1];

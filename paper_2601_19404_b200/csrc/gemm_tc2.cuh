@@ -323,11 +323,6 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 template <int EPI, int RM>
 inline int tc2_launch(rpo_ctx* c, const CUtensorMap* ma, const CUtensorMap* mw, const TcParams& p) {
   using Cfg = Tc2Cfg<RM>;
-  static int max_clusters_dev[64];
-  static bool init_done[64] = {};
-  const int dev_i = (c->device >= 0 && c->device < 64) ? c->device : 0;
-  if (!init_done[dev_i]) { max_clusters_dev[dev_i] = -1; init_done[dev_i] = true; }
-  int& max_clusters = max_clusters_dev[dev_i];
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -336,15 +331,20 @@ inline int tc2_launch(rpo_ctx* c, const CUtensorMap* ma, const CUtensorMap* mw, 
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.blockDim = dim3(192); cfg.dynamicSmemBytes = Cfg::SMEM_BYTES; cfg.stream = c->stream;
   cfg.attrs = attr;
-  if (max_clusters < 0) {
-    if (cudaFuncSetAttribute(gemm_tc2_kernel<EPI, RM>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM_BYTES) != cudaSuccess)
-      return RPO_ERR_CUDA;
+  static OncePerDevice once;
+  static std::atomic<int> max_clusters_dev[OncePerDevice::DEVICES + 1];
+  std::atomic<int>& max_clusters = max_clusters_dev[c->device >= 0 && c->device < OncePerDevice::DEVICES ? c->device : OncePerDevice::DEVICES];
+  const cudaError_t rc = once.run(c->device, [&] {
+    const cudaError_t e = cudaFuncSetAttribute(gemm_tc2_kernel<EPI, RM>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM_BYTES);
+    if (e != cudaSuccess) return e;
     cfg.gridDim = dim3(2 * (c->sm_count / 2)); cfg.numAttrs = 1;
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, gemm_tc2_kernel<EPI, RM>, &cfg) != cudaSuccess || n < 1) { cudaGetLastError(); n = c->sm_count / 2; }
-    max_clusters = std::min(n, c->sm_count / 2);
-  }
-  const int clusters = std::min(p.tiles_m * p.tiles_n * p.splits, max_clusters);
+    max_clusters.store(std::min(n, c->sm_count / 2));
+    return cudaSuccess;
+  });
+  if (rc != cudaSuccess) return RPO_ERR_CUDA;
+  const int clusters = std::min(p.tiles_m * p.tiles_n * p.splits, max_clusters.load());
   cfg.gridDim = dim3(2 * clusters);
   cfg.numAttrs = c->pdl_now() ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, gemm_tc2_kernel<EPI, RM>, *ma, *mw, p) == cudaSuccess ? RPO_OK : RPO_ERR_CUDA;

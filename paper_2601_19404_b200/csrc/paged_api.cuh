@@ -67,9 +67,7 @@ template <int DH, int MT>
 static int chunk_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const bf16* k_new, const bf16* v_new,
                        int64_t new_stride, float scale, bf16* out, float* lse) {
   using Cfg = StepCfg<DH, MT>;
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(paged_step_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4));
+  CUDA_TRY((allow_smem<paged_step_kernel<DH, MT>>(c, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4)));
   const int grid = 2 * c->sm_count;
   StepArgs s;
   s.kv = view; s.c = a; s.q = q; s.q_stride = q_stride; s.k_new = k_new; s.v_new = v_new; s.new_stride = new_stride; s.scale_log2 = scale * 1.4426950408889634f;
@@ -113,9 +111,7 @@ template <int DH>
 static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const bf16* k_new, const bf16* v_new,
                       int64_t new_stride, float scale, bf16* out, float* lse) {
   using Cfg = ChunkCfg<DH>;
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(paged_chunk_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+  CUDA_TRY((allow_smem<paged_chunk_kernel<DH>>(c, Cfg::SMEM)));
   ChunkTcArgs t;
   t.kv = view; t.c = a; t.scale_log2 = scale * 1.4426950408889634f;
   t.o.out = out; t.o.lse = lse; t.o.hq = a.hq; t.o.rep = a.hq / view.hkv; t.ws = split_ws(c, OP_PART_ROWS);
@@ -140,9 +136,7 @@ template <int DH, int BM>
 static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& a, const float* q, int64_t q_stride, const float* k_new, const float* v_new,
                       int64_t new_stride, float scale, float* out, float* lse) {
   using Cfg = F32Cfg<DH, BM>;
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(paged_f32_kernel<DH, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+  CUDA_TRY((allow_smem<paged_f32_kernel<DH, BM>>(c, Cfg::SMEM)));
   F32Args f;
   f.kv = view; f.c = a; f.q = q; f.q_stride = q_stride; f.scale_log2 = scale * 1.4426950408889634f;
   f.o.out = out; f.o.lse = lse; f.o.hq = a.hq; f.o.rep = a.hq / view.hkv; f.ws = split_ws(c, BM);
@@ -197,9 +191,7 @@ template <int DH, int MT>
 static int mass_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const float* lse, float scale,
                       const float* in, float* out, int stride) {
   using Cfg = MassStepCfg<DH, MT>;
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(mass_step_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4));
+  CUDA_TRY((allow_smem<mass_step_kernel<DH, MT>>(c, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4)));
   MassArgs m;
   m.kv = view; m.c = a; m.q = q; m.q_stride = q_stride; m.scale_log2 = scale * 1.4426950408889634f; m.lse = lse; m.in = in; m.out = out;
   m.stride = stride; m.rep = a.hq / view.hkv;
@@ -211,9 +203,7 @@ template <int DH>
 static int mass_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const float* lse, float scale,
                       const float* in, float* out, int stride) {
   using Cfg = MassCfg<DH>;
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(mass_chunk_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+  CUDA_TRY((allow_smem<mass_chunk_kernel<DH>>(c, Cfg::SMEM)));
   MassTcArgs m;
   m.kv = view; m.c = a; m.scale_log2 = scale * 1.4426950408889634f; m.lse = lse; m.in = in; m.out = out; m.stride = stride;
   m.rep = a.hq / view.hkv; m.tq = MS_ROWS / m.rep;
@@ -233,9 +223,7 @@ template <int DH, int BM>
 static int mass_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& a, const float* q, int64_t q_stride, const float* lse, float scale,
                     const float* in, float* out, int stride) {
   constexpr int smem = ((MF_KEYS + 2 * BM) * (DH + 4) + 2 * BM) * 4;
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(mass_f32_kernel<DH, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  CUDA_TRY((allow_smem<mass_f32_kernel<DH, BM>>(c, smem)));
   MassF32Args m;
   m.kv = view; m.c = a; m.q = q; m.q_stride = q_stride; m.scale_log2 = scale * 1.4426950408889634f; m.lse = lse; m.in = in; m.out = out;
   m.stride = stride; m.rep = a.hq / view.hkv;
@@ -278,9 +266,7 @@ extern "C" int rpo_attention_mass(rpo_ctx* c, const rpo_paged_kv* kv, int32_t n_
 
 template <int THREADS, int KPT, int C>
 static int evict_launch(rpo_ctx* c, EvictArgs a) {
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(evict_kernel<THREADS, KPT, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (EV_MAX_STRIDE / 2 / 8 + 1) * 4));
+  CUDA_TRY((allow_smem<evict_kernel<THREADS, KPT, C>>(c, (EV_MAX_STRIDE / 2 / 8 + 1) * 4)));
   a.list_cap = ceil_div(std::max(1, std::min(a.budget, a.mass_stride / 2 + 1)), C);     // holes: at most half of the slots
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.n_seqs * a.hkv * C); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = (size_t)a.list_cap * 4; cfg.stream = c->stream;

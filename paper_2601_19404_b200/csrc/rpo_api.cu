@@ -506,9 +506,7 @@ static int rmsnorm(rpo_ctx* c, float* x, const float* g, T* h, int rows) {
 template <int DH, int MODE, bool CLM = false>
 static int launch_flash(rpo_ctx* c, const FlashArgs& a, dim3 grid) {
   constexpr int smem = FaCfg<MODE>::template smem_bytes<DH>();
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(flash_attn_kernel<DH, MODE, CLM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  CUDA_TRY((allow_smem<flash_attn_kernel<DH, MODE, CLM>>(c, smem)));
   if (CLM) c->launch_cluster_x = a.n_splits;         // the splits of a work item are consecutive along x
   LAUNCH(c, (flash_attn_kernel<DH, MODE, CLM>), grid, FaCfg<MODE>::THREADS + 32, smem, a);
   return RPO_OK;
@@ -549,15 +547,11 @@ static int attention(rpo_ctx* c, int layer, int rows) {
         f.hq = s.n_q_heads; f.hkv = s.n_kv_heads; f.scale_log2 = scale * 1.4426950408889634f; f.tiles = (const int2*)w.tiles;
         f.q_col0 = 0; f.status = c->d_status;
         if (c->use_tc5_pipelined) {                    // 64-key tiles, O accumulated in tensor memory
-          static bool p5_attr[64] = {};
-          if (tc_first_use_on_device(c, p5_attr))
-            CUDA_TRY(cudaFuncSetAttribute(flash_prefill_tc5_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, P5_SMEM));
+          CUDA_TRY((allow_smem<flash_prefill_tc5_kernel>(c, P5_SMEM)));
           LAUNCH(c, flash_prefill_tc5_kernel, dim3(s.n_q_heads, c->attn_tiles), 320, P5_SMEM, *qm, f);
           return RPO_OK;
         }
-        static bool attr_done[64] = {};
-        if (tc_first_use_on_device(c, attr_done))
-          CUDA_TRY(cudaFuncSetAttribute(flash_attn_tc5_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T5_SMEM));
+        CUDA_TRY((allow_smem<flash_attn_tc5_kernel>(c, T5_SMEM)));
         LAUNCH(c, flash_attn_tc5_kernel, dim3(s.n_q_heads, c->attn_tiles), 320, T5_SMEM, *qm, f);
         return RPO_OK;
       }
@@ -576,9 +570,7 @@ static int attention(rpo_ctx* c, int layer, int rows) {
         d5.block_table = c->d_block_table; d5.pool = kv_pool<bf16>(c);
         d5.layer = layer; d5.hq = s.n_q_heads; d5.hkv = s.n_kv_heads; d5.G = c->attn_G; d5.scale_log2 = a.scale_log2;
         d5.n_splits = c->attn_splits; d5.split_chunk = c->attn_split_chunk; d5.status = c->d_status;
-        static bool d5_attr[64] = {};
-        if (tc_first_use_on_device(c, d5_attr))
-          CUDA_TRY(cudaFuncSetAttribute(flash_decode_tc5_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, D5_SMEM));
+        CUDA_TRY((allow_smem<flash_decode_tc5_kernel>(c, D5_SMEM)));
         LAUNCH(c, flash_decode_tc5_kernel, dim3(c->attn_groups * c->attn_splits, s.n_kv_heads), 320, D5_SMEM, d5);
         const int mgrid = ceil_div((int64_t)rows * s.n_q_heads, 4);
         LAUNCH(c, (attn_decode_merge_kernel<128>), mgrid, 128, 0, a.out, a.part_ml, a.part_o, c->attn_splits, w.row_t, rows, a.hq);
@@ -906,9 +898,7 @@ extern "C" int rpo_release_groups(rpo_ctx* c, int32_t n_groups, const rpo_group*
 // decode
 // ---------------------------------------------------------------------------------------------
 static int launch_sampler(rpo_ctx* c, int n_rows, const SamplerArgs& a) {
-  static bool attr_done[64] = {};
-  if (tc_first_use_on_device(c, attr_done))
-    CUDA_TRY(cudaFuncSetAttribute(sampler_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SAMPLER_SMEM));
+  CUDA_TRY((allow_smem<sampler_kernel>(c, SAMPLER_SMEM)));
   ProfScope ps(c, KC_SAMPLER);
   LAUNCH(c, sampler_kernel, n_rows, 1024, SAMPLER_SMEM, a);
   return RPO_OK;

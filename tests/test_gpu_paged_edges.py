@@ -1,5 +1,9 @@
 """The operators on a caller-owned paged cache at the edges of what the header allows; tolerances as derived in
 test_gpu_paged_ops.py."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -58,3 +62,47 @@ def test_large_values_behind_growing_scores(contexts, dtype, new):  # noqa: F811
         c.k[:, page, at % 16, 0] = torch.where(at < 300, 0.0, torch.where(at < 700, 22.0, 22.0 + (at - 700) // 64)).to(c.dtype)
     c.check(*c.attend(contexts[dtype]))
     assert contexts[dtype].device_status() == 0
+
+
+FIRST_CALLS = """
+import threading, torch, paper_2601_19404_b200 as rpo
+N = 4
+streams = [torch.cuda.Stream() for _ in range(N)]
+ctx = [rpo.Context(rpo.shape_preset("tiny", dtype=1), kv_pool_blocks=8, max_groups=1, max_seqs=1, max_chunk_tokens=16, max_positions=32, stream=s)
+       for s in streams]
+work = []
+for i in range(N):
+    k = torch.randn(2, 40, 16, 128, device="cuda").bfloat16()
+    lens = torch.full((2,), 300, dtype=torch.int32, device="cuda")
+    kv = rpo.PagedKV(k, torch.randn_like(k), torch.arange(38, dtype=torch.int32, device="cuda").reshape(2, 19), lens)
+    for n in (1, 6, 90):                                       # a kernel of its own for each
+        q = torch.randn(2 * n, 8, 128, device="cuda").bfloat16(); off = torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda")
+        work.append((i, n, q, kv, off, torch.zeros_like(q), torch.zeros(2 * n, 8, device="cuda"), torch.zeros(2, 2, 304, device="cuda")))
+torch.cuda.synchronize()
+gate, failed = threading.Barrier(N), []
+def run(i):
+    try:
+        for j, n, q, kv, off, out, lse, mass in work:
+            if j == i:
+                gate.wait()
+                ctx[i].chunk_attention(q, kv, off, n, out, lse)
+                gate.wait()
+                ctx[i].attention_mass(q, kv, off, n, lse, mass)
+    except Exception as e:
+        failed.append(repr(e)); gate.abort()
+threads = [threading.Thread(target=run, args=(i,)) for i in range(N)]
+[t.start() for t in threads]; [t.join() for t in threads]
+torch.cuda.synchronize()
+assert not failed, failed
+for j, n, q, kv, off, out, lse, mass in work:
+    assert abs(mass.double().sum().item() - 16 * n) < 1e-3 * n, (j, n)
+assert all(c.device_status() == 0 for c in ctx)
+print("all done")
+"""
+
+
+def test_first_calls_from_several_threads():
+    """Contexts of several host threads, whose first launches of every kernel in the process come at once."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "all done" in r.stdout, r.stdout + r.stderr[-2000:]
