@@ -315,7 +315,7 @@ typedef struct rpo_chunk_cfg {
  * Errors: RPO_ERR_INVALID_ARG (NULL, misaligned, scale <= 0, negative sizes), RPO_ERR_SHAPE (head_dim,
  * n_q_heads not a multiple of n_kv_heads or more than 64 query heads per KV head), RPO_ERR_LIMIT (more
  * than 4096 sequences, 2^30 rows x heads, 2^31 tokens x KV heads in the pool, 2^31 table entries x KV
- * heads, or 2^18 tiles of rows: at least 2^18 rows fit). */
+ * heads, or 2^18 tiles of rows and one for every sequence: 2^18 rows always fit). */
 int rpo_chunk_attention(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_chunk,
                         const void* d_q, int64_t q_stride, const void* d_k_new, const void* d_v_new,
                         int64_t kv_new_stride, const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg, void* d_out,
@@ -327,8 +327,8 @@ int rpo_chunk_attention(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, in
  * for j < len; entries behind are left as they are.  The chunk's K must be in the cache, d_lse as
  * rpo_chunk_attention wrote it.  d_mass_in NULL: zeros; d_mass_out may be d_mass_in (accumulation
  * over steps).  Both float [n_seqs][n_kv_heads][mass_stride].  Sums are float32 in a fixed order.
- * Errors as in rpo_chunk_attention; more than 2^18 x 256 cached tokens in a call with chunks of many
- * rows are cut off and set bit 3 of the status word. */
+ * Errors as in rpo_chunk_attention; a call with chunks of many rows always takes 2^18 x 256 cached
+ * tokens; sequences beyond what fits are cut off and set bit 3 of the status word. */
 int rpo_attention_mass(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_chunk,
                        const void* d_q, int64_t q_stride, const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg,
                        const float* d_lse, const float* d_mass_in, float* d_mass_out, int32_t mass_stride);

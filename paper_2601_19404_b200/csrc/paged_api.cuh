@@ -23,7 +23,7 @@ static int check_paged(const rpo_ctx* c, const rpo_paged_kv* kv) {
   return RPO_OK;
 }
 
-constexpr int OP_MAX_SEQS = 4096, OP_MAX_REP = 64;
+constexpr int OP_MAX_REP = 64;
 
 static int check_chunk(const rpo_ctx* c, const rpo_paged_kv* kv, int n_rows, int hq, int max_chunk, const void* d_q, int64_t q_stride,
                        const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg) {

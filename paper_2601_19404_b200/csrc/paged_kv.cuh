@@ -11,9 +11,11 @@
 
 namespace rpo {
 
-// Workspace of the operators: rows of the largest part of a split item (two parts per CTA), items of one call.
+// Workspace of the operators: rows of the largest part of a split item (two parts per CTA), items of one call (2^18 full
+// ones, and one more for every sequence, whose last may not be full).
 constexpr int OP_GRID = 3;                // CTAs per SM at most in a kernel that leaves parts
-constexpr int OP_PART_ROWS = 256, OP_MAX_ITEMS = 1 << 18;
+constexpr int OP_MAX_SEQS = 4096;
+constexpr int OP_PART_ROWS = 256, OP_MAX_ITEMS = (1 << 18) + OP_MAX_SEQS;
 constexpr int STATUS_BAD_LENGTH = 8;      // a length, chunk offset or chunk size out of range (clamped)
 
 template <typename T>

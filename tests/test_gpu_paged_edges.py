@@ -8,6 +8,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2601_19404_b200 as rpo
 from gpu_util import DEV
 from oracle import paged
 from test_gpu_paged_ops import U, Case, contexts  # noqa: F401
@@ -106,3 +107,29 @@ def test_first_calls_from_several_threads():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "all done" in r.stdout, r.stdout + r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("rows", [1 << 18, (1 << 18) + 64])
+def test_the_largest_number_of_rows(contexts, rows):  # noqa: F811
+    """2^18 rows of 4096 sequences fit, in 32 bits with 64 query heads on a KV head too, where every row is an item; more
+    rows do not, and nothing is written.  Under a window of one token a row's output is its own value."""
+    n, hq, dh = 4096, 64, 64
+    new = [64] * n
+    new[0] += rows - (1 << 18)
+    off = torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)).to(DEV)
+    k = torch.zeros(1, n * 8, 16, dh, device=DEV)
+    kv = rpo.PagedKV(k, torch.zeros_like(k), torch.arange(n * 8, dtype=torch.int32, device=DEV).reshape(n, 8), torch.tensor(new, dtype=torch.int32, device=DEV))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    q = torch.randn(rows, hq, dh, generator=g, device=DEV)
+    k_new, v_new = torch.randn(rows, 1, dh, generator=g, device=DEV), torch.randn(rows, 1, dh, generator=g, device=DEV)
+    out, ctx = torch.full_like(q, 7.0), contexts["fp32"]
+    call = lambda: ctx.chunk_attention(q, kv, off, max(new), out, d_k_new=k_new, d_v_new=v_new, window=1)  # noqa: E731
+    if rows > 1 << 18:
+        with pytest.raises(rpo.RpoError) as e:
+            call()
+        assert e.value.code == -7
+    else:
+        call()
+    torch.cuda.synchronize()
+    assert bool((out == (7.0 if rows > 1 << 18 else v_new)).all()) and ctx.device_status() == 0
