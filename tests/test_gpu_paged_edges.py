@@ -11,7 +11,7 @@ import torch
 import paper_2601_19404_b200 as rpo
 from gpu_util import DEV
 from oracle import paged
-from test_gpu_paged_ops import U, Case, contexts  # noqa: F401
+from test_gpu_paged_ops import CHUNKS, LONG, STEPS, U, Case, contexts  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,84 @@ def test_the_largest_number_of_rows(contexts, rows):  # noqa: F811
         call()
     torch.cuda.synchronize()
     assert bool((out == (7.0 if rows > 1 << 18 else v_new)).all()) and ctx.device_status() == 0
+
+
+FEW = [((28, 4, 128), [4, 1, 0, 3, 4, 4, 2, 4], [300, 16, 40, 2, 17, 128, 18, 5003]), ((8, 1, 64), [3, 4, 0, 4, 1, 2], [50, 4, 9, 33, 0, 700]),
+       ((4, 2, 64), [16, 9, 13, 2, 16], [200, 9, 7, 65, 1000]), ((12, 2, 128), [5, 5, 1, 4], [36, 3, 17, 260]), ((32, 1, 64), [1, 1, 0, 1], [77, 16, 3, 1030])]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("few", FEW, ids=lambda f: "x".join(map(str, f[0])))
+@pytest.mark.parametrize("mask", [(0, 0), (1, 0), (3, 0), (70, 0), (33, 5), (20, 40)])
+def test_a_few_tokens_per_step(contexts, dtype, few, mask):  # noqa: F811
+    """17 to 32 rows per sequence and KV head: chunks over two pages, longer than their cache, written to it by the same call."""
+    heads, new, lens = few
+    c = Case(dtype, *heads, new, lens, seed=heads[0], extra_rows=2, window=mask[0], sinks=mask[1])
+    k, v = c.np(c.k), c.np(c.v)
+    for cache, fresh in ((k, c.k_new), (v, c.v_new)):
+        paged.append(cache, c.np(fresh), c.table, c.lens, c.off)
+    out, lse = c.attend(contexts[dtype], append=True)
+    assert np.array_equal(c.np(c.k), k, equal_nan=True) and np.array_equal(c.np(c.v), v, equal_nan=True)
+    c.check(out, lse)
+    again, lse2 = c.attend(contexts[dtype])
+    assert torch.equal(out, again) and torch.equal(lse, lse2)              # the same values, read from the cache now
+    c.hide_pages()
+    c.check(*c.attend(contexts[dtype]))
+    check_mass(contexts[dtype], c, max(lens) + 3)
+    check_mass(contexts[dtype], c, max(lens) + 3, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads", [(12, 2, 128), (3, 3, 64)])
+@pytest.mark.parametrize("rows", [STEPS, CHUNKS, LONG], ids=["steps", "chunks", "long"])
+@pytest.mark.parametrize("mask", [(20, 3), (100, 0)])
+def test_mass_does_not_use_hidden_pages(contexts, dtype, heads, rows, mask):  # noqa: F811
+    c = Case(dtype, *heads, *rows, seed=3, window=mask[0], sinks=mask[1])
+    c.hide_pages()
+    for in_place in (False, True):
+        check_mass(contexts[dtype], c, max(c.lens) + 5, in_place)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [[1] * 6, [3, 1, 4, 0, 2, 4], [40, 1, 129, 9, 0, 33]], ids=["steps", "few", "chunks"])
+def test_sequences_that_share_blocks(contexts, dtype, new):  # noqa: F811
+    """Continuations of one prefix: the prefix' whole pages are the same blocks, what is written lies behind them."""
+    lens = [160 + n + 7 * s for s, n in enumerate(new)]
+    c = Case(dtype, 12, 2, 128, new, lens, seed=51)
+    c.table[1:, :10] = c.table[0, :10]
+    c.kv.d_block_table.copy_(torch.from_numpy(c.table))
+    out, lse = c.attend(contexts[dtype], append=True)
+    c.check(out, lse)
+    check_mass(contexts[dtype], c, max(lens))
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("fp32", 64)])
+def test_a_pool_beyond_32_bit_offsets(contexts, dtype, dh):  # noqa: F811
+    """Blocks whose elements lie behind 2^31 of their KV head (and behind 2^32 bytes)."""
+    for new, lens in (([1, 1, 0], [100, 2000, 30]), ([4, 2, 3], [100, 500, 30]), ([90, 1, 33], [500, 100, 200])):
+        c = Case(dtype, 4, 2, dh, new, lens, seed=61)
+        used, blocks = c.k.shape[1], (1 << 31) // (16 * dh) + 64
+        pools = []
+        for cache in (c.k, c.v):
+            pool = torch.empty(2, blocks, 16, dh, dtype=c.dtype, device=DEV)
+            pool[:, blocks - used:] = cache
+            pools.append(pool)
+        table = np.where(c.table >= 0, c.table + blocks - used, c.table)
+        small, c.kv = c.kv, rpo.PagedKV(*pools, torch.from_numpy(table.astype(np.int32)).to(DEV), c.kv.d_lens)
+        out, lse = c.attend(contexts[dtype], append=True)
+        c.k, c.v = pools[0][:, blocks - used:], pools[1][:, blocks - used:]
+        c.check(out, lse)
+        check_mass(contexts[dtype], c, max(lens))
+        # the same eviction in the large pool and in a small one
+        small = rpo.PagedKV(c.k.contiguous(), c.v.contiguous(), small.d_block_table, small.d_lens)
+        mass = torch.rand(len(lens), 2, max(lens), generator=torch.Generator().manual_seed(2)).to(DEV)
+        pos = torch.arange(max(lens), dtype=torch.int32, device=DEV).expand(len(lens), 2, max(lens)).contiguous()
+        for kv in (c.kv, small):
+            src, out = torch.zeros(len(lens), 2, 40, dtype=torch.int32, device=DEV), torch.zeros(len(lens), 2, 40, device=DEV)
+            contexts[dtype].evict_cache(kv, mass, pos, 40, torch.zeros_like(c.kv.d_lens), src, out, torch.zeros_like(src), recent=3)
+        torch.cuda.synchronize()
+        for a, b in ((c.k, small.d_k), (c.v, small.d_v)):
+            assert torch.equal(torch.nan_to_num(a.float()), torch.nan_to_num(b.float()))
+        assert contexts[dtype].device_status() == 0
+        del c, small, pools, pool
+        torch.cuda.empty_cache()
