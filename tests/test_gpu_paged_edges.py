@@ -214,3 +214,154 @@ def test_a_pool_beyond_32_bit_offsets(contexts, dtype, dh):  # noqa: F811
         assert contexts[dtype].device_status() == 0
         del c, small, pools, pool
         torch.cuda.empty_cache()
+
+
+def evict_src(mass, pos, budget, sinks, recent):
+    """oracle.paged.evict for long caches: the slot each kept slot's row comes from."""
+    n = len(mass)
+    if n <= budget:
+        return np.arange(n)
+    safe, nan = (pos < sinks) | (pos > int(pos.max()) - recent), np.isnan(mass)
+    kept = np.sort(np.lexsort((np.arange(n), np.where(nan, 0.0, -mass), nan, ~safe))[:budget])
+    src = np.arange(budget)
+    holes = np.ones(budget, dtype=bool)
+    holes[kept[kept < budget]] = False
+    src[holes] = kept[kept >= budget]
+    return src
+
+
+def test_the_long_reference_is_the_oracle():
+    rng = np.random.default_rng(3)
+    for n, budget, sinks, recent in ((40, 17, 2, 5), (9, 9, 0, 0), (300, 20, 8, 12), (64, 63, 0, 0)):
+        mass = np.round(rng.exponential(size=n) * 4) / 4
+        mass[rng.random(n) < 0.1] = np.nan
+        pos = rng.permutation(n) if n % 2 else np.zeros(n, dtype=int)
+        assert evict_src(mass, pos, budget, sinks, recent).tolist() == paged.evict(mass, pos, budget, sinks, recent)
+
+
+# (lengths, budget, sinks, recent, slots of the arrays): counts of caches and slots at which the CTAs of a cache, their threads and
+# the slots in registers change; the longest arrays, with as many moved slots as there can be
+EVICT = [([4000, 70, 2500] * 27, 900, 4, 60, 4001), ([8192, 8191, 30] * 16, 2000, 0, 0, 8192), ([2049, 5000] * 10, 2048, 3, 9, 6001),
+         ([9000, 10, 16384] * 27, 41, 4, 20, 16384), ([12000, 300] * 20, 5000, 16, 100, 12001), ([131072, 9], 60000, 4, 100, 131072),
+         ([131073, 500], 65536, 4, 1000, 131073), ([200001], 1, 0, 1, 262147), ([1 << 19], 1 << 18, 16, 5000, 1 << 19),
+         ([(1 << 19) - 3, 1 << 19], (1 << 19) - 4, 0, 0, 1 << 19)]
+
+
+@pytest.mark.parametrize("case", EVICT, ids=lambda c: f"{len(c[0])}x{max(c[0])}to{c[1]}")
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_over_the_range_of_sizes(contexts, case, in_place):  # noqa: F811
+    lens, budget, sinks, recent, slots = case
+    rng = np.random.default_rng(slots)
+    n, shape = len(lens), (len(lens), 1, slots)
+    pages = [-(-x // 16) for x in lens]
+    table = np.full((n, max(pages) + 1), -1, dtype=np.int32)
+    order, at = rng.permutation(sum(pages)).astype(np.int32), 0
+    for s, p in enumerate(pages):
+        table[s, :p], at = order[at:at + p], at + p
+    g = torch.Generator(device=DEV)
+    g.manual_seed(slots)
+    k = torch.randn(1, sum(pages), 16, 64, generator=g, device=DEV).bfloat16()
+    v = torch.randn(1, sum(pages), 16, 64, generator=g, device=DEV).bfloat16()
+    d_lens = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    kv = rpo.PagedKV(k, v, torch.from_numpy(table).to(DEV), d_lens)
+    mass = (np.round(rng.exponential(size=shape) * 8) / 8).astype(np.float32)                         # many ties
+    mass[rng.random(shape) < 0.02] = np.nan
+    mass[rng.random(shape) < 0.02] = -0.0
+    mass[rng.random(shape) < 0.01] = np.inf
+    # the heavy ones lie at the end: every hole below the budget is filled from behind it
+    mass[:, :, slots // 2:] += 100.0
+    pos = np.stack([rng.permutation(slots) for _ in lens])[:, None].astype(np.int32)
+    if len(lens) % 2:
+        pos[:] = np.arange(slots)
+    d_mass, d_pos = torch.from_numpy(mass).to(DEV), torch.from_numpy(pos).to(DEV)
+    k0, v0 = k.clone(), v.clone()
+    src = torch.full((n, 1, budget), -9, dtype=torch.int32, device=DEV)
+    lens_out = d_lens if in_place else torch.full_like(d_lens, -5)
+    mass_out = d_mass if in_place else torch.full((n, 1, budget + 3), 7.0, device=DEV)
+    pos_out = d_pos if in_place else torch.full((n, 1, budget + 3), -7, dtype=torch.int32, device=DEV)
+    contexts["bf16"].evict_cache(kv, d_mass, d_pos, budget, lens_out, src, mass_out, pos_out, sinks=sinks, recent=recent)
+    torch.cuda.synchronize()
+    got_src, got_mass, got_pos = src.cpu().numpy(), mass_out.cpu().numpy(), pos_out.cpu().numpy()
+    assert lens_out.tolist() == [min(x, budget) for x in lens]
+    want_k, want_v = k0.clone().view(-1, 64), v0.clone().view(-1, 64)
+    for s, x in enumerate(lens):
+        want = evict_src(mass[s, 0, :x], pos[s, 0, :x], budget, sinks, recent)
+        m = len(want)
+        assert np.array_equal(got_src[s, 0, :m], want) and np.all(got_src[s, 0, m:] == -1)
+        assert np.array_equal(got_mass[s, 0, :m], mass[s, 0, want], equal_nan=True) and np.array_equal(got_pos[s, 0, :m], pos[s, 0, want])
+        assert np.array_equal(got_mass[s, 0, m:], mass[s, 0, m:], equal_nan=True) if in_place else np.all(got_mass[s, 0, m:] == 7.0)
+        assert np.array_equal(got_pos[s, 0, m:], pos[s, 0, m:]) if in_place else np.all(got_pos[s, 0, m:] == -7)
+        to = np.nonzero(want != np.arange(m))[0]
+        row = lambda i: torch.from_numpy(table[s, i // 16].astype(np.int64) * 16 + i % 16).to(DEV)  # noqa: E731
+        want_k[row(to)], want_v[row(to)] = k0.view(-1, 64)[row(want[to])], v0.view(-1, 64)[row(want[to])]
+    assert torch.equal(k.view(-1, 64), want_k) and torch.equal(v.view(-1, 64), want_v)
+    assert contexts["bf16"].device_status() == 0
+
+
+def test_evict_refuses_longer_arrays(contexts):  # noqa: F811
+    kv = rpo.PagedKV(torch.zeros(1, 2, 16, 64, device=DEV), torch.zeros(1, 2, 16, 64, device=DEV), torch.zeros(1, 2, dtype=torch.int32, device=DEV),
+                     torch.full((1,), 20, dtype=torch.int32, device=DEV))
+    mass, pos = torch.zeros(1, 1, (1 << 19) + 1, device=DEV), torch.zeros(1, 1, (1 << 19) + 1, dtype=torch.int32, device=DEV)
+    src, n = torch.zeros(1, 1, 8, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    with pytest.raises(rpo.RpoError) as e:
+        contexts["fp32"].evict_cache(kv, mass, pos, 8, n, src, mass, pos)
+    assert e.value.code == -7
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [([1, 1, 1], [50, 60, 40]), ([4, 3, 2], [50, 60, 40]), ([20, 30, 10], [50, 60, 40])], ids=["steps", "few", "chunks"])
+@pytest.mark.parametrize("what", ["block", "length", "negative length", "offset", "backward offsets", "chunk"])
+def test_a_bad_sequence_is_reported_and_leaves_its_neighbours_alone(contexts, dtype, rows, what):  # noqa: F811
+    ctx = contexts[dtype]
+    c = Case(dtype, 8, 2, 64, *rows, seed=12, bad=0.0)
+    good, good_lse = c.attend(ctx, append=True)
+    slots = 128                                                            # more than the table can name: nothing is cut there
+    start = torch.rand(3, 2, slots, device=DEV)
+    good_mass = start.clone()
+    ctx.attention_mass(c.q, c.kv, c.d_off, c.max_chunk, good_lse, good_mass, d_mass_in=good_mass)
+    assert ctx.device_status() == 0
+    k0 = c.k.clone()
+    if what == "block":
+        c.kv.d_block_table[1, 1] = c.k.shape[1] + 1000
+        c.kv.d_block_table[1, 2] = -77
+    elif what == "length":
+        c.kv.d_lens[1] = 1 << 30
+    elif what == "negative length":
+        c.kv.d_lens[1] = -3
+    elif what == "offset":
+        c.d_off[3] = 1 << 29
+    elif what == "backward offsets":
+        c.d_off[1:3] = torch.tensor([rows[0][0] + 1, rows[0][0]], dtype=torch.int32)
+    elif c.max_chunk == 1:
+        return
+    else:
+        c.max_chunk = max(rows[0]) - 1
+    bit = 4 if what == "block" else 8
+    out, lse = c.attend(ctx, append=what not in ("length", "backward offsets"))
+    assert ctx.device_status() & bit
+    mass = start.clone()
+    ctx.attention_mass(c.q, c.kv, c.d_off, c.max_chunk, good_lse, mass, d_mass_in=mass)
+    assert ctx.device_status() & bit
+    torch.cuda.synchronize()
+    # the neighbours.  Where the lengths stay, so does the division of the work: bit for bit.  Elsewhere pieces may end at
+    # other pages, and both results lie within the tolerances of the definition
+    want, want_lse = paged.chunk_attention(c.np(c.q), c.np(k0), np.nan_to_num(c.np(c.v)), c.table, c.lens, c.off, c.scale)
+    ew, el, a = c.errors()
+    tol = a * (2 * ew + 3 * max(c.lens) * U)[..., None] + torch.finfo(c.dtype).eps / 2 * np.abs(want) + (2.0 ** -8 * a if dtype == "bf16" else 0)
+    for s in (0, 2):
+        if (what, s) in (("backward offsets", 0), ("backward offsets", 2)) or (what == "chunk" and rows[0][s] > c.max_chunk):
+            continue                                                       # its own rows are others now
+        r = slice(c.off[s], c.off[s + 1])
+        if what in ("block", "offset"):
+            assert torch.equal(out[r], good[r]) and torch.equal(lse[r], good_lse[r]) and torch.equal(mass[s], good_mass[s])
+        assert np.all(np.abs(c.np(out)[r] - want[r]) <= tol[r]) and np.all(np.abs(c.np(lse)[r] - want_lse[r]) <= el[r])
+        m, n = c.np(mass)[s], c.lens[s]
+        # both sums are off by the weights' errors and their own roundings
+        terms = rows[0][s] * 4
+        rel = ew.max() + U * np.abs(want_lse).max() + 2.0 ** -20 + (terms + 2) * U
+        assert np.all(np.abs(m - c.np(good_mass)[s])[:, :n] <= 2 * rel * m[:, :n]) and np.array_equal(m[:, n:], c.np(start)[s][:, n:])
+    # nothing of the other sequences' keys was written
+    for s in (0, 2):
+        mine = torch.from_numpy(c.table[s, :-(-c.lens[s] // 16)].astype(np.int64)).to(DEV)
+        if what not in ("chunk",):
+            assert torch.equal(c.k[:, mine], k0[:, mine])
