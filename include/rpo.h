@@ -340,7 +340,8 @@ int rpo_attention_mass(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, int
  *   d_mass       float [n_seqs][n_kv_heads][mass_stride]
  *   d_positions  int32, same shape: position of the token in every slot (attention after an eviction
  *                no longer has slot = position; the caller fills in the slots it appends)
- *   d_lens_out   [n_seqs] min(len, budget); may be kv->d_lens
+ *   d_lens_out   [n_seqs] min(len, budget); may be kv->d_lens.  Where the layers of a model share one array of
+ *                lengths, only the last layer's call may write it: the others still have to read the old ones
  *   d_src_out    int32 [n_seqs][n_kv_heads][budget]: the slot each kept slot's row came from; -1 behind
  *                the last.  Kept slots below budget stay; the i-th kept slot at or above it moves to the
  *                i-th free one below (K, V, weight and position; the order of cached keys is free)

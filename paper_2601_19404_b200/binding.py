@@ -390,7 +390,7 @@ class Context:
     def evict_cache(self, kv, d_mass, d_positions, budget, d_lens_out, d_src_out, d_mass_out, d_positions_out, sinks=0, recent=0):
         """rpo_evict_cache: d_mass float32 and d_positions int32 [n_seqs, n_kv_heads, slots], d_src_out int32 [n_seqs, n_kv_heads,
         budget], d_mass_out / d_positions_out of at least budget slots (or d_mass / d_positions themselves), d_lens_out int32
-        [n_seqs] (or the cache's own d_lens)."""
+        [n_seqs] (or the cache's own d_lens; of layers that share one, in the last layer's call only)."""
         self._paged_dtype(kv)
         n, h = kv.struct.n_seqs, kv.struct.n_kv_heads
         slots, out_slots = d_mass.shape[-1], d_mass_out.shape[-1]

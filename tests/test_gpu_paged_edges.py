@@ -365,3 +365,23 @@ def test_a_bad_sequence_is_reported_and_leaves_its_neighbours_alone(contexts, dt
         mine = torch.from_numpy(c.table[s, :-(-c.lens[s] // 16)].astype(np.int64)).to(DEV)
         if what not in ("chunk",):
             assert torch.equal(c.k[:, mine], k0[:, mine])
+
+
+def test_layers_that_share_their_lengths(contexts):  # noqa: F811
+    """Every layer evicts from the same lengths; the last call writes them in place."""
+    lens, budget, n = torch.tensor([50, 20, 33], dtype=torch.int32, device=DEV), 24, 3
+    table = torch.arange(12, dtype=torch.int32, device=DEV).reshape(3, 4)
+    pos = torch.arange(64, dtype=torch.int32, device=DEV).expand(n, 2, 64).contiguous()
+    scratch = torch.zeros_like(lens)
+    for layer in range(3):
+        k = torch.randn(2, 12, 16, 64, generator=torch.Generator().manual_seed(layer)).bfloat16().to(DEV)
+        kv = rpo.PagedKV(k, k.clone(), table, lens)
+        mass = torch.rand(n, 2, 64, generator=torch.Generator().manual_seed(layer)).to(DEV)
+        src, out = torch.zeros(n, 2, budget, dtype=torch.int32, device=DEV), torch.zeros(n, 2, budget, device=DEV)
+        contexts["bf16"].evict_cache(kv, mass, pos, budget, lens if layer == 2 else scratch, src, out, torch.zeros_like(src), sinks=2, recent=4)
+        torch.cuda.synchronize()
+        for s, m in enumerate((50, 20, 33)):
+            for h in range(2):
+                want = paged.evict(mass[s, h, :m].tolist(), list(range(m)), budget, 2, 4)
+                assert src[s, h, :len(want)].tolist() == want
+    assert lens.tolist() == [24, 20, 24] and contexts["bf16"].device_status() == 0
