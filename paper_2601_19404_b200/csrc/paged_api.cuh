@@ -63,16 +63,16 @@ static SplitWs split_ws(rpo_ctx* c, int rows_cap) {
 }
 
 // Few rows per sequence (decode steps): one CTA pair per SM over an equal share of all pages.
-template <int DH, int MT>
+template <int DH>
 static int chunk_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const bf16* k_new, const bf16* v_new,
                        int64_t new_stride, float scale, bf16* out, float* lse) {
-  using Cfg = StepCfg<DH, MT>;
-  CUDA_TRY((allow_smem<paged_step_kernel<DH, MT>>(c, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4)));
+  using Cfg = StepCfg<DH>;
+  CUDA_TRY((allow_smem<paged_step_kernel<DH>>(c, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4)));
   const int grid = 2 * c->sm_count;
   StepArgs s;
   s.kv = view; s.c = a; s.q = q; s.q_stride = q_stride; s.k_new = k_new; s.v_new = v_new; s.new_stride = new_stride; s.scale_log2 = scale * 1.4426950408889634f;
   s.o.out = out; s.o.lse = lse; s.o.hq = a.hq; s.o.rep = a.hq / view.hkv; s.ws = split_ws(c, Cfg::ROWS); s.min_share = 4;
-  LAUNCH_OP(c, (paged_step_kernel<DH, MT>), grid, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, s);
+  LAUNCH_OP(c, (paged_step_kernel<DH>), grid, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, s);
   LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(grid, std::min(a.max_chunk * s.o.rep, Cfg::ROWS)), MERGE_WARPS * 32, 0, s.ws, s.o);
   return RPO_OK;
 }
@@ -158,10 +158,11 @@ static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs
                              const void* v_new, int64_t new_stride, float scale, void* out, float* lse) {
   const PagedView<T> view = paged_view<T>(c, kv);
   const int64_t rows = a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads);           // of the longest chunk, per KV head
+  // Up to 16 rows have kernels of one 16-row tile.  16 bits: measured on both sides in paged_step.cuh.  32 bits, 32 sequences of
+  // 1024 .. 4096, 12 on 2 heads of 128: 1 token 154 us (in 64-row tiles 227), 2 tokens 156 (233), 3 tokens 236 in 64-row tiles.
   if constexpr (std::is_same<T, bf16>::value) {
-    if (rows <= 32)
-      return rows <= 16 ? chunk_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse)
-                        : chunk_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
+    if (rows <= StepCfg<DH>::ROWS)
+      return chunk_steps<DH>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
     return chunk_tiles<DH>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
   } else {
     if (rows <= 16) return chunk_f32<DH, 16>(c, view, a, (const float*)q, q_stride, (const float*)k_new, (const float*)v_new, new_stride, scale, (float*)out, lse);
@@ -239,6 +240,9 @@ static int attention_mass_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs&
                             const float* in, float* out, int stride) {
   const PagedView<T> view = paged_view<T>(c, kv);
   const int64_t rows = a.n_rows == 0 ? 0 : a.max_chunk * (int64_t)(a.hq / kv->n_kv_heads);
+  // 16 bits, 128 sequences of 1024 .. 6144, 28 on 4 heads of 128: 1 token 104 us, 4 tokens (two 16-row tiles) 162, in the tiled
+  // kernel 240 either way; 5 tokens there 242; 4 sequences of 100 .. 300, 12 on 2 heads: 12 us against 31.  32 bits, 32 sequences of
+  // 1024 .. 4096, 12 on 2 heads of 128: 1 token 80 us (in 64-row tiles 137), 3 tokens 141 in 64-row tiles.
   if constexpr (std::is_same<T, bf16>::value) {
     if (rows <= 16) return mass_steps<DH, 1>(c, view, a, (const bf16*)q, q_stride, lse, scale, in, out, stride);
     if (rows <= 32) return mass_steps<DH, 2>(c, view, a, (const bf16*)q, q_stride, lse, scale, in, out, stride);

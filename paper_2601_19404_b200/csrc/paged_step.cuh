@@ -1,5 +1,7 @@
 // Attention of few rows per sequence over a caller-owned paged cache (16-bit storage): decode steps, and chunks whose
-// rows x query heads of a KV head fit MT 16-row tensor-core tiles.
+// rows x query heads of a KV head fit one 16-row tensor-core tile.  (Two tiles, up to 32 rows, were slower than the tiled
+// kernel of paged_chunk.cuh: 128 x 4 tokens on 1024 .. 6144, 28 on 4 heads of 128, 285 us against 207; 4 x 5 on 100 .. 300, 12 on
+// 2 heads, 37 against 29.  With one tile it is the other way: 128 x 1 184 against 205, 4 x 1 22.5 against 29.)
 //
 // Bound by HBM: K and V of every visible page are read once per (sequence, KV head), all query heads of the group at
 // once.  All pages of all (sequence, KV head) items form one list; every CTA takes an equal piece of it, whatever the
@@ -197,13 +199,13 @@ __device__ __forceinline__ int page_list_seq(const int* pref, int n_seqs, int f)
   return lo;
 }
 
-template <int DH, int MT>
+template <int DH>
 struct StepCfg {
   static constexpr int WARPS = 4;
   static constexpr int PAGE_BYTES = KV_BLOCK * DH * 2;                 // of K or of V
   static constexpr int STAGES = 3;
   static constexpr int RING = WARPS * STAGES * 2 * PAGE_BYTES;
-  static constexpr int ROWS = 16 * MT;
+  static constexpr int ROWS = 16;
   static constexpr int XO = DH + 4;                                    // floats per row of a warp's result in shared memory
   static constexpr int XCH = WARPS * ROWS * (XO + 2) * 4;
   static constexpr int SMEM = (RING > XCH ? RING : XCH);               // + (n_seqs + 1) ints
@@ -217,9 +219,9 @@ struct StepArgs {
   int min_share;
 };
 
-template <int DH, int MT>
+template <int DH>
 __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
-  using Cfg = StepCfg<DH, MT>;
+  using Cfg = StepCfg<DH>;
   constexpr int ROWS = Cfg::ROWS, STAGES = Cfg::STAGES, PB = Cfg::PAGE_BYTES, KS = DH / 16, NT = DH / 8, CPR = DH / 8;
   extern __shared__ __align__(128) uint8_t st_smem[];
   int* s_pref = reinterpret_cast<int*>(st_smem + Cfg::SMEM);          // pages of all items of the sequences before s
@@ -253,30 +255,24 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
     const int32_t* tbl = a.kv.table + (int64_t)s * a.kv.table_stride;
 
     // ---- queries as A fragments: rows g, g + 8 of every 16
-    uint32_t qf[MT][KS][4];
-    int prow[MT][2];
+    uint32_t qf[KS][4];
+    int prow[2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int hh = 0; hh < 2; ++hh) {
+      const int r = hh * 8 + g;
+      const bool v = r < R;
+      prow[hh] = v ? p0 + r / rep : p1;
+      const uint32_t* qp = reinterpret_cast<const uint32_t*>(a.q + (int64_t)(sp.row0 + (v ? r / rep : 0)) * a.q_stride + (h * rep + (v ? r % rep : 0)) * DH) + tq;
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        const int r = mt * 16 + hh * 8 + g;
-        const bool v = r < R;
-        prow[mt][hh] = v ? p0 + r / rep : p1;
-        const uint32_t* qp = reinterpret_cast<const uint32_t*>(a.q + (int64_t)(sp.row0 + (v ? r / rep : 0)) * a.q_stride + (h * rep + (v ? r % rep : 0)) * DH) + tq;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          qf[mt][k][hh] = v ? qp[k * 8] : 0u;
-          qf[mt][k][hh + 2] = v ? qp[k * 8 + 4] : 0u;
-        }
+      for (int k = 0; k < KS; ++k) {
+        qf[k][hh] = v ? qp[k * 8] : 0u;
+        qf[k][hh + 2] = v ? qp[k * 8 + 4] : 0u;
       }
-
-    float o[MT][NT][4], m[MT][2], l[MT][2];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      m[mt][0] = m[mt][1] = -INFINITY; l[mt][0] = l[mt][1] = 0.f;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
     }
+
+    float o[NT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < NT; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
     const int n_mine = (i1 - i0 - warp + 3) / 4;                       // pages i0 + warp, i0 + warp + 4, ...
     int ids = 0;                                                       // lane t: block of my page 32 b + t
     auto fetch_ids = [&](int base) {
@@ -327,55 +323,51 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
       fa::cp_wait<STAGES - 1>();
       __syncwarp();
       const uint32_t sk = ring + (it % STAGES) * (2 * PB), sv = sk + PB;
-      float sc[MT][2][4];
+      float sc[2][4];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int n = 0; n < 2; ++n) sc[mt][n][0] = sc[mt][n][1] = sc[mt][n][2] = sc[mt][n][3] = 0.f;
+      for (int n = 0; n < 2; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         uint32_t b0, b1, b2, b3;
         fa::ldsm_x4(sk + sw(((lane >> 4) << 3) + (lane & 7), k * 2 + ((lane >> 3) & 1)), b0, b1, b2, b3);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) { fa::mma_bf16(sc[mt][0], qf[mt][k], b0, b1); fa::mma_bf16(sc[mt][1], qf[mt][k], b2, b3); }
+        fa::mma_bf16(sc[0], qf[k], b0, b1);
+        fa::mma_bf16(sc[1], qf[k], b2, b3);
       }
       const int key0 = kp.page(i0 + warp + 4 * it) * KV_BLOCK;
       const bool whole = key0 + KV_BLOCK - 1 <= p0 && (a.c.window <= 0 || key0 > p1 - a.c.window || key0 + KV_BLOCK <= a.c.sinks);
-      uint32_t pf[MT][4];
+      uint32_t pf[4];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int hh = 0; hh < 2; ++hh) {
+        float x[4] = {sc[0][2 * hh], sc[0][2 * hh + 1], sc[1][2 * hh], sc[1][2 * hh + 1]};
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          float x[4] = {sc[mt][0][2 * hh], sc[mt][0][2 * hh + 1], sc[mt][1][2 * hh], sc[mt][1][2 * hh + 1]};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[e] *= a.scale_log2;
-            if (!whole && !chunk_visible(a.c, key0 + (e >> 1) * 8 + tq * 2 + (e & 1), prow[mt][hh])) x[e] = -INFINITY;
-          }
-          float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-          // the reference maximum moves when it is outgrown; the sums are exact for any reference
-          const float mn = fmaxf(m[mt][hh], mx);
-          if (__any_sync(0xffffffffu, mn > m[mt][hh])) {
-            const float corr = mn == -INFINITY ? 1.f : fa::ex2(m[mt][hh] - mn);
-            l[mt][hh] *= corr;
-            m[mt][hh] = mn;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) { o[mt][n][2 * hh] *= corr; o[mt][n][2 * hh + 1] *= corr; }
-          }
-          const float mu = m[mt][hh] == -INFINITY ? 0.f : m[mt][hh];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { x[e] = fa::ex2(x[e] - mu); l[mt][hh] += x[e]; }
-          pf[mt][hh] = fa::pack_bf16(x[0], x[1]);
-          pf[mt][hh + 2] = fa::pack_bf16(x[2], x[3]);
+        for (int e = 0; e < 4; ++e) {
+          x[e] *= a.scale_log2;
+          if (!whole && !chunk_visible(a.c, key0 + (e >> 1) * 8 + tq * 2 + (e & 1), prow[hh])) x[e] = -INFINITY;
         }
+        float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        // the reference maximum moves when it is outgrown; the sums are exact for any reference
+        const float mn = fmaxf(m[hh], mx);
+        if (__any_sync(0xffffffffu, mn > m[hh])) {
+          const float corr = mn == -INFINITY ? 1.f : fa::ex2(m[hh] - mn);
+          l[hh] *= corr;
+          m[hh] = mn;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) { o[n][2 * hh] *= corr; o[n][2 * hh + 1] *= corr; }
+        }
+        const float mu = m[hh] == -INFINITY ? 0.f : m[hh];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[e] = fa::ex2(x[e] - mu); l[hh] += x[e]; }
+        pf[hh] = fa::pack_bf16(x[0], x[1]);
+        pf[hh + 2] = fa::pack_bf16(x[2], x[3]);
+      }
 #pragma unroll
       for (int n = 0; n < NT; n += 2) {
         uint32_t b0, b1, b2, b3;
         fa::ldsm_x4_t(sv + sw((((lane >> 3) & 1) << 3) + (lane & 7), n + (lane >> 4)), b0, b1, b2, b3);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) { fa::mma_bf16(o[mt][n], pf[mt], b0, b1); fa::mma_bf16(o[mt][n + 1], pf[mt], b2, b3); }
+        fa::mma_bf16(o[n], pf, b0, b1);
+        fa::mma_bf16(o[n + 1], pf, b2, b3);
       }
       __syncwarp();
     }
@@ -384,19 +376,17 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
 
     // ---- join the warps
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int hh = 0; hh < 2; ++hh) {
+      const int r = hh * 8 + g;
+      float ls = l[hh];
+      ls += __shfl_xor_sync(0xffffffffu, ls, 1);
+      ls += __shfl_xor_sync(0xffffffffu, ls, 2);
+      if (tq == 0) x_ml[warp * ROWS + r] = make_float2(m[hh], ls);
+      if (r < R)
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        const int r = mt * 16 + hh * 8 + g;
-        float ls = l[mt][hh];
-        ls += __shfl_xor_sync(0xffffffffu, ls, 1);
-        ls += __shfl_xor_sync(0xffffffffu, ls, 2);
-        if (tq == 0) x_ml[warp * ROWS + r] = make_float2(m[mt][hh], ls);
-        if (r < R)
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            *reinterpret_cast<float2*>(x_o + (warp * ROWS + r) * Cfg::XO + n * 8 + tq * 2) = make_float2(o[mt][n][2 * hh], o[mt][n][2 * hh + 1]);
-      }
+        for (int n = 0; n < NT; ++n)
+          *reinterpret_cast<float2*>(x_o + (warp * ROWS + r) * Cfg::XO + n * 8 + tq * 2) = make_float2(o[n][2 * hh], o[n][2 * hh + 1]);
+    }
     __syncthreads();
     const bool begins = i0 == 0, ends = i1 == n_pages;
     const int slot = begins ? 2 * blockIdx.x + 1 : 2 * blockIdx.x;
