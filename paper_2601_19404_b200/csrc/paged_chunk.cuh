@@ -232,6 +232,28 @@ __device__ __forceinline__ float chunk_exp(uint32_t* v, float scale_log2, float 
   return x0 + x1;
 }
 
+// tc::mbar_wait_warp with the limit counted from the last tile that passed: while items of one sub-tile pass, however long that
+// takes, the second sub-tile's warps already wait for the first S of the next item of two.  (Only there: in every wait
+// for S it cost 1.4 % of a long chunk's time.)
+__device__ __forceinline__ bool chunk_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, const volatile int* passed) {
+  bool ok = tc::mbar_try_wait(bar, parity);
+  if (!ok) {
+    const long long limit = g_wait_limit_cycles;
+    long long t0 = clock64();
+    int seen = *passed;
+    while (!(ok = tc::mbar_try_wait(bar, parity))) {
+      if (*abort_flag) break;
+      if (clock64() - t0 > limit) {
+        const int now = *passed;
+        if (now == seen) { *abort_flag = 1; break; }
+        seen = now;
+        t0 = clock64();
+      }
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
+}
+
 template <int DH>
 __global__ void __launch_bounds__(ChunkCfg<DH>::THREADS, 1)
 paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
@@ -250,6 +272,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
   uint32_t* tmem_slot = (uint32_t*)(v_ready + NSV);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   int* s_first = (int*)(tmem_slot + 2);
+  volatile int* s_passed = (volatile int*)(tmem_slot + 3);   // the last tile without work for the second sub-tile
 
   const int warp = (int)t5::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int hkv = a.kv.hkv, rep = a.o.rep;
@@ -260,7 +283,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     for (int i = 0; i < 4; ++i) { tc::mbar_init(&s_full[i], 1); tc::mbar_init(&p_full[i], 4); }
     for (int i = 0; i < 2; ++i) { tc::mbar_init(&pv_done[i], 1); tc::mbar_init(&o_full[i], 1); }
     tc::mbar_init(q_full, 1); tc::mbar_init(q_free, 2);
-    *abort_flag = 0; *s_first = 0;
+    *abort_flag = 0; *s_first = 0; *s_passed = 0;
     a.ws.rec[blockIdx.x] = SplitRec{0, 0, 0, 0};
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -406,6 +429,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
           if (t5::elect_one()) {
             tc::mbar_arrive(&v_empty[sv]);
             if (more) tc::mbar_arrive(&k_empty[sk]);
+            *s_passed = kt + 1;
           }
           continue;
         }
@@ -437,9 +461,14 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     const bool in_tile = tok < a.tq;
     uint32_t s_phase = 0, o_phase = 0;
     int steps = 0;                                           // halves of this sub-tile so far: phases of pv_done
-    bool ok = true;
-    for (int seg = 0; ok && walk.next(); ++seg) {
-      if (x == 1 && walk.it.n_tok <= a.tq) continue;
+    bool ok = true, skipped = false;
+    while (ok && walk.next()) {
+      if (x == 1 && walk.it.n_tok <= a.tq) { skipped = true; continue; }
+      if (skipped) {
+        ok = chunk_wait_warp(&s_full[2], s_phase, abort_flag, s_passed);     // (x is 1; the first half's S)
+        if (!ok) break;
+        skipped = false;
+      }
       const int p_item = walk.it.p0, p1 = p_item + walk.it.n_tok - 1;
       const KeyTiles<CH_BN / KV_BLOCK> kt_of(a.c, p_item, p1);
       const bool row_valid = in_tile && x * a.tq + tok < walk.it.n_tok;

@@ -385,3 +385,30 @@ def test_layers_that_share_their_lengths(contexts):  # noqa: F811
                 want = paged.evict(mass[s, h, :m].tolist(), list(range(m)), budget, 2, 4)
                 assert src[s, h, :len(want)].tolist() == want
     assert lens.tolist() == [24, 20, 24] and contexts["bf16"].device_status() == 0
+
+
+def test_long_runs_of_single_tokens_before_chunks(contexts):  # noqa: F811
+    """A call of chunks and single tokens: of the two halves of a row tile only the first works on single tokens, for about a
+    millisecond here.  The second one's wait meanwhile does not count against the limit of device-side waits."""
+    ctx, (hq, hkv, dh), keys = contexts["bf16"], (28, 4, 128), 40000
+    new = ([1] * 25 + [100]) * 4
+    g = torch.Generator(device=DEV)
+    g.manual_seed(71)
+    k, v = (torch.randn(hkv, keys // 16, 16, dh, generator=g, device=DEV).bfloat16() for _ in range(2))
+    table = torch.randperm(keys // 16, generator=g, device=DEV).to(torch.int32).expand(len(new), -1).contiguous()     # one cache for all
+    kv = rpo.PagedKV(k, v, table, torch.full((len(new),), keys, dtype=torch.int32, device=DEV))
+    off = torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)).to(DEV)
+    q = torch.randn(sum(new), hq, dh, generator=g, device=DEV).bfloat16()
+    got = []
+    for limit in (0, 500000):                                              # the default; about 0.3 ms
+        ctx.set_option("wait_limit_cycles", limit)
+        try:
+            out, lse = torch.zeros_like(q), torch.zeros(len(q), hq, device=DEV)
+            ctx.chunk_attention(q, kv, off, 100, out, lse)
+            mass = torch.zeros(len(new), hkv, keys, device=DEV)
+            ctx.attention_mass(q, kv, off, 100, lse, mass)
+            assert ctx.device_status() == 0
+            got.append((out, lse, mass))
+        finally:
+            ctx.set_option("wait_limit_cycles", 0)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
