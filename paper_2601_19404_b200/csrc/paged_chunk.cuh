@@ -3,13 +3,15 @@
 //
 // An item is up to 2 tq tokens of one sequence x the rep query heads of one KV head, as two sub-tiles of tq rep <= 128
 // packed rows (token-major); its keys come in tiles of 128.  All key tiles of all items form one list, cut into equal
-// pieces for one persistent CTA per SM (plan kernel); an item cut by a piece border leaves unnormalised parts that
+// pieces for one persistent CTA per SM (chunk_prepare_kernel); an item cut by a piece border leaves unnormalised parts that
 // split_merge_kernel joins.  A tile is worked on in two halves of 64 keys; per half and sub-tile x:
 //
 //   S = Q_x K^T      tcgen05.mma, both operands in shared memory (128-byte swizzle, filled by TMA straight from the
 //                    pages: 16 x 64 boxes), accumulator in tensor memory, one buffer per half
 //   softmax          one warpgroup per sub-tile, one thread per row = TMEM lane: no shuffles, no exchange.  P = 2^(s - m)
-//                    goes back to tensor memory as bf16, over the S it came from
+//                    goes back to tensor memory as bf16, over the S it came from (the matrix instruction wants both
+//                    operands of one type, and V is bf16; a second part of P would be half as much matrix work
+//                    again.  Outputs are 2.3e-3 off 64 bits, of which 1.66e-3 is their own rounding)
 //   O_x += P V       tcgen05.mma with A = P from tensor memory; accumulates over all tiles.  m is a reference, not
 //                    the running maximum.  Halves with masked keys, and all halves until every row of a warp has a
 //                    reference, take the maximum and move m (rescaling the row's O in place) where it grows; later
@@ -23,8 +25,9 @@
 // between sinks and window) are zeroed in shared memory before P V, since 0 x NaN is not 0; scores there are masked by
 // selection.
 //
-// Measured (28 on 4 heads of 128, 4 x 2048 tokens behind 4096): 600 us, 1.0 PFLOP/s.  A half takes about 2000 clocks; both
-// sub-tiles' exponentials need 1024 of them, the matrix products 1282 (Q K^T at N = 64 is bound by shared memory).  A quarter
+// Measured (28 on 4 heads of 128, 4 x 2048 tokens behind 4096): 600 to 620 us on different cards, 1.0 PFLOP/s.  A half takes about
+// 2000 clocks; both sub-tiles' exponentials need 1024 of them, the matrix products 1282 (Q K^T at N = 64 is bound by shared
+// memory); neither alone, nor all of tensor and shared memory in use, lets anything run further ahead.  A quarter
 // of the exponentials as polynomials on the multiply-add pipe made it 5 % slower.
 #pragma once
 #include "attn_tc5.cuh"

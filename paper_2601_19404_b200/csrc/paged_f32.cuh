@@ -4,11 +4,12 @@
 // Same items, pieces and merge as the 16-bit kernels (paged_chunk.cuh).  256 threads as 16 x 16: thread (ty, tx) owns
 // TM = BM / 16 consecutive rows and the keys tx, tx + 16, ... of a tile, then the same rows and 4 (or 2 x 4) output dims.
 // Operands are read from shared memory as float4: per four dims 4 TM multiply-adds for each of its keys against TM + KPT
-// loads, so BM = 64 is bound by the multiply-adds (64 per 4 + 4 loads); BM = 16 serves decode steps, where HBM and the
-// shared-memory loads are the limit.  K and V of the next tile are fetched (cp.async, zero-filled where no row looks)
-// while the other half of this tile is worked on.  Measured: 3 chunks of up to 777 tokens behind up to 1500, window 500, 4 on 2
-// heads of 64: 64 us; a float4 load takes four passes of shared memory whatever it shares, so the loads of a 4 x 4 tile take
-// twice the time of its multiply-adds.
+// loads.  A float4 load takes four passes of shared memory whatever it shares, so the loads bound both variants: with BM = 64
+// (64 multiply-adds per 4 + 4 loads) they take twice the time of the multiply-adds, with BM = 16, which serves decode steps,
+// more.  K and V of the next tile are fetched (cp.async, zero-filled where no row looks) while the other half of this tile
+// is worked on.  Measured: 3 chunks of up to 777 tokens behind up to 1500, window 500, 4 on 2 heads of 64: 64 us (18 % of the
+// nominal multiply-add rate), their attention mass 113; one token for each of 32 sequences of 1024 .. 4096, 12 on 2 heads of 128: 154 us
+// (19 % of a copy's rate), their mass 80.
 #pragma once
 #include "paged_chunk.cuh"
 

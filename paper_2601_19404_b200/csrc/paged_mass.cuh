@@ -17,7 +17,7 @@ struct MassArgs {
 
 // Few rows per sequence (16-bit storage): HBM-bound, K of every page once.  A page's sums need nothing of other pages:
 // every warp takes an equal share of the pages of all (sequence, KV head)s, with a ring of pages of its own.  Measured: one
-// token for each of 128 sequences of 1024 .. 6144 tokens, 4 KV heads of 128: 87 us, 5.6 TB/s.
+// token for each of 128 sequences of 1024 .. 6144 tokens, 4 KV heads of 128: 87 to 89 us, 5.5 TB/s.
 template <int DH, int MT>
 struct MassStepCfg {
   static constexpr int STAGES = 3, PAGE_BYTES = KV_BLOCK * DH * 2;

@@ -11,9 +11,13 @@
 // warps' results are joined through shared memory at the end of an item; an item that runs over several CTAs leaves
 // unnormalised parts, joined in piece order by split_merge_kernel.
 //
-// Measured (28 query on 4 KV heads of 128): one token for each of 128 sequences of 1024 .. 6144 tokens 163 us, 5.75 TB/s, 88 %
-// of a copy's rate; pages fetched as one bulk copy per row 212 us, as TMA boxes 168 us and 3.6 us of host time per tensor map;
-// K and V of the new token written by a kernel of their own 3 us more.
+// Measured (28 query on 4 KV heads of 128): one token for each of 128 sequences of 1024 .. 6144 tokens 164 to 171 us on different
+// cards, 5.5 to 5.7 TB/s, 84 to 88 % of a copy's rate.  Beside 164: pages fetched as one bulk copy per row 212 us, as TMA boxes 168
+// and 3.6 us of host time per tensor map; K and V of the new token written by a kernel of their own 3 us more.
+//
+// Weights are rounded to 16 bits before P V (sums of weights are not), as in the rollout's own attention and in the tiled
+// kernel: against 64 bits the outputs are 1.9e-3 off, of which 1.65e-3 is their own rounding to 16 bits.  With a second 16-bit
+// part of every weight the error is that 1.65e-3 alone, and the call above takes 179 us instead of 170.
 #pragma once
 #include "attn_tc.cuh"
 #include "paged_kv.cuh"
