@@ -412,3 +412,46 @@ def test_long_runs_of_single_tokens_before_chunks(contexts):  # noqa: F811
         finally:
             ctx.set_option("wait_limit_cycles", 0)
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("longest", [2, 64], ids=["steps", "chunks"])
+def test_a_captured_call_follows_offsets_and_lengths(dtype, longest):
+    """One graph, replayed for other chunks: rows before the first sequence and behind the last are left alone."""
+    s = torch.cuda.Stream()
+    with rpo.Context(rpo.shape_preset("tiny", dtype=1 if dtype == "bf16" else 0), kv_pool_blocks=8, max_groups=1, max_seqs=1, max_chunk_tokens=16,
+                     max_positions=32, stream=s) as ctx:
+        c = Case(dtype, 8, 2, 64, [longest] * 4, [300, 90, 1000, 64], seed=81, extra_rows=5, window=200, sinks=2)
+        out, lse = torch.zeros_like(c.q), torch.zeros(c.q.shape[:2], device=DEV)
+        mass = torch.zeros(4, 2, 1000, device=DEV)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            ctx.chunk_attention(c.q, c.kv, c.d_off, longest, out, lse, window=200, sinks=2)
+            ctx.attention_mass(c.q, c.kv, c.d_off, longest, lse, mass, window=200, sinks=2)
+        full = list(c.lens)
+        for first, new, less in ((0, [longest] * 4, 0), (3, [1, 0, longest, 2], 17), (5, [0, 0, 0, 0], 5), (1, [2, longest, 0, 1], 60)):
+            c.new, c.lens = new, [n - less for n in full]
+            c.off = (first + np.concatenate([[0], np.cumsum(new)])).astype(np.int32)
+            c.d_off.copy_(torch.from_numpy(c.off))
+            c.kv.d_lens.copy_(torch.tensor(c.lens, dtype=torch.int32))
+            out.fill_(7.0)
+            lse.fill_(7.0)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(s):
+                graph.replay()
+            torch.cuda.synchronize()
+            assert bool((out[:first] == 7.0).all()) and bool((lse[:first] == 7.0).all())
+            n = int(c.off[-1])
+            want, want_lse = paged.chunk_attention(c.np(c.q), np.nan_to_num(c.np(c.k)), np.nan_to_num(c.np(c.v)), c.table, c.lens, c.off, c.scale, 200, 2)
+            ew, el, a = c.errors()
+            tol = a * (2 * ew + 3 * max(c.lens) * U)[..., None] + torch.finfo(c.dtype).eps / 2 * np.abs(want) + (2.0 ** -8 * a if dtype == "bf16" else 0)
+            assert np.all(np.abs(c.np(out) - want)[first:n] <= tol[first:n] + 1e-30) and np.all(c.np(out)[n:] == 7.0)
+            g, want_lse, empty = c.np(lse), want_lse[first:n], np.isneginf(want_lse[first:n])          # rows before their first token
+            assert np.array_equal(np.isneginf(g[first:n]), empty) and np.all(g[n:] == 7.0)
+            assert np.all(np.abs(g[first:n][~empty] - want_lse[~empty]) <= el[first:n][~empty])
+            total = c.np(mass)
+            for i in range(4):
+                assert np.allclose(total[i, :, :c.lens[i]].sum(1), min(new[i], c.lens[i]) * 4, rtol=1e-4, atol=1e-30)
+        assert ctx.device_status() == 0
+        del graph
