@@ -355,6 +355,113 @@ int rpo_evict_cache(rpo_ctx* ctx, const rpo_paged_kv* kv, const float* d_mass, c
                     int32_t mass_stride, int32_t budget, int32_t sinks, int32_t recent, int32_t* d_lens_out,
                     int32_t* d_src_out, float* d_mass_out, int32_t* d_positions_out, int32_t out_stride);
 
+/* ---------------------------------------------------------------------------------------------
+ * Drafted tokens and shared pages on a cache that the caller owns
+ *
+ * A step of a rollout with drafted tokens (of a draft model, or looked up in a cached response): room for the
+ * drafts (rpo_reserve_pages), attention of the tree they form (rpo_tree_attention, per layer), which of them
+ * the target accepts and the token behind them (rpo_verify_drafts), and their K and V in place
+ * (rpo_commit_path).  A rollout's G samples begin as the first tokens of one sequence
+ * (rpo_fork_pages).  (The paper has no counterpart.)  Streams, workspaces, capture and checks on the device
+ * are as for the operators above: enqueued on the context's stream, nothing allocated or synchronised,
+ * the same call gives the same bits, calls on one context must not overlap.
+ *
+ * A tree is a list of nodes: rows [d_offsets[s], d_offsets[s+1]) of sequence s, node i of it naming its parent
+ * among the nodes before it, d_parents[row] < i.  -1: the node follows the last cached token.  -2: there is no
+ * node in this row (padding); neither is there where the chain of parents ends in one.  Any other number is
+ * taken for -2 and sets bit 3 of the status word. */
+
+/* Attention of a tree of drafted tokens per sequence over the paged cache.  Node i of n lies in slot len - n + i
+ * and sits at position p = len - n + depth (0 for a child of the last cached token).  It sees the len - n cached
+ * tokens j, of the tree its ancestors and itself; with window > 0 only what sits at positions > p - window or
+ * < sinks.  Otherwise as rpo_chunk_attention; a row without a node becomes 0 (log-sum -inf), its K and V are
+ * not written and what its slot holds is not used.  A chain is a chunk: the same results, up to rounding.
+ * Errors as there; RPO_ERR_LIMIT also for max_nodes > 256 or n_rows > 2^17. */
+int rpo_tree_attention(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_nodes,
+                       const void* d_q, int64_t q_stride, const void* d_k_new, const void* d_v_new,
+                       int64_t kv_new_stride, const int32_t* d_q_offsets, const int32_t* d_parents,
+                       const rpo_chunk_cfg* cfg, void* d_out, float* d_lse_out);
+
+/* Which drafted tokens the target accepts, from given random numbers, and the token behind them.  Node 0 of a
+ * sequence is accepted already (the last emitted token).  The walk starts there; at a node with the sampler's kept
+ * weights a_i (w_i >= tau of rpo_sample_rows; greedy: 1 at the lowest arg max) of mass A = sum a_i it tests the
+ * node's children in order of their rows, child with token x and random number u:
+ *   d_i = floor(q_i A), one product in double precision, with the draft's probabilities q for the node's children;
+ *         without d_draft_probs: A for i = x, else 0
+ *   accepted when (d_x floor(2^24 u)) >> 24 < a_x: the walk goes on at the child
+ *   refused: a_i <- max(a_i - d_i, 0) and A <- sum a_i (unless that is 0: then both stay); next child
+ * Where no child is left, the next token is the first i whose running sum of a exceeds (A floor(2^24 u_0)) >> 24, u_0 the
+ * number of node 0.  With independent u, and the children of a node drawn from q independently (or given beforehand:
+ * no d_draft_probs, distinct children are then tested against what is left of a), every emitted token is distributed
+ * as rpo_sample_rows draws it.  Only rows of accepted nodes are read.
+ *   d_logits       float [n_rows][vocab], rows logits_stride elements apart: the target's logits behind every node.
+ *                  NaN and +inf count as -inf (excluded)
+ *   d_draft_probs  NULL or float [n_rows][vocab], probs_stride apart; no numbers or negative ones count as 0
+ *   d_tokens, d_parents  int32 [n_rows]; d_offsets int32 [n_seqs + 1]; d_uniform float [n_rows] in [0, 1)
+ *   sampler        temperature, top_p, greedy, eos_id (the walk ends at an accepted eos_id, no token follows); the seed
+ *                  plays no part
+ *   d_path_out     int32 [n_seqs][max_path]: accepted nodes, node 0 first, -1 behind.  At the last one that fits no
+ *                  child is tested
+ *   d_n_path_out   int32 [n_seqs]; 0 for a sequence without rows
+ *   d_next_out     int32 [n_seqs]: the token behind the last accepted node; -1 where that is eos_id, its row excludes
+ *                  every token, or there are no rows
+ *   d_logprobs_out NULL or float [n_seqs][max_path]: log-probability (full vocabulary, at the temperature) of the token
+ *                  behind d_path_out's node: the next node's, or d_next_out; -inf where its row excludes every token,
+ *                  0 where none follows
+ * A token outside the vocabulary is refused and sets bit 1 of the status word, bad offsets set bit 3.
+ * Errors: RPO_ERR_INVALID_ARG, RPO_ERR_LIMIT (vocab >= 2^18). */
+int rpo_verify_drafts(rpo_ctx* ctx, int32_t n_seqs, int32_t n_rows, int32_t vocab, const float* d_logits,
+                      int64_t logits_stride, const float* d_draft_probs, int64_t probs_stride, const int32_t* d_tokens,
+                      const int32_t* d_parents, const int32_t* d_offsets, const float* d_uniform,
+                      const rpo_sampler* sampler, int32_t max_path, int32_t* d_path_out, int32_t* d_n_path_out,
+                      int32_t* d_next_out, float* d_logprobs_out);
+
+/* The accepted nodes' K and V, in all layers, to the front of the tree's slots: with n nodes in the last n of len slots,
+ * slot len - n + path[i] moves to slot len - n + i for i < n_path, and the length becomes len - n + n_path.
+ *   h_layers     host array of the layers' caches: equal pool sizes, heads, tables and lengths (the same pointers)
+ *   d_q_offsets  int32 [n_seqs + 1] as in the attention call (differences count)
+ *   d_path       int32 [n_seqs][path_stride], ascending, d_n_path int32 [n_seqs] <= path_stride: as rpo_verify_drafts wrote them
+ *   d_lens_out   int32 [n_seqs]; may be the caches' own d_lens
+ * The pages of the moved slots must belong to one sequence only.  A path that is not ascending or leaves the tree
+ * leaves its sequence alone (its length too) and sets bit 3.  Errors: RPO_ERR_INVALID_ARG, RPO_ERR_SHAPE, RPO_ERR_LIMIT (more
+ * than 128 layers or 4096 sequences). */
+int rpo_commit_path(rpo_ctx* ctx, const rpo_paged_kv* h_layers, int32_t n_layers, const int32_t* d_q_offsets,
+                    const int32_t* d_path, int32_t path_stride, const int32_t* d_n_path, int32_t* d_lens_out);
+
+/* Pages under reference counts.  Every page of the pool is held by d_refs[page] table entries; those without any
+ * lie on the stack d_free[0 .. *d_n_free).  At first: counts 0, all pages on the stack, nothing held. */
+typedef struct rpo_page_pool {
+  int32_t* d_refs;         /* [n_blocks]                                                                 */
+  int32_t* d_free;         /* [n_blocks]: free pages; what lies at and above *d_n_free means nothing     */
+  int32_t* d_n_free;       /* [1]                                                                        */
+  int32_t* d_block_table;  /* [n_seqs][table_stride]: the table of the caches (the same pointer)         */
+  int32_t* d_held;         /* [n_seqs]: a sequence holds the first d_held entries of its row             */
+  int32_t n_blocks, n_seqs, table_stride;
+} rpo_page_pool;
+
+/* Both calls take the pages that they need from the end of the stack, in order of fork or sequence and of its pages:
+ * the k-th is d_free[n_free - 1 - k].  Forks or sequences are served in order as long as the pages that were free before
+ * the call last; those behind that need any are left as they were, and bit 4 of the status word is set.  Pages
+ * that nobody holds any more are pushed in the order in which forks or sequences (and their pages) first gave them up.
+ * They serve from the next call on. */
+
+/* Sequence d_dst[i] becomes the first d_fork_lens[i] tokens of sequence d_src[i]: whole pages are shared, the tokens
+ * of a last, partial one are copied, in all layers, to a page of its own; what the destination held is given up.
+ * d_lens_out (NULL, or the caches' d_lens, say) receives the length at d_dst[i].  No sequence may be the destination of two
+ * forks, or destination and source: the later fork, or the one that reads it, is left out and sets bit 3, as are
+ * numbers out of range and lengths that the source does not hold.  To cut a sequence short in place, reserve.
+ * Errors: RPO_ERR_INVALID_ARG, RPO_ERR_SHAPE, RPO_ERR_LIMIT (4096 forks or sequences, 128 layers, forks x table_stride >= 2^29). */
+int rpo_fork_pages(rpo_ctx* ctx, const rpo_page_pool* pool, const rpo_paged_kv* h_layers, int32_t n_layers,
+                   int32_t n_forks, const int32_t* d_src, const int32_t* d_dst, const int32_t* d_fork_lens,
+                   int32_t* d_lens_out);
+
+/* Every sequence holds the pages of d_target_lens[s] tokens afterwards, more or fewer than before (0: none).  Its first
+ * min(d_lens[s], d_target_lens[s]) tokens stay; pages that hold tokens behind those are its own: one that others hold too
+ * is replaced, the tokens that stay in it copied in all layers.  Neither d_lens nor the caches' lengths are written.
+ * d_lens beyond what is held, or numbers out of range, are clamped and set bit 3.  Errors as in rpo_fork_pages. */
+int rpo_reserve_pages(rpo_ctx* ctx, const rpo_page_pool* pool, const rpo_paged_kv* h_layers, int32_t n_layers,
+                      const int32_t* d_lens, const int32_t* d_target_lens);
+
 /* Dense product C[M,N] = A[M,K] * W[N,K]^T through the same GEMM kernel the layers use
  * (storage type of the context; C is float32).  For kernel-level parity tests.
  * impl: 0 = the kernel the context would choose, 1 = plain CUDA-core kernel,
@@ -374,7 +481,7 @@ int rpo_gemm_bench(rpo_ctx* ctx, int32_t M, int32_t N, int32_t K, const void* d_
 /* Device status word, sticky until read: 0 = clean; bit 0 = a bounded wait expired
  * (TMA / MMA pipeline), bit 1 = token id out of range (clamped), bit 2 = block-table
  * index out of range (access skipped), bit 3 = a length or offset given to an operator on a
- * caller-owned cache out of range (clamped).  Synchronises the stream; *out receives the word
+ * caller-owned cache out of range (clamped), bit 4 = not enough free pages (rpo_fork_pages, rpo_reserve_pages).  Synchronises the stream; *out receives the word
  * and the word is cleared.  Returns RPO_ERR_DEVICE_TIMEOUT when bit 0 was set (the results of
  * the work enqueued since the last read are not to be trusted; the context stays usable),
  * else RPO_OK.  The asynchronous entry points (prefill, decode, token log-probs) cannot

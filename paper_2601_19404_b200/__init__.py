@@ -5,4 +5,4 @@ exposes the same calls as `include/rpo.h`; it only marshals arguments.  There is
 CPU path: importing works anywhere, computing needs a CUDA device.
 """
 from .binding import (Context, Sampler, Group, ObjectiveCfg, shape_preset, load_library, RpoError, EXPORTED_SYMBOLS,
-                      sample_rows_noalloc, PagedKV)  # noqa: F401
+                      sample_rows_noalloc, PagedKV, PagedLayers, PagePool)  # noqa: F401

@@ -14,7 +14,8 @@ _LIB = None
 EXPORTED_SYMBOLS = [
     "rpo_strerror", "rpo_shape_preset", "rpo_create", "rpo_destroy", "rpo_init_weights", "rpo_read_tensor",
     "rpo_write_tensor", "rpo_prefill_prefix", "rpo_decode_suffix", "rpo_decode_wave", "rpo_token_logprobs", "rpo_release_groups",
-    "rpo_policy_objective", "rpo_rollout_host", "rpo_sample_rows", "rpo_sample_rows_noalloc", "rpo_gemm", "rpo_gemm_bench", "rpo_chunk_attention", "rpo_attention_mass", "rpo_evict_cache", "rpo_device_status", "rpo_debug_tap", "rpo_counters", "rpo_set_option", "rpo_profile_read",
+    "rpo_policy_objective", "rpo_rollout_host", "rpo_sample_rows", "rpo_sample_rows_noalloc", "rpo_gemm", "rpo_gemm_bench", "rpo_chunk_attention", "rpo_attention_mass", "rpo_evict_cache", "rpo_tree_attention", "rpo_verify_drafts",
+    "rpo_commit_path", "rpo_fork_pages", "rpo_reserve_pages", "rpo_device_status", "rpo_debug_tap", "rpo_counters", "rpo_set_option", "rpo_profile_read",
 ]
 
 
@@ -85,6 +86,53 @@ class PagedKV:
         self.ref = C.byref(self.struct)
 
 
+class PagedLayers:
+    """The caches of all layers of a model (PagedKV objects that share their block table and lengths): what calls that move rows
+    or pages work on.  Keeps references; build it once and reuse it."""
+
+    def __init__(self, layers):
+        self.layers = list(layers)
+        if not self.layers:
+            raise ValueError("at least one layer is needed")
+        first = self.layers[0]
+        for kv in self.layers:
+            if (kv.dtype is not first.dtype or kv.device != first.device or kv.d_k.shape != first.d_k.shape
+                    or kv.d_block_table.data_ptr() != first.d_block_table.data_ptr() or kv.d_block_table.shape != first.d_block_table.shape
+                    or kv.d_lens.data_ptr() != first.d_lens.data_ptr()):
+                raise ValueError("the layers must have one type, device and shape, and share d_block_table and d_lens")
+        self.dtype, self.device, self.n_seqs = first.dtype, first.device, first.struct.n_seqs
+        self.array = (_PagedKVStruct * len(self.layers))(*[kv.struct for kv in self.layers])
+
+
+class _PagePoolStruct(C.Structure):
+    _fields_ = [("d_refs", C.c_void_p), ("d_free", C.c_void_p), ("d_n_free", C.c_void_p), ("d_block_table", C.c_void_p), ("d_held", C.c_void_p),
+                ("n_blocks", C.c_int32), ("n_seqs", C.c_int32), ("table_stride", C.c_int32)]
+
+
+class PagePool:
+    """rpo_page_pool: reference counts and free pages in int32 tensors of the caller.
+
+    d_refs, d_free [n_blocks], d_n_free [1], d_block_table [n_seqs, table_stride] (the caches'), d_held [n_seqs]."""
+
+    def __init__(self, d_refs, d_free, d_n_free, d_block_table, d_held):
+        self.device = d_block_table.device
+        for t, name, shape in ((d_refs, "d_refs", d_free.shape[:1]), (d_free, "d_free", d_refs.shape[:1]), (d_n_free, "d_n_free", (1,)),
+                               (d_block_table, "d_block_table", (d_held.shape[0], d_block_table.shape[-1])), (d_held, "d_held", (d_block_table.shape[0],))):
+            _expect(t, name, "int32", shape, self.device)
+        self.d_refs, self.d_free, self.d_n_free, self.d_block_table, self.d_held = d_refs, d_free, d_n_free, d_block_table, d_held
+        self.struct = _PagePoolStruct(_ptr(d_refs), _ptr(d_free), _ptr(d_n_free), _ptr(d_block_table), _ptr(d_held), d_refs.shape[0],
+                                      d_block_table.shape[0], d_block_table.shape[1])
+        self.ref = C.byref(self.struct)
+
+    @classmethod
+    def empty(cls, n_blocks, n_seqs, table_stride, device="cuda"):
+        """A pool of free pages (page 0 on top of the stack), with a table of sequences that hold none."""
+        import torch
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.zeros(n_blocks, **i32), torch.arange(n_blocks - 1, -1, -1, **i32), torch.full((1,), n_blocks, **i32),
+                   torch.full((n_seqs, table_stride), -1, **i32), torch.zeros(n_seqs, **i32))
+
+
 def load_library(path=None):
     """Load librpo.so (building it first if it is missing) and declare the prototypes."""
     global _LIB
@@ -118,6 +166,12 @@ def load_library(path=None):
     lib.rpo_chunk_attention.argtypes = [vp, pkv, i32, i32, i32, vp, i64, vp, vp, i64, vp, ccfg, vp, vp]
     lib.rpo_attention_mass.argtypes = [vp, pkv, i32, i32, i32, vp, i64, vp, ccfg, vp, vp, vp, i32]
     lib.rpo_evict_cache.argtypes = [vp, pkv, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, i32]
+    lib.rpo_tree_attention.argtypes = [vp, pkv, i32, i32, i32, vp, i64, vp, vp, i64, vp, vp, ccfg, vp, vp]
+    lib.rpo_verify_drafts.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, C.POINTER(Sampler), i32, vp, vp, vp, vp]
+    pool = C.POINTER(_PagePoolStruct)
+    lib.rpo_commit_path.argtypes = [vp, pkv, i32, vp, vp, i32, vp, vp]
+    lib.rpo_fork_pages.argtypes = [vp, pool, pkv, i32, i32, vp, vp, vp, vp]
+    lib.rpo_reserve_pages.argtypes = [vp, pool, pkv, i32, vp, vp]
     lib.rpo_device_status.argtypes = [vp, C.POINTER(i32)]
     lib.rpo_debug_tap.argtypes = [vp, vp, i64, C.POINTER(i64)]
     lib.rpo_counters.argtypes = [vp, C.POINTER(i64), C.POINTER(i64)]
@@ -346,9 +400,8 @@ class Context:
     def _chunk_cfg(self, kv, scale, window, sinks):
         return _ChunkCfg(kv.struct.head_dim ** -0.5 if scale is None else scale, window, sinks)
 
-    def chunk_attention(self, d_q, kv, d_q_offsets, max_chunk, d_out, d_lse_out=None, d_k_new=None, d_v_new=None, scale=None, window=0, sinks=0):
-        """rpo_chunk_attention: d_q [rows, n_q_heads, head_dim] (rows may be strided), kv a PagedKV, d_out contiguous, d_lse_out
-        float32 [rows, n_q_heads].  scale defaults to head_dim ** -0.5."""
+    def _chunk_rows(self, d_q, kv, d_q_offsets, d_out, d_lse_out, d_k_new, d_v_new):
+        """Checks what attention calls share; (rows, query heads, row strides of d_q and of d_k_new)."""
         dt, st = self._paged_dtype(kv), kv.struct
         n, hq = d_q.shape[0], d_q.shape[1]
         q_stride = _head_rows(d_q, "d_q", dt, hq, st.head_dim, kv.device)
@@ -364,11 +417,99 @@ class Context:
             raise ValueError("d_out must be contiguous, of d_q's type and shape, on its device")
         if d_lse_out is not None:
             _expect(d_lse_out, "d_lse_out", "float32", (n, hq), kv.device)
+        return n, hq, q_stride, new_stride
+
+    def chunk_attention(self, d_q, kv, d_q_offsets, max_chunk, d_out, d_lse_out=None, d_k_new=None, d_v_new=None, scale=None, window=0, sinks=0):
+        """rpo_chunk_attention: d_q [rows, n_q_heads, head_dim] (rows may be strided), kv a PagedKV, d_out contiguous, d_lse_out
+        float32 [rows, n_q_heads].  scale defaults to head_dim ** -0.5."""
+        n, hq, q_stride, new_stride = self._chunk_rows(d_q, kv, d_q_offsets, d_out, d_lse_out, d_k_new, d_v_new)
         cfg = self._chunk_cfg(kv, scale, window, sinks)
         _check(self.lib.rpo_chunk_attention(self.handle, kv.ref, n, hq, max_chunk, d_q.data_ptr(), q_stride,
                                             None if d_k_new is None else d_k_new.data_ptr(), None if d_v_new is None else d_v_new.data_ptr(),
                                             new_stride, d_q_offsets.data_ptr(), C.byref(cfg), d_out.data_ptr(),
                                             None if d_lse_out is None else d_lse_out.data_ptr()), "rpo_chunk_attention")
+
+    def tree_attention(self, d_q, kv, d_q_offsets, d_parents, max_nodes, d_out, d_lse_out=None, d_k_new=None, d_v_new=None, scale=None, window=0,
+                       sinks=0):
+        """rpo_tree_attention: as chunk_attention, the rows of a sequence being the nodes of a tree; d_parents int32 [rows], -1 a child of
+        the last cached token, -2 no node."""
+        n, hq, q_stride, new_stride = self._chunk_rows(d_q, kv, d_q_offsets, d_out, d_lse_out, d_k_new, d_v_new)
+        _expect(d_parents, "d_parents", "int32", (n,), kv.device)
+        cfg = self._chunk_cfg(kv, scale, window, sinks)
+        _check(self.lib.rpo_tree_attention(self.handle, kv.ref, n, hq, max_nodes, d_q.data_ptr(), q_stride,
+                                           None if d_k_new is None else d_k_new.data_ptr(), None if d_v_new is None else d_v_new.data_ptr(),
+                                           new_stride, d_q_offsets.data_ptr(), d_parents.data_ptr(), C.byref(cfg), d_out.data_ptr(),
+                                           None if d_lse_out is None else d_lse_out.data_ptr()), "rpo_tree_attention")
+
+    def verify_drafts(self, d_logits, d_tokens, d_parents, d_offsets, d_uniform, sampler, d_path_out, d_n_path_out, d_next_out, d_logprobs_out=None,
+                      d_draft_probs=None):
+        """rpo_verify_drafts: d_logits and d_draft_probs float32 [rows, vocab] (rows may be strided), d_tokens and d_parents int32 [rows],
+        d_offsets int32 [n_seqs + 1], d_uniform float32 [rows], d_path_out int32 [n_seqs, max_path], d_n_path_out and d_next_out
+        int32 [n_seqs], d_logprobs_out float32 like d_path_out."""
+        dev = d_logits.device
+        if self.device is not None and dev != self.device:
+            raise ValueError(f"d_logits is on {dev}, the context on {self.device}")
+        strides = []
+        for t, name in ((d_logits, "d_logits"), (d_draft_probs, "d_draft_probs")):
+            if t is None:
+                strides.append(0)
+                continue
+            if t.dim() != 2 or t.dtype is not _dtype("float32") or t.shape != d_logits.shape or t.device != dev or (t.shape[1] > 1 and t.stride(1) != 1):
+                raise ValueError(f"{name} must be float32 [rows, vocab] on {dev} with contiguous rows, got {t.dtype} {tuple(t.shape)}")
+            strides.append(t.stride(0) if t.shape[0] > 1 else t.shape[1])
+        n, vocab = d_logits.shape
+        n_seqs = d_offsets.shape[0] - 1
+        _expect(d_offsets, "d_offsets", "int32", (n_seqs + 1,), dev)
+        _expect(d_tokens, "d_tokens", "int32", (n,), dev)
+        _expect(d_parents, "d_parents", "int32", (n,), dev)
+        _expect(d_uniform, "d_uniform", "float32", (n,), dev)
+        max_path = d_path_out.shape[-1]
+        _expect(d_path_out, "d_path_out", "int32", (n_seqs, max_path), dev)
+        _expect(d_n_path_out, "d_n_path_out", "int32", (n_seqs,), dev)
+        _expect(d_next_out, "d_next_out", "int32", (n_seqs,), dev)
+        if d_logprobs_out is not None:
+            _expect(d_logprobs_out, "d_logprobs_out", "float32", (n_seqs, max_path), dev)
+        _check(self.lib.rpo_verify_drafts(self.handle, n_seqs, n, vocab, d_logits.data_ptr(), strides[0],
+                                          None if d_draft_probs is None else d_draft_probs.data_ptr(), strides[1], d_tokens.data_ptr(),
+                                          d_parents.data_ptr(), d_offsets.data_ptr(), d_uniform.data_ptr(), C.byref(sampler), max_path,
+                                          d_path_out.data_ptr(), d_n_path_out.data_ptr(), d_next_out.data_ptr(),
+                                          None if d_logprobs_out is None else d_logprobs_out.data_ptr()), "rpo_verify_drafts")
+
+    def commit_path(self, layers, d_q_offsets, d_path, d_n_path, d_lens_out):
+        """rpo_commit_path: layers a PagedLayers, d_q_offsets int32 [n_seqs + 1], d_path int32 [n_seqs, max_path], d_n_path and
+        d_lens_out (the caches' d_lens, say) int32 [n_seqs]."""
+        self._paged_dtype(layers)
+        n = layers.n_seqs
+        _expect(d_q_offsets, "d_q_offsets", "int32", (n + 1,), layers.device)
+        _expect(d_path, "d_path", "int32", (n, d_path.shape[-1]), layers.device)
+        _expect(d_n_path, "d_n_path", "int32", (n,), layers.device)
+        _expect(d_lens_out, "d_lens_out", "int32", (n,), layers.device)
+        _check(self.lib.rpo_commit_path(self.handle, layers.array, len(layers.layers), d_q_offsets.data_ptr(), d_path.data_ptr(), d_path.shape[-1],
+                                        d_n_path.data_ptr(), d_lens_out.data_ptr()), "rpo_commit_path")
+
+    def _page_pool(self, pool, layers):
+        self._paged_dtype(layers)
+        if pool.device != layers.device or pool.d_block_table.data_ptr() != layers.layers[0].d_block_table.data_ptr():
+            raise ValueError("the pool must share its block table with the caches")
+
+    def fork_pages(self, pool, layers, d_src, d_dst, d_fork_lens, d_lens_out=None):
+        """rpo_fork_pages: pool a PagePool, layers a PagedLayers, d_src, d_dst, d_fork_lens int32 [forks], d_lens_out int32 [n_seqs]."""
+        self._page_pool(pool, layers)
+        n = d_src.shape[0]
+        for t, name in ((d_src, "d_src"), (d_dst, "d_dst"), (d_fork_lens, "d_fork_lens")):
+            _expect(t, name, "int32", (n,), layers.device)
+        if d_lens_out is not None:
+            _expect(d_lens_out, "d_lens_out", "int32", (layers.n_seqs,), layers.device)
+        _check(self.lib.rpo_fork_pages(self.handle, pool.ref, layers.array, len(layers.layers), n, d_src.data_ptr(), d_dst.data_ptr(),
+                                       d_fork_lens.data_ptr(), None if d_lens_out is None else d_lens_out.data_ptr()), "rpo_fork_pages")
+
+    def reserve_pages(self, pool, layers, d_lens, d_target_lens):
+        """rpo_reserve_pages: d_lens (tokens that stay) and d_target_lens (tokens to hold pages for) int32 [n_seqs]."""
+        self._page_pool(pool, layers)
+        for t, name in ((d_lens, "d_lens"), (d_target_lens, "d_target_lens")):
+            _expect(t, name, "int32", (layers.n_seqs,), layers.device)
+        _check(self.lib.rpo_reserve_pages(self.handle, pool.ref, layers.array, len(layers.layers), d_lens.data_ptr(), d_target_lens.data_ptr()),
+               "rpo_reserve_pages")
 
     def attention_mass(self, d_q, kv, d_q_offsets, max_chunk, d_lse, d_mass_out, d_mass_in=None, scale=None, window=0, sinks=0):
         """rpo_attention_mass: d_lse float32 [rows, n_q_heads] of chunk_attention, d_mass_out (and d_mass_in, which may be the same

@@ -73,6 +73,8 @@ struct Workspace {
   void* op_part_ml = nullptr;     // float2
   void* op_rec = nullptr;         // SplitRec per CTA
   void* op_items = nullptr;       // ChunkItem[OP_MAX_ITEMS], then one ChunkPlan
+  void* op_tree = nullptr;        // TreeRow[TREE_MAX_ROWS]: masks of trees of drafted tokens (paged_tree.cuh)
+  void* op_pages = nullptr;       // PageCopy[PG_MAX_ITEMS], int[PG_MAX_ITEMS], a ticket (pages.cuh)
 };
 
 }  // namespace rpo

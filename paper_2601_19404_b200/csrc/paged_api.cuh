@@ -52,6 +52,7 @@ static ChunkArgs chunk_args(int n_rows, int hq, int max_chunk, const int32_t* of
   ChunkArgs a;
   // positions lie in (-2^30, 2^30): a longer window or more sinks see no more, and sums with them stay in 32 bits
   constexpr int32_t most = 1 << 30;
+  a.parents = nullptr; a.tree = nullptr;
   a.offsets = offsets; a.n_rows = n_rows; a.max_chunk = max_chunk; a.window = std::min(cfg->window, most); a.sinks = std::min(cfg->sinks, most); a.hq = hq;
   return a;
 }
@@ -63,16 +64,16 @@ static SplitWs split_ws(rpo_ctx* c, int rows_cap) {
 }
 
 // Few rows per sequence (decode steps): one CTA pair per SM over an equal share of all pages.
-template <int DH>
+template <int DH, bool TREE>
 static int chunk_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const bf16* k_new, const bf16* v_new,
                        int64_t new_stride, float scale, bf16* out, float* lse) {
   using Cfg = StepCfg<DH>;
-  CUDA_TRY((allow_smem<paged_step_kernel<DH>>(c, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4)));
+  CUDA_TRY((allow_smem<paged_step_kernel<DH, TREE>>(c, Cfg::SMEM + (OP_MAX_SEQS + 1) * 4)));
   const int grid = 2 * c->sm_count;
   StepArgs s;
   s.kv = view; s.c = a; s.q = q; s.q_stride = q_stride; s.k_new = k_new; s.v_new = v_new; s.new_stride = new_stride; s.scale_log2 = scale * 1.4426950408889634f;
   s.o.out = out; s.o.lse = lse; s.o.hq = a.hq; s.o.rep = a.hq / view.hkv; s.ws = split_ws(c, Cfg::ROWS); s.min_share = 4;
-  LAUNCH_OP(c, (paged_step_kernel<DH>), grid, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, s);
+  LAUNCH_OP(c, (paged_step_kernel<DH, TREE>), grid, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, s);
   LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(grid, std::min(a.max_chunk * s.o.rep, Cfg::ROWS)), MERGE_WARPS * 32, 0, s.ws, s.o);
   return RPO_OK;
 }
@@ -100,18 +101,22 @@ static int op_map_rows(rpo_ctx* c, CUtensorMap* m, const bf16* q, int64_t q_stri
   return op_map(c, m, q, 3, dims, strides, box);
 }
 
-// One CTA for the list of items, up to two per SM for the chunk's K and V.
-template <typename T, int DH>
+// One CTA for the list of items, up to two per SM for the chunk's K and V (trees: and the masks of at least one sequence each).
+template <typename T, int DH, bool TREE>
 static int prepare_grid(const PagedView<T>& view, const ChunkArgs& a, const T* k_new) {
+  if (TREE) {
+    const int per = k_new ? ceil_div((int64_t)a.max_chunk * view.hkv * 2 * (DH * sizeof(T) / 16), 2048) : 1;
+    return 1 + std::min<int64_t>((int64_t)view.n_seqs * per, std::max(view.n_seqs, 2 * 148));
+  }
   return 1 + (k_new ? grid_for((int64_t)a.n_rows * view.hkv * 2 * (DH * sizeof(T) / 16), 1024, 2 * 148) : 0);
 }
 
 // Many rows per sequence: tensor-core tiles of 2 x (tokens x heads of a KV head <= 128) rows against 128 keys.
-template <int DH>
+template <int DH, bool TREE>
 static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const bf16* k_new, const bf16* v_new,
                       int64_t new_stride, float scale, bf16* out, float* lse) {
   using Cfg = ChunkCfg<DH>;
-  CUDA_TRY((allow_smem<paged_chunk_kernel<DH>>(c, Cfg::SMEM)));
+  CUDA_TRY((allow_smem<paged_chunk_kernel<DH, TREE>>(c, Cfg::SMEM)));
   ChunkTcArgs t;
   t.kv = view; t.c = a; t.scale_log2 = scale * 1.4426950408889634f;
   t.o.out = out; t.o.lse = lse; t.o.hq = a.hq; t.o.rep = a.hq / view.hkv; t.ws = split_ws(c, OP_PART_ROWS);
@@ -124,19 +129,19 @@ static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   RPO_TRY(op_map_rows(c, &qm, q, q_stride, a.n_rows, a.hq, DH, t.o.rep, t.tq));
   RPO_TRY(op_map_pages(c, &km, view, view.k, DH));
   RPO_TRY(op_map_pages(c, &vm, view, view.v, DH));
-  LAUNCH_OP(c, (chunk_prepare_kernel<bf16, DH, CH_BN / KV_BLOCK>), (prepare_grid<bf16, DH>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4,
+  LAUNCH_OP(c, (chunk_prepare_kernel<bf16, DH, CH_BN / KV_BLOCK, TREE>), (prepare_grid<bf16, DH, TREE>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4,
             2, items, plan, k_new, v_new, new_stride);
-  LAUNCH_OP(c, (paged_chunk_kernel<DH>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
+  LAUNCH_OP(c, (paged_chunk_kernel<DH, TREE>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
   LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, OP_PART_ROWS / (MERGE_WARPS * MERGE_ROWS)), MERGE_WARPS * 32, 0, t.ws, t.o);
   return RPO_OK;
 }
 
 // 32-bit storage: BM rows of an item against tiles of keys on CUDA cores.
-template <int DH, int BM>
+template <int DH, int BM, bool TREE>
 static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& a, const float* q, int64_t q_stride, const float* k_new, const float* v_new,
                       int64_t new_stride, float scale, float* out, float* lse) {
   using Cfg = F32Cfg<DH, BM>;
-  CUDA_TRY((allow_smem<paged_f32_kernel<DH, BM>>(c, Cfg::SMEM)));
+  CUDA_TRY((allow_smem<paged_f32_kernel<DH, BM, TREE>>(c, Cfg::SMEM)));
   F32Args f;
   f.kv = view; f.c = a; f.q = q; f.q_stride = q_stride; f.scale_log2 = scale * 1.4426950408889634f;
   f.o.out = out; f.o.lse = lse; f.o.hq = a.hq; f.o.rep = a.hq / view.hkv; f.ws = split_ws(c, BM);
@@ -146,14 +151,14 @@ static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& 
   ChunkPlan* plan = (ChunkPlan*)(items + OP_MAX_ITEMS);
   f.items = items; f.plan = plan;
   const int grid = std::min(Cfg::CTAS * c->sm_count, OP_GRID * c->sm_count);
-  LAUNCH_OP(c, (chunk_prepare_kernel<float, DH, Cfg::BN / KV_BLOCK>), (prepare_grid<float, DH>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, f.tok, grid, 2, 1, items,
+  LAUNCH_OP(c, (chunk_prepare_kernel<float, DH, Cfg::BN / KV_BLOCK, TREE>), (prepare_grid<float, DH, TREE>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, f.tok, grid, 2, 1, items,
             plan, k_new, v_new, new_stride);
-  LAUNCH_OP(c, (paged_f32_kernel<DH, BM>), grid, 256, Cfg::SMEM, f);
+  LAUNCH_OP(c, (paged_f32_kernel<DH, BM, TREE>), grid, 256, Cfg::SMEM, f);
   LAUNCH_OP(c, (split_merge_kernel<float, DH>), dim3(grid, BM == 64 ? BM / (MERGE_WARPS * MERGE_ROWS) : std::min(a.max_chunk * f.o.rep, BM)), MERGE_WARPS * 32, 0, f.ws, f.o);
   return RPO_OK;
 }
 
-template <typename T, int DH>
+template <typename T, int DH, bool TREE>
 static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs& a, const void* q, int64_t q_stride, const void* k_new,
                              const void* v_new, int64_t new_stride, float scale, void* out, float* lse) {
   const PagedView<T> view = paged_view<T>(c, kv);
@@ -162,30 +167,54 @@ static int chunk_attention_t(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs
   // 1024 .. 4096, 12 on 2 heads of 128: 1 token 154 us (in 64-row tiles 227), 2 tokens 156 (233), 3 tokens 236 in 64-row tiles.
   if constexpr (std::is_same<T, bf16>::value) {
     if (rows <= StepCfg<DH>::ROWS)
-      return chunk_steps<DH>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
-    return chunk_tiles<DH>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
+      return chunk_steps<DH, TREE>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
+    return chunk_tiles<DH, TREE>(c, view, a, (const bf16*)q, q_stride, (const bf16*)k_new, (const bf16*)v_new, new_stride, scale, (bf16*)out, lse);
   } else {
-    if (rows <= 16) return chunk_f32<DH, 16>(c, view, a, (const float*)q, q_stride, (const float*)k_new, (const float*)v_new, new_stride, scale, (float*)out, lse);
-    return chunk_f32<DH, 64>(c, view, a, (const float*)q, q_stride, (const float*)k_new, (const float*)v_new, new_stride, scale, (float*)out, lse);
+    if (rows <= 16) return chunk_f32<DH, 16, TREE>(c, view, a, (const float*)q, q_stride, (const float*)k_new, (const float*)v_new, new_stride, scale, (float*)out, lse);
+    return chunk_f32<DH, 64, TREE>(c, view, a, (const float*)q, q_stride, (const float*)k_new, (const float*)v_new, new_stride, scale, (float*)out, lse);
   }
+}
+
+static int check_append(const rpo_ctx* c, const rpo_paged_kv* kv, int n_rows, const void* d_k_new, const void* d_v_new, int64_t kv_new_stride, const void* d_out) {
+  if ((n_rows > 0 && !d_out) || !aligned16(d_out) || !d_k_new != !d_v_new) return RPO_ERR_INVALID_ARG;
+  if (d_k_new && (!aligned16(d_k_new) || !aligned16(d_v_new) || (kv_new_stride * (int64_t)c->esz) % 16 ||
+                  (n_rows > 1 && kv_new_stride < (int64_t)kv->n_kv_heads * kv->head_dim)))
+    return RPO_ERR_INVALID_ARG;
+  return RPO_OK;
+}
+
+template <bool TREE>
+static int chunk_attention(rpo_ctx* c, const rpo_paged_kv* kv, const ChunkArgs& a, const void* d_q, int64_t q_stride, const void* d_k_new, const void* d_v_new,
+                           int64_t kv_new_stride, float scale, void* d_out, float* d_lse_out) {
+  RPO_TRY(enter(c));
+  ProfScope ps(c, KC_ATTN);
+#define CHUNK_ATTN(T, DH) chunk_attention_t<T, DH, TREE>(c, kv, a, d_q, q_stride, d_k_new, d_v_new, kv_new_stride, scale, d_out, d_lse_out)
+  if (c->bf16) return kv->head_dim == 128 ? CHUNK_ATTN(bf16, 128) : CHUNK_ATTN(bf16, 64);
+  return kv->head_dim == 128 ? CHUNK_ATTN(float, 128) : CHUNK_ATTN(float, 64);
+#undef CHUNK_ATTN
 }
 
 extern "C" int rpo_chunk_attention(rpo_ctx* c, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_chunk, const void* d_q,
                                    int64_t q_stride, const void* d_k_new, const void* d_v_new, int64_t kv_new_stride,
                                    const int32_t* d_q_offsets, const rpo_chunk_cfg* cfg, void* d_out, float* d_lse_out) {
   RPO_TRY(check_chunk(c, kv, n_rows, n_q_heads, max_chunk, d_q, q_stride, d_q_offsets, cfg));
-  if ((n_rows > 0 && !d_out) || !aligned16(d_out) || !d_k_new != !d_v_new) return RPO_ERR_INVALID_ARG;
-  if (d_k_new && (!aligned16(d_k_new) || !aligned16(d_v_new) || (kv_new_stride * (int64_t)c->esz) % 16 ||
-                  (n_rows > 1 && kv_new_stride < (int64_t)kv->n_kv_heads * kv->head_dim)))
-    return RPO_ERR_INVALID_ARG;
+  RPO_TRY(check_append(c, kv, n_rows, d_k_new, d_v_new, kv_new_stride, d_out));
   if (n_rows == 0) return RPO_OK;
-  RPO_TRY(enter(c));
-  ProfScope ps(c, KC_ATTN);
-  const ChunkArgs a = chunk_args(n_rows, n_q_heads, max_chunk, d_q_offsets, cfg);
-#define CHUNK_ATTN(T, DH) chunk_attention_t<T, DH>(c, kv, a, d_q, q_stride, d_k_new, d_v_new, kv_new_stride, cfg->scale, d_out, d_lse_out)
-  if (c->bf16) return kv->head_dim == 128 ? CHUNK_ATTN(bf16, 128) : CHUNK_ATTN(bf16, 64);
-  return kv->head_dim == 128 ? CHUNK_ATTN(float, 128) : CHUNK_ATTN(float, 64);
-#undef CHUNK_ATTN
+  return chunk_attention<false>(c, kv, chunk_args(n_rows, n_q_heads, max_chunk, d_q_offsets, cfg), d_q, q_stride, d_k_new, d_v_new, kv_new_stride, cfg->scale,
+                                d_out, d_lse_out);
+}
+
+extern "C" int rpo_tree_attention(rpo_ctx* c, const rpo_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t max_nodes, const void* d_q,
+                                  int64_t q_stride, const void* d_k_new, const void* d_v_new, int64_t kv_new_stride,
+                                  const int32_t* d_q_offsets, const int32_t* d_parents, const rpo_chunk_cfg* cfg, void* d_out, float* d_lse_out) {
+  RPO_TRY(check_chunk(c, kv, n_rows, n_q_heads, max_nodes, d_q, q_stride, d_q_offsets, cfg));
+  RPO_TRY(check_append(c, kv, n_rows, d_k_new, d_v_new, kv_new_stride, d_out));
+  if (n_rows > 0 && !d_parents) return RPO_ERR_INVALID_ARG;
+  if (max_nodes > TREE_MAX_NODES || n_rows > TREE_MAX_ROWS) return RPO_ERR_LIMIT;
+  if (n_rows == 0) return RPO_OK;
+  ChunkArgs a = chunk_args(n_rows, n_q_heads, max_nodes, d_q_offsets, cfg);
+  a.parents = d_parents; a.tree = (TreeRow*)c->ws.op_tree;
+  return chunk_attention<true>(c, kv, a, d_q, q_stride, d_k_new, d_v_new, kv_new_stride, cfg->scale, d_out, d_lse_out);
 }
 
 template <int DH, int MT>

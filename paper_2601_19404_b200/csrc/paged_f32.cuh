@@ -62,7 +62,8 @@ __device__ __forceinline__ void f32_scores(const float* sq, const float* sk, int
   }
 }
 
-template <int DH, int BM>
+// TREE: the chunks are trees (paged_tree.cuh).
+template <int DH, int BM, bool TREE>
 __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F32Args a) {
   using Cfg = F32Cfg<DH, BM>;
   constexpr int BN = Cfg::BN, TM = BM / 16, KPT = BN / 16, DG = DH / 64, QS = Cfg::QS, PS = Cfg::PS, CPR = DH / 4, LD = BN * CPR / 256;
@@ -88,7 +89,8 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
 
   while (walk.next()) {
     const int R = walk.it.n_tok * rep, p0 = walk.it.p0, p1 = p0 + walk.it.n_tok - 1;
-    const KeyTiles<BN / KV_BLOCK> kt(a.c, p0, p1);
+    const KeyTiles<BN / KV_BLOCK> kt(a.c, walk.it.key0, p1);
+    const TreeRow* nodes = TREE ? a.c.tree + (walk.it.row0 - (p0 - walk.it.key0)) : nullptr;      // the sequence's first node
     const int32_t* tbl = a.kv.table + (int64_t)walk.it.seq * a.kv.table_stride;
     const float* kb = a.kv.k + walk.head * a.kv.head_stride;
     const float* vb = a.kv.v + walk.head * a.kv.head_stride;
@@ -109,7 +111,7 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
 #pragma unroll
       for (int e = 0; e < LD; ++e) {
         const int x = e * 256 + tid, row = x / CPR, ch = x % CPR, j = key0 + row, bk = b[e * 256 / CPR / KV_BLOCK];
-        const bool live = bk >= 0 && j < end && (j >= kt.kp.lo || j < a.c.sinks);
+        const bool live = bk >= 0 && j < end && (j >= kt.kp.lo || j < a.c.sinks) && !(TREE && j >= walk.it.key0 && nodes[j - walk.it.key0].depth < 0);
         cp_async16_zfill(dst + (row * stride + ch * 4) * 4, base + ((int64_t)max(bk, 0) * KV_BLOCK + row % KV_BLOCK) * DH + ch * 4, live);
       }
       fa::cp_commit();
@@ -124,10 +126,15 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
     load(uv, DH, vb, walk.t0, blk);
     float o[TM][DG][4], m[TM], l[TM];
     int prow[TM];
+    const TreeRow* node[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       m[i] = -INFINITY; l[i] = 0.f;
       prow[i] = min(p0 + (r0 + i) / rep, p1);
+      if (TREE) {
+        node[i] = nodes + (prow[i] - walk.it.key0);
+        prow[i] = node[i]->depth < 0 ? -1 : walk.it.key0 + node[i]->depth;
+      }
 #pragma unroll
       for (int g = 0; g < DG; ++g) o[i][g][0] = o[i][g][1] = o[i][g][2] = o[i][g][3] = 0.f;
     }
@@ -141,7 +148,8 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
       if (t + 1 < walk.t1) load(uk, QS, kb, t + 1, blk_next); else fa::cp_commit();
       const int key0 = kt.page0(t) * KV_BLOCK;
       const bool first_range = t < kt.n1;
-      const bool whole = key0 + BN - 1 <= (first_range ? min(p0, a.c.sinks - 1) : p0) &&
+      const int p_whole = TREE ? walk.it.key0 - 1 : p0;
+      const bool whole = key0 + BN - 1 <= (first_range ? min(p_whole, a.c.sinks - 1) : p_whole) &&
                          (a.c.window <= 0 || key0 > p1 - a.c.window || key0 + BN <= a.c.sinks);
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
@@ -150,7 +158,10 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
         for (int j = 0; j < KPT; ++j) {
           s[i][j] *= a.scale_log2;
           const int key = key0 + tx + 16 * j;
-          if (!whole && (!chunk_visible(a.c, key, prow[i]) || (first_range && key >= a.c.sinks))) s[i][j] = -INFINITY;
+          if (TREE && !whole && key >= walk.it.key0) {
+            const int slot = key - walk.it.key0;
+            if (prow[i] < 0 || first_range || slot >= TREE_MAX_NODES || !((node[i]->seen[slot >> 5] >> (slot & 31)) & 1)) s[i][j] = -INFINITY;
+          } else if (!whole && (!chunk_visible(a.c, key, prow[i]) || (first_range && key >= a.c.sinks))) s[i][j] = -INFINITY;
           mx = fmaxf(mx, s[i][j]);
         }
 #pragma unroll
@@ -201,6 +212,11 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
       for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
       const int r = r0 + i;
       if (r >= R) continue;
+      if (TREE && prow[i] < 0) {                             // no node: whatever the tiles without masks gave
+        m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+        for (int g = 0; g < DG; ++g) o[i][g][0] = o[i][g][1] = o[i][g][2] = o[i][g][3] = 0.f;
+      }
       const int64_t dst = (int64_t)(walk.it.row0 + r / rep) * a.o.hq + walk.head * rep + r % rep;
       const int64_t part = (int64_t)(2 * blockIdx.x + (begins ? 1 : 0)) * a.ws.rows_cap + r;
       const float inv = split ? 1.f : l[i] > 0.f ? 1.0f / l[i] : 0.f;

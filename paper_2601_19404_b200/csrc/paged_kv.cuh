@@ -30,10 +30,14 @@ struct PagedView {
 // Rows of the call that belong to sequence s, and the tokens it has in the cache (the chunk's included).
 struct ChunkSpan { int row0, rows, len; };
 
+struct TreeRow;                           // paged_tree.cuh
+
 struct ChunkArgs {
   const int32_t* offsets;                 // [n_seqs + 1]
   int n_rows, max_chunk, window, sinks;   // window 0: none
   int hq;
+  const int32_t* parents;                 // [n_rows], chunks that are trees only
+  TreeRow* tree;                          // [n_rows] workspace of the tiled kernels
 };
 
 __device__ __forceinline__ int paged_len(const int32_t* lens, int s, int table_stride, int* status) {

@@ -21,6 +21,7 @@
 #pragma once
 #include "attn_tc.cuh"
 #include "paged_kv.cuh"
+#include "paged_tree.cuh"
 
 namespace rpo {
 
@@ -223,7 +224,8 @@ struct StepArgs {
   int min_share;
 };
 
-template <int DH>
+// TREE: the chunk's rows are the nodes of a tree (paged_tree.cuh).
+template <int DH, bool TREE>
 __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
   using Cfg = StepCfg<DH>;
   constexpr int ROWS = Cfg::ROWS, STAGES = Cfg::STAGES, PB = Cfg::PAGE_BYTES, KS = DH / 16, NT = DH / 8, CPR = DH / 8;
@@ -258,14 +260,21 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
     bf16* vb = a.kv.v + h * a.kv.head_stride;
     const int32_t* tbl = a.kv.table + (int64_t)s * a.kv.table_stride;
 
+    TreeLane tree;                                                     // lane i: node i
+    if (TREE) tree = tree_lane(a.c, sp, p0, lane, a.kv.status);
+
     // ---- queries as A fragments: rows g, g + 8 of every 16
-    uint32_t qf[KS][4];
+    uint32_t qf[KS][4], seen[2];                                       // TREE: slots of the chunk that the row sees (none: no node)
     int prow[2];
 #pragma unroll
     for (int hh = 0; hh < 2; ++hh) {
       const int r = hh * 8 + g;
       const bool v = r < R;
       prow[hh] = v ? p0 + r / rep : p1;
+      if (TREE) {
+        seen[hh] = __shfl_sync(0xffffffffu, tree.seen, r / rep);
+        prow[hh] = p0 + __shfl_sync(0xffffffffu, tree.depth, r / rep);
+      }
       const uint32_t* qp = reinterpret_cast<const uint32_t*>(a.q + (int64_t)(sp.row0 + (v ? r / rep : 0)) * a.q_stride + (h * rep + (v ? r % rep : 0)) * DH) + tq;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
@@ -294,7 +303,7 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
       auto piece = [&](int e, bool fresh) {
         const int x = e * 32 + lane, row = x / CPR, ch = x % CPR, j = key0 + row;
         // rows that none of the queries sees become zeros: whatever the cache holds there, 0 x NaN included
-        const int bytes = (blk >= 0 && j <= p1 && (j >= kp.lo || j < a.c.sinks)) ? 16 : 0;
+        const int bytes = (blk >= 0 && j <= p1 && (j >= kp.lo || j < a.c.sinks) && (!TREE || j < p0 || ((tree.nodes >> (j - p0)) & 1))) ? 16 : 0;
         const int64_t at = ((int64_t)max(blk, 0) * KV_BLOCK + row) * DH + ch * 8;
         const bf16 *ks = kb + at, *vs = vb + at;
         if (fresh && j >= p0 && bytes) {
@@ -338,7 +347,7 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
         fa::mma_bf16(sc[1], qf[k], b2, b3);
       }
       const int key0 = kp.page(i0 + warp + 4 * it) * KV_BLOCK;
-      const bool whole = key0 + KV_BLOCK - 1 <= p0 && (a.c.window <= 0 || key0 > p1 - a.c.window || key0 + KV_BLOCK <= a.c.sinks);
+      const bool whole = key0 + KV_BLOCK - 1 <= p0 - (TREE ? 1 : 0) && (a.c.window <= 0 || key0 > p1 - a.c.window || key0 + KV_BLOCK <= a.c.sinks);
       uint32_t pf[4];
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
@@ -346,7 +355,9 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           x[e] *= a.scale_log2;
-          if (!whole && !chunk_visible(a.c, key0 + (e >> 1) * 8 + tq * 2 + (e & 1), prow[hh])) x[e] = -INFINITY;
+          const int key = key0 + (e >> 1) * 8 + tq * 2 + (e & 1);
+          if (TREE) { if (!whole && !(key < p0 ? seen[hh] && chunk_visible(a.c, key, prow[hh]) : ((seen[hh] >> (key - p0)) & 1))) x[e] = -INFINITY; }
+          else if (!whole && !chunk_visible(a.c, key, prow[hh])) x[e] = -INFINITY;
         }
         float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
@@ -382,6 +393,11 @@ __global__ void __launch_bounds__(128, 2) paged_step_kernel(StepArgs a) {
 #pragma unroll
     for (int hh = 0; hh < 2; ++hh) {
       const int r = hh * 8 + g;
+      if (TREE && !seen[hh]) {                                         // no node: whatever the pages without masks gave
+        m[hh] = -INFINITY; l[hh] = 0.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[n][2 * hh] = o[n][2 * hh + 1] = 0.f;
+      }
       float ls = l[hh];
       ls += __shfl_xor_sync(0xffffffffu, ls, 1);
       ls += __shfl_xor_sync(0xffffffffu, ls, 2);

@@ -25,8 +25,11 @@
 #include "paged_f32.cuh"
 #include "paged_mass.cuh"
 #include "paged_step.cuh"
+#include "paged_tree.cuh"
+#include "pages.cuh"
 #include "ref_kernels.cuh"
 #include "sampler.cuh"
+#include "verify.cuh"
 
 using namespace rpo;
 
@@ -334,6 +337,8 @@ extern "C" int rpo_create(rpo_ctx** out, const rpo_shape* shape, const rpo_limit
   ALLOC(w.op_part_ml, op_rows * sizeof(float2));
   ALLOC(w.op_rec, (size_t)OP_GRID * c->sm_count * sizeof(SplitRec));
   ALLOC(w.op_items, (size_t)OP_MAX_ITEMS * sizeof(ChunkItem) + sizeof(ChunkPlan));
+  ALLOC(w.op_tree, (size_t)TREE_MAX_ROWS * sizeof(TreeRow));
+  ALLOC(w.op_pages, (size_t)PG_MAX_ITEMS * (sizeof(PageCopy) + 4) + 16);
   if (rc == RPO_OK && cudaMemsetAsync(w.tile_ctr, 0, (size_t)TC_CTR_CAPACITY * 4, c->stream) != cudaSuccess) { cudaGetLastError(); rc = RPO_ERR_CUDA; }
   if (rc == RPO_OK) rc = tc_create(c);
   // The attention kernels mask keys beyond a segment's end instead of zero-filling them, so the
@@ -345,6 +350,7 @@ extern "C" int rpo_create(rpo_ctx** out, const rpo_shape* shape, const rpo_limit
 #undef ALLOC
   if (rc != RPO_OK) { rpo_destroy(c); return rc; }
   cudaMemsetAsync(c->d_status, 0, 16, c->stream);
+  cudaMemsetAsync(w.op_pages, 0, (size_t)PG_MAX_ITEMS * (sizeof(PageCopy) + 4) + 16, c->stream);
   rope_table_kernel<<<grid_for((int64_t)lim->max_positions * (dh / 2), 256), 256, 0, c->stream>>>(
       (float2*)c->d_rope, lim->max_positions, dh / 2, (double)s.rope_base);
   c->launches++;
@@ -1449,6 +1455,7 @@ extern "C" int rpo_gemm_bench(rpo_ctx* c, int32_t M, int32_t N, int32_t K, const
 }
 
 #include "paged_api.cuh"
+#include "draft_api.cuh"
 
 // Reads and clears the device status word (synchronises the stream).  After an expired wait the
 // arrival counters of the split-K launches may be left half-counted: they are cleared too.
