@@ -14,8 +14,10 @@
 // buckets of the exponent and three more bits, so that the elements spread over them whatever the temperature, then nine
 // bits at a time.
 #pragma once
+#include <type_traits>
+
 #include "attn_tc.cuh"
-#include "cache_evict.cuh"
+#include "paged_chunk.cuh"
 #include "sampler.cuh"
 
 namespace rpo {
@@ -34,15 +36,14 @@ struct VerifyArgs {
 
 constexpr int VF_THREADS = 512, VF_WARPS = VF_THREADS / 32;
 constexpr int VF_B1 = 256, VF_COPIES = 8, VF_B2 = 512, VF_BITS = 9;
-constexpr int VF_HIST = VF_B1 * VF_COPIES * 8 + 2 * VF_B2 * 8;
+constexpr int VF_HIST = VF_B1 * VF_COPIES * 8 + VF_B1 * 8 + 3 * VF_B2 * 8;
+constexpr int VF_NODES = 512;                     // what concerns so many nodes is gathered in shared memory at the start
 
 struct MassPair { uint32_t lo, hi; };             // sums of the lower 16 bits and of the others
+struct VerifyNode { int parent, token; uint32_t u24; float q, logit; };       // q, logit: of its token, in its parent's rows
 
-__device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t addr) {
-  uint64_t v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
-  return v;
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // Bucket of a weight >= 1: exponent and three bits below it (monotone).
 __device__ __forceinline__ int verify_bucket(uint32_t w) {
@@ -59,19 +60,44 @@ __device__ __forceinline__ uint64_t verify_scaled(float q, double mass) {
   return q > 0.f ? (uint64_t)__double2ull_rz(fmin(__dmul_rn((double)q, mass), 4.0e18)) : 0ull;
 }
 
+// exp_nonpos(x) 2^30 with the same roundings in fewer instructions: rint by adding 1.5 x 2^23 (and 30), whose low bits then are the
+// exponent that the polynomial's result is raised by.  Numbers below -40 count as -40: between there and -24 the sampler's
+// exponential is 0, this one below 2^-4, which is a weight of 0 too and nothing in a sum.
+__device__ __forceinline__ float verify_exp(float x) {
+  constexpr float shift = 12582912.0f + 30.0f;
+  x = fmaxf(x, -40.0f);
+  const float t = radd(rmul(x, (float)1.44269504088896340736), shift), n = radd(t, -shift);
+  float r = radd(x, rmul(n, -__uint_as_float(0x3F317200u)));
+  r = radd(r, rmul(n, -(float)(0.69314718055994530942 - 0.693145751953125)));
+  float p = (float)(1.0 / 5040.0);
+  p = radd(rmul(p, r), (float)(1.0 / 720.0));
+  p = radd(rmul(p, r), (float)(1.0 / 120.0));
+  p = radd(rmul(p, r), (float)(1.0 / 24.0));
+  p = radd(rmul(p, r), (float)(1.0 / 6.0));
+  p = radd(rmul(p, r), 0.5f);
+  p = radd(rmul(p, r), 1.0f);
+  p = radd(rmul(p, r), 1.0f);
+  return __uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23));
+}
+
 template <int C>
-__global__ void __launch_bounds__(VF_THREADS) verify_kernel(VerifyArgs a) {
+__global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
+  constexpr int PARTS = C * VF_WARPS, PPL = PARTS / 32;                  // sums of the cluster's warps, per lane
   extern __shared__ __align__(16) uint8_t vf_smem[];
-  uint64_t* h1 = reinterpret_cast<uint64_t*>(vf_smem);                   // [bucket][copy] as MassPair, then copy 0 as the bucket's mass
-  uint64_t* h2 = h1 + VF_B1 * VF_COPIES;                                  // two buffers of VF_B2
+  MassPair* h1 = reinterpret_cast<MassPair*>(vf_smem);                   // [bucket][copy]: this CTA's masses
+  uint64_t* t1 = reinterpret_cast<uint64_t*>(h1 + VF_B1 * VF_COPIES);     // [bucket]: the cluster's
+  MassPair* h2 = reinterpret_cast<MassPair*>(t1 + VF_B1);                // of later rounds
+  uint64_t* t2 = reinterpret_cast<uint64_t*>(h2 + VF_B2);                // in turns
   uint32_t* wt = reinterpret_cast<uint32_t*>(vf_smem + (a.top_p24 < (1u << 24) ? VF_HIST : 0));     // this CTA's weights
-  __shared__ uint64_t s_slot[2][2], s_red[VF_WARPS], s_bcast[4], s_wsum[VF_WARPS];
-  __shared__ float s_sume[VF_WARPS];
-  __shared__ int s_bin, s_child, s_token;
+  const uint32_t wt_addr = (uint32_t)__cvta_generic_to_shared(wt);
+  __shared__ __align__(16) ulonglong2 s_part[2][PARTS];      // what the cluster's warps tell, in turns
+  __shared__ uint64_t s_scan[2][VF_WARPS], s_found[2][2];
+  __shared__ int s_bin[2];
+  __shared__ VerifyNode s_node[VF_NODES];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x % C, s = blockIdx.x / C, V = a.V;
   const int c0 = min(V, rank * a.slice), n = min(V, c0 + a.slice) - c0;   // my words [c0, c0 + n)
   const int chunk = ((a.slice + VF_WARPS - 1) / VF_WARPS + 3) & ~3;       // of a warp
-  const int w0 = min(n, warp * chunk), w1 = min(n, w0 + chunk);
+  const int w0 = min(n, warp * chunk), w1 = min(n, w0 + chunk), w4 = w0 + (w1 - w0) / 4 * 4;
   int32_t* path = a.path + (int64_t)s * a.max_path;
   float* logp = a.logprobs ? a.logprobs + (int64_t)s * a.max_path : nullptr;
 
@@ -79,305 +105,355 @@ __global__ void __launch_bounds__(VF_THREADS) verify_kernel(VerifyArgs a) {
   if (row0 < 0 || rows < row0 || rows > a.n_rows) { if (tid == 0) atomicOr(a.status, STATUS_BAD_LENGTH); }
   row0 = min(max(row0, 0), a.n_rows);
   rows = min(max(rows - row0, 0), a.n_rows - row0);
-
-  int turn = 0;                                   // exchanges so far: s_slot is used in turns
-  auto remote = [&](const void* p, int r) { return fa::map_rank((uint32_t)__cvta_generic_to_shared(p), r); };
-  // Sum (or maximum) over the CTAs of one or two words that thread 0 of each holds.
-  auto exchange = [&](uint64_t x, uint64_t y, bool is_max, uint64_t* y_out) {
-    const int b = turn++ & 1;
-    if (tid == 0) { s_slot[b][0] = x; s_slot[b][1] = y; }
-    fa::cluster_sync();
-    if (warp == 0) {
-      uint64_t u = lane < C ? ld_cluster_u64(remote(&s_slot[b][0], lane)) : 0, v = lane < C ? ld_cluster_u64(remote(&s_slot[b][1], lane)) : 0;
-#pragma unroll
-      for (int o = C / 2; o > 0; o >>= 1) {
-        const uint64_t u2 = __shfl_xor_sync(0xffffffffu, u, o);
-        u = is_max ? (u2 > u ? u2 : u) : u + u2;
-        v += __shfl_xor_sync(0xffffffffu, v, o);
-      }
-      if (lane == 0) { s_bcast[0] = u; s_bcast[1] = v; }
-    }
-    __syncthreads();
-    const uint64_t r = s_bcast[0];
-    if (y_out) *y_out = s_bcast[1];
-    __syncthreads();
-    return r;
+  const bool vec = ((a.logits_stride & 3) == 0) && (((uintptr_t)a.logits & 15) == 0);
+  const bool vec_q = ((a.probs_stride & 3) == 0) && (((uintptr_t)a.probs & 15) == 0);
+  const bool unit_T = a.temperature == 1.0f, nucleus = a.top_p24 < (1u << 24) && !a.greedy;
+  auto scaled = [&](float x) { return unit_T ? x : __fdiv_rn(x, a.temperature); };
+  auto fetch = [&](int node) {                    // my words of a node's logits, asynchronously where they are aligned
+    const float* row = a.logits + (int64_t)(row0 + node) * a.logits_stride + c0;
+    if (vec) for (int i = w0 + lane * 4; i < w4; i += 128) fa::cp_async16(wt_addr + i * 4, row + i);
+    fa::cp_commit();
+    for (int i = (vec ? w4 : w0) + lane; i < w1; i += 32) wt[i] = __float_as_uint(row[i]);
   };
-  auto block_max = [&](uint64_t v) {              // valid in thread 0
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) { const uint64_t x = __shfl_xor_sync(0xffffffffu, v, o); v = x > v ? x : v; }
-    if (lane == 0) s_red[warp] = v;
-    __syncthreads();
-    if (warp == 0) {
-      v = lane < VF_WARPS ? s_red[lane] : 0;
-#pragma unroll
-      for (int o = VF_WARPS / 2; o > 0; o >>= 1) { const uint64_t x = __shfl_xor_sync(0xffffffffu, v, o); v = x > v ? x : v; }
+  if (rows > 0) fetch(0);
+  auto gather = [&](int j) {
+    VerifyNode v = {a.parents[row0 + j], a.tokens[row0 + j], verify_u24(a.uniform[row0 + j]), 0.f, 0.f};
+    if (v.parent >= 0 && v.parent < j && v.token >= 0 && v.token < V) {
+      v.logit = a.logits[(int64_t)(row0 + v.parent) * a.logits_stride + v.token];
+      if (a.probs) v.q = a.probs[(int64_t)(row0 + v.parent) * a.probs_stride + v.token];
     }
     return v;
   };
-  // Warps leave their sums in s_wsum; their sum, valid in thread 0.
-  auto block_sum = [&](uint64_t v) {
+  for (int j = tid; j < min(rows, VF_NODES); j += VF_THREADS) s_node[j] = gather(j);
+  auto parent_of = [&](int j) { return j < VF_NODES ? s_node[j].parent : a.parents[row0 + j]; };
+  auto token_of = [&](int j) { return j < VF_NODES ? s_node[j].token : a.tokens[row0 + j]; };
+
+  int turn = 0, pick = 0;                         // exchanges and selections so far: their shared memory is used in turns
+  auto remote = [&](const void* p, int r) { return fa::map_rank((uint32_t)__cvta_generic_to_shared(p), r); };
+  auto warp_sum_u64 = [&](uint64_t v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if (lane == 0) s_wsum[warp] = v;
-    __syncthreads();
-    uint64_t t = 0;
-    if (tid == 0)
-      for (int w = 0; w < VF_WARPS; ++w) t += s_wsum[w];
-    return t;
+    return v;
   };
-  // Among nb buckets with `mass(b)` over all CTAs: the highest with above + (mass of the buckets from it on) >= target.
-  // (nb <= VF_THREADS; every CTA finds the same.)  *above grows by the mass above it.
-  auto select = [&](const uint64_t* hist, int stride, int nb, uint64_t target, uint64_t* above, uint64_t* at) {
-    const int b = nb - 1 - tid;
-    uint64_t m = 0;
-    if (b >= 0) {
+  // Every warp tells all CTAs two words; every warp learns, in x[i] and y[i] of lane l, those of part i * 32 + l (parts in
+  // order of CTA and warp).  One cluster barrier.
+  auto tell = [&](uint64_t x, uint64_t y, uint64_t (&xs)[PPL], uint64_t (&ys)[PPL]) {
+    const int b = turn++ & 1;
+    if (lane < C) asm volatile("st.shared::cluster.v2.u64 [%0], {%1, %2};" ::"r"(remote(&s_part[b][rank * VF_WARPS + warp], lane)), "l"(x), "l"(y) : "memory");
+    fa::cluster_sync();
 #pragma unroll
-      for (int r = 0; r < C; ++r) m += ld_cluster_u64(remote(hist + b * stride, r));
-    }
-    const uint64_t incl = warp_incl_scan_u64(m, lane);
-    if (tid == 0) s_bin = -1;
-    if (lane == 31) s_red[warp] = incl;
-    __syncthreads();
-    uint64_t run = *above + incl - m;
-    for (int w = 0; w < warp; ++w) run += s_red[w];
-    if (b >= 0 && m > 0 && run + m >= target) atomicMax(&s_bin, b);
-    __syncthreads();
-    const int bin = s_bin;
-    if (b == bin) { s_bcast[2] = run; s_bcast[3] = m; }
-    __syncthreads();
-    *above = s_bcast[2]; *at = s_bcast[3];
-    __syncthreads();
-    return bin;
+    for (int i = 0; i < PPL; ++i) { const ulonglong2 v = s_part[b][i * 32 + lane]; xs[i] = v.x; ys[i] = v.y; }
   };
+  auto sum_of = [&](const uint64_t (&xs)[PPL]) {
+    uint64_t v = 0;
+#pragma unroll
+    for (int i = 0; i < PPL; ++i) v += xs[i];
+    return warp_sum_u64(v);
+  };
+  // Adds a bucket's mass to all CTAs' totals (few buckets hold any).
+  auto spread = [&](uint64_t* total, MassPair p) {
+    const uint64_t m = p.lo + ((uint64_t)p.hi << 16);
+    if (m == 0) return;
+#pragma unroll
+    for (int r = 0; r < C; ++r) asm volatile("red.relaxed.cluster.shared::cluster.add.u64 [%0], %1;" ::"r"(remote(total, r)), "l"(m) : "memory");
+  };
+  // Among nb <= VF_THREADS buckets of masses total[b]: the highest with *above + (mass of the buckets from it on) >= target (the
+  // highest that is not empty, for a target of 0).  *above grows by the mass above it.  Leaves zeros behind.
+  auto select = [&](uint64_t* total, int nb, uint64_t target, uint64_t* above, uint64_t* at) {
+    const int b = nb - 1 - tid, k = pick++ & 1;
+    uint64_t m = 0;
+    if (b >= 0) { m = total[b]; total[b] = 0; }
+    const uint64_t incl = warp_incl_scan_u64(m, lane);
+    if (lane == 31) s_scan[k][warp] = incl;
+    __syncthreads();
+    const uint64_t before = warp_sum_u64(lane < warp ? s_scan[k][lane & (VF_WARPS - 1)] : 0) + incl - m, run = *above + before;
+    if (m > 0 && run + m >= target && (run < target || before == 0)) { s_bin[k] = b; s_found[k][0] = run; s_found[k][1] = m; }
+    __syncthreads();
+    *above = s_found[k][0]; *at = s_found[k][1];
+    return s_bin[k];
+  };
+  // Weights below this never decide the nucleus: all of them together are less than what it leaves out (the largest is 2^30).
+  const uint32_t floor_w = max(1u, (uint32_t)(((uint64_t)((1u << 24) - a.top_p24) << 6) / (uint32_t)V));
 
-  const bool vec = ((a.logits_stride & 3) == 0) && (((uintptr_t)a.logits & 15) == 0);
-  const bool unit_T = a.temperature == 1.0f;
+  if (nucleus) {
+    for (int i = tid; i < VF_B1; i += VF_THREADS) t1[i] = 0;
+    for (int i = tid; i < 2 * VF_B2; i += VF_THREADS) t2[i] = 0;
+  }
+  __syncthreads();
   int cur = 0, count = 0, next = -1;
   bool live = rows > 0;
-  for (; live && count < a.max_path; ) {
-    const int node_row = row0 + cur, token_here = a.tokens[node_row];
+  uint64_t xs[PPL], ys[PPL];
+  while (live && count < a.max_path) {
     if (rank == 0 && tid == 0) path[count] = cur;
-    if (a.eos_id >= 0 && token_here == a.eos_id) {
+    if (a.eos_id >= 0 && token_of(cur) == a.eos_id) {
       if (rank == 0 && tid == 0 && logp) logp[count] = 0.f;
       ++count;
       break;
     }
-    // ---- the row's logits into shared memory, their maximum (lowest token among equal ones)
-    const float* row = a.logits + (int64_t)node_row * a.logits_stride;
-    float best = -INFINITY; int best_c = 0x7FFFFFFF;
-    auto see = [&](int i, float x) {
-      x = x < INFINITY ? x : -INFINITY;           // what is no number, or too large, counts as excluded
-      if (x > best) { best = x; best_c = c0 + i; }
-      return __float_as_uint(x);
-    };
-    if (vec) {
-      for (int i = w0 + lane * 4; i < w1; i += 128) {
-        if (i + 3 < w1) {
-          const float4 x = *reinterpret_cast<const float4*>(row + c0 + i);
-          uint4 y;
-          y.x = see(i, x.x); y.y = see(i + 1, x.y); y.z = see(i + 2, x.z); y.w = see(i + 3, x.w);
-          *reinterpret_cast<uint4*>(wt + i) = y;
-        } else {
-          for (int j = i; j < w1; ++j) wt[j] = see(j, row[c0 + j]);
-        }
+    // ---- the first child, whose row is likely to be next
+    auto child_behind = [&](int last) {
+      for (int j = last + 1; j < rows; j += 32) {
+        const unsigned hit = __ballot_sync(0xffffffffu, j + lane < rows && parent_of(j + lane) == cur);
+        if (hit) return j + __ffs(hit) - 1;
       }
-    } else {
-      for (int i = w0 + lane; i < w1; i += 32) wt[i] = see(i, row[c0 + i]);
+      return -1;
+    };
+    int child = count + 1 < a.max_path ? child_behind(cur) : -1;
+    // ---- the row's logits are in shared memory: their maximum
+    const float* row = a.logits + (int64_t)(row0 + cur) * a.logits_stride;
+    if (nucleus) for (int i = tid; i < VF_B1 * VF_COPIES; i += VF_THREADS) h1[i] = MassPair{0, 0};
+    fa::cp_wait<0>();
+    __syncwarp();
+    if (child >= 0)
+      for (int i = w0 + lane * 32; i < w1; i += 1024)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(a.logits + (int64_t)(row0 + child) * a.logits_stride + c0 + i));
+    auto row_max = [&]() {                        // (what is no number counts as excluded)
+      float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      for (int i = w0 + lane * 4; i < w4; i += 128) {
+        const float4 y = *reinterpret_cast<const float4*>(wt + i);
+        m[0] = fmaxf(m[0], y.x); m[1] = fmaxf(m[1], y.y); m[2] = fmaxf(m[2], y.z); m[3] = fmaxf(m[3], y.w);
+      }
+      if (w4 + lane < w1) m[0] = fmaxf(m[0], __uint_as_float(wt[w4 + lane]));
+      tell(__float_as_uint(warp_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])))), 0, xs, ys);
+      float top = __uint_as_float((uint32_t)xs[0]);
+#pragma unroll
+      for (int i = 1; i < PPL; ++i) top = fmaxf(top, __uint_as_float((uint32_t)xs[i]));
+      return warp_max(top);
+    };
+    float top = row_max();
+    if (top == INFINITY) {                        // too large: excluded too
+      for (int i = w0 + lane; i < w1; i += 32) if (__uint_as_float(wt[i]) == INFINITY) wt[i] = __float_as_uint(-INFINITY);
+      __syncwarp();
+      top = row_max();
     }
-    uint64_t key = 0;
-    if (best_c != 0x7FFFFFFF) {
-      const uint32_t b = __float_as_uint(best + 0.0f);
-      key = ((uint64_t)((b & 0x80000000u) ? ~b : (b | 0x80000000u)) << 32) | (0xFFFFFFFFu - (uint32_t)best_c);
-    }
-    key = exchange(block_max(key), 0, true, nullptr);
-    const int argmax = key ? (int)(0xFFFFFFFFu - (uint32_t)key) : -1;
-    const uint32_t ord = (uint32_t)(key >> 32);
-    const float top = key ? __uint_as_float((ord & 0x80000000u) ? (ord & 0x7FFFFFFFu) : ~ord) : 0.f;
-    const float zmax = unit_T ? top : __fdiv_rn(top, a.temperature);
-    const bool nucleus = a.top_p24 < (1u << 24) && !a.greedy;
-    // ---- weights, their sum, and the sum of the exponentials for the log-probability
-    if (nucleus) {
-      for (int i = tid; i < VF_B1 * VF_COPIES; i += VF_THREADS) h1[i] = 0;
-      __syncthreads();
-    }
+    const bool any = top > -INFINITY;
+    const float zmax = any ? scaled(top) : 0.f;
+    // ---- weights, their sum, and the sum of the exponentials (times 2^30) for the log-probability
     uint64_t tot = 0;
     float sume = 0.f;
-    for (int i = w0 + lane; i < w1; i += 32) {
-      const float x = __uint_as_float(wt[i]);
-      const float e = key ? exp_nonpos(radd(unit_T ? x : __fdiv_rn(x, a.temperature), -zmax)) : 0.f;
-      sume += e;
-      const uint32_t w = a.greedy ? (c0 + i == argmax ? 1u : 0u) : __float2uint_rz(rmul(e, 1073741824.0f));
-      wt[i] = w;
-      tot += w;
-      if (nucleus && w) {
-        MassPair* h = reinterpret_cast<MassPair*>(h1) + verify_bucket(w) * VF_COPIES + (lane & (VF_COPIES - 1));
-        atomicAdd(&h->lo, w & 0xFFFFu);
-        if (w >> 16) atomicAdd(&h->hi, w >> 16);
+    auto put = [&](uint32_t w) {
+      if (w < floor_w) return;
+      MassPair* h = h1 + verify_bucket(w) * VF_COPIES + (lane & (VF_COPIES - 1));
+      atomicAdd(&h->lo, w & 0xFFFFu);
+      if (w >> 16) atomicAdd(&h->hi, w >> 16);
+    };
+    auto weigh = [&](auto unit, auto hist) {      // (what does not change within a row is decided outside the loop)
+      auto e_of = [&](float x) { return verify_exp(radd(unit.value ? x : __fdiv_rn(x, a.temperature), -zmax)); };
+      for (int i = w0 + lane * 4; i < w4; i += 128) {
+        const float4 y = *reinterpret_cast<const float4*>(wt + i);
+        const float e0 = e_of(y.x), e1 = e_of(y.y), e2 = e_of(y.z), e3 = e_of(y.w);
+        const uint4 w = make_uint4(__float2uint_rz(e0), __float2uint_rz(e1), __float2uint_rz(e2), __float2uint_rz(e3));
+        sume += (e0 + e1) + (e2 + e3);
+        tot += w.x + w.y;                         // (2^31 at most)
+        tot += w.z + w.w;
+        *reinterpret_cast<uint4*>(wt + i) = w;
+        if (hist.value) { put(w.x); put(w.y); put(w.z); put(w.w); }
       }
-    }
-    sume = warp_sum(sume);
-    if (lane == 0) s_sume[warp] = sume;
-    const uint64_t mine = block_sum(tot);
-    float sum_cta = 0.f;
-    if (tid == 0)
-      for (int w = 0; w < VF_WARPS; ++w) sum_cta += s_sume[w];
-    if (nucleus) {                                // (block_sum's barriers: the histogram is complete)
-      if (tid < VF_B1) {
-        uint64_t m = 0;
+      if (w4 + lane < w1) {
+        const float e = e_of(__uint_as_float(wt[w4 + lane]));
+        const uint32_t w = __float2uint_rz(e);
+        sume += e; tot += w; wt[w4 + lane] = w;
+        if (hist.value) put(w);
+      }
+    };
+    using yes = std::true_type; using no = std::false_type;
+    if (!any) {
+      for (int i = w0 + lane; i < w1; i += 32) wt[i] = 0;
+    } else if (nucleus) {
+      if (unit_T) weigh(yes(), yes()); else weigh(no(), yes());
+    } else if (a.greedy) {                        // a weight of one at the lowest maximum
+      int at = INT_MAX;
+      for (int i = w0 + lane; i < w1; i += 32) if (__uint_as_float(wt[i]) == top) at = min(at, c0 + i);
+      if (unit_T) weigh(yes(), no()); else weigh(no(), no());
+      tell(__reduce_min_sync(0xffffffffu, at), 0, xs, ys);
+      at = INT_MAX;
 #pragma unroll
-        for (int k = 0; k < VF_COPIES; ++k) { const MassPair p = reinterpret_cast<MassPair*>(h1)[tid * VF_COPIES + k]; m += p.lo + ((uint64_t)p.hi << 16); }
-        h1[tid * VF_COPIES] = m;
+      for (int i = 0; i < PPL; ++i) at = min(at, (int)xs[i]);
+      at = __reduce_min_sync(0xffffffffu, at) - c0;
+      tot = 0;
+      for (int i = w0 + lane; i < w1; i += 32) { wt[i] = i == at; tot += i == at; }
+    } else {
+      if (unit_T) weigh(yes(), no()); else weigh(no(), no());
+    }
+    uint64_t left = warp_sum_u64(tot);            // what is left in this warp's words, where `sums` says so
+    if (nucleus) {
+      __syncthreads();                            // the histogram is complete
+      if (tid < VF_B1) {
+        MassPair p = {0, 0};                      // (a word sums pieces of 2^18 / 8 weights below 2^16 at most)
+#pragma unroll
+        for (int k = 0; k < VF_COPIES; ++k) { const MassPair y = h1[tid * VF_COPIES + ((k + tid) & (VF_COPIES - 1))]; p.lo += y.lo; p.hi += y.hi; }
+        spread(t1 + tid, p);
       }
     }
-    uint64_t sum_fixed;                           // of the exponentials, in units of 2^-40 (each CTA's float sum rounded once)
-    uint64_t mass = exchange(mine, (uint64_t)__float2ull_rn(sum_cta * 1099511627776.f), false, &sum_fixed);
+    // (the warps' sums of exponentials travel as whole multiples of 2^-10 x 2^-30, so that their order plays no part)
+    tell(left, (uint64_t)__float2ull_rn(warp_sum(sume) * 1024.f), xs, ys);
+    uint64_t mass = sum_of(xs);
+    const float log_total = logf((float)sum_of(ys) * (1.f / 1099511627776.f));
     uint32_t tau = 1;
     if (nucleus && mass) {
       const uint64_t target = mul_shift24(mass, a.top_p24);
       uint64_t above = 0, at = 0;
-      const int b1 = select(h1, VF_COPIES, VF_B1, target, &above, &at);
+      const int b1 = select(t1, VF_B1, target, &above, &at);
       // b1: exponent e and three bits; the bits below in steps of nine
       const int e = b1 >> 3;
       int rest = max(e - 3, 0);
       uint32_t pre = e >= 3 ? 8u | (b1 & 7) : (8u | (b1 & 7)) >> (3 - e);       // the weight's leading bits so far
       for (int round = 0; rest > 0; ++round) {
         const int bits = min(rest, VF_BITS);
-        uint64_t* h = h2 + (round & 1) * VF_B2;
-        for (int i = tid; i < VF_B2; i += VF_THREADS) h[i] = 0;
+        h2[tid] = MassPair{0, 0};
+        static_assert(VF_B2 == VF_THREADS, "a bucket per thread");
         __syncthreads();
-        for (int i = w0 + lane; i < w1; i += 32) {
-          const uint32_t w = wt[i];
-          if (w >> rest == pre) {
-            MassPair* p = reinterpret_cast<MassPair*>(h) + ((w >> (rest - bits)) & ((1u << bits) - 1));
-            atomicAdd(&p->lo, w & 0xFFFFu);
-            if (w >> 16) atomicAdd(&p->hi, w >> 16);
-          }
+        auto add = [&](uint32_t w) {
+          if (w >> rest != pre) return;
+          MassPair* p = h2 + ((w >> (rest - bits)) & ((1u << bits) - 1));
+          atomicAdd(&p->lo, w & 0xFFFFu);
+          if (w >> 16) atomicAdd(&p->hi, w >> 16);
+        };
+        for (int i = w0 + lane * 4; i < w4; i += 128) {
+          const uint4 y = *reinterpret_cast<const uint4*>(wt + i);
+          add(y.x); add(y.y); add(y.z); add(y.w);
         }
+        if (w4 + lane < w1) add(wt[w4 + lane]);
         __syncthreads();
-        for (int i = tid; i < VF_B2; i += VF_THREADS) { const MassPair p = reinterpret_cast<MassPair*>(h)[i]; h[i] = p.lo + ((uint64_t)p.hi << 16); }
+        uint64_t* t = t2 + (round & 1) * VF_B2;
+        spread(t + tid, h2[tid]);
         fa::cluster_sync();
-        const int bin = select(h, 1, 1 << bits, target, &above, &at);
+        const int bin = select(t, 1 << bits, target, &above, &at);
         pre = (pre << bits) | bin;
         rest -= bits;
       }
       tau = pre;
       mass = above + at;
     }
-    // ---- children
-    int accepted = -1, token = -1;
-    bool lazy = false, sums = !nucleus;           // lazy: a - d with the last test's mass is what is left; sums: s_wsum holds it by warps
+    // ---- children (every warp by itself, all with the same result)
+    int accepted = -1;
+    float accepted_logit = 0.f;
+    bool lazy = false, sums = !nucleus;           // lazy: a - d with the last test's mass is what is left
     double lazy_mass = 0;
-    auto value = [&](int i) -> uint32_t {         // what is left of word i
-      const uint32_t w = wt[i];
-      return w >= tau ? w : 0u;
-    };
-    const float* q = a.probs ? a.probs + (int64_t)node_row * a.probs_stride : nullptr;
-    auto less = [&](int i, double m) -> uint32_t {
-      const uint32_t w = value(i);
-      if (!w) return 0u;
-      const uint64_t d = verify_scaled(q[c0 + i], m);
+    auto value = [&](uint32_t w) -> uint32_t { return w >= tau ? w : 0u; };
+    const float* q = a.probs ? a.probs + (int64_t)(row0 + cur) * a.probs_stride : nullptr;
+    auto less = [&](uint32_t w, float prob, double m) -> uint32_t {
+      const uint64_t d = verify_scaled(prob, m);
       return d < w ? w - (uint32_t)d : 0u;
     };
-    bool refused = false;                         // drafts without probabilities: some child was refused
-    for (int last = cur; count + 1 < a.max_path; ) {
-      // the next child: all CTAs' first warps look for it
-      if (warp == 0) {
-        int child = -1;
-        for (int j = last + 1; j < rows; j += 32) {
-          const unsigned hit = __ballot_sync(0xffffffffu, j + lane < rows && a.parents[row0 + j + lane] == cur);
-          if (hit) { child = j + __ffs(hit) - 1; break; }
+    // f(i, x) for this warp's words, four at a time: what is left of words i .. i + 3 after the test with mass m (or all of them, without
+    // q); probabilities are read where something is left to take from.
+    auto each4 = [&](bool test, double m, auto f) {
+      for (int i0 = w0 + lane * 4; i0 < w1; i0 += 128 * 4) {
+        uint4 y[4];
+        float4 p[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int i = i0 + 128 * u;
+          y[u] = make_uint4(0, 0, 0, 0); p[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (i >= w1) continue;
+          y[u] = *reinterpret_cast<const uint4*>(wt + i);                  // (words behind w1 are another warp's, or padding)
+          y[u].x = value(y[u].x);
+          y[u].y = i + 1 < w1 ? value(y[u].y) : 0u; y[u].z = i + 2 < w1 ? value(y[u].z) : 0u; y[u].w = i + 3 < w1 ? value(y[u].w) : 0u;
+          if (!test || !(y[u].x | y[u].y | y[u].z | y[u].w)) continue;
+          if (vec_q && i + 3 < w1) p[u] = *reinterpret_cast<const float4*>(q + c0 + i);
+          else { p[u].x = q[c0 + i]; if (y[u].y) p[u].y = q[c0 + i + 1]; if (y[u].z) p[u].z = q[c0 + i + 2]; if (y[u].w) p[u].w = q[c0 + i + 3]; }
         }
-        if (lane == 0) s_child = child;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int i = i0 + 128 * u;
+          if (i >= w1) continue;
+          if (test) {
+            if (y[u].x) y[u].x = less(y[u].x, p[u].x, m);
+            if (y[u].y) y[u].y = less(y[u].y, p[u].y, m);
+            if (y[u].z) y[u].z = less(y[u].z, p[u].z, m);
+            if (y[u].w) y[u].w = less(y[u].w, p[u].w, m);
+          }
+          f(i, y[u]);
+        }
       }
-      __syncthreads();
-      const int child = s_child;
-      if (child < 0) break;
-      last = child;
-      if (lazy) {                                 // make what the last test left the weights
-        for (int i = w0 + lane; i < w1; i += 32) wt[i] = less(i, lazy_mass);      // (nobody reads them for that test any more)
+    };
+    bool refused = false;                         // drafts without probabilities: some child was refused
+    auto same_before = [&](int child, int x) {    // has an earlier child the same token?
+      bool again = false;
+      for (int j = cur + 1; j < child; j += 32) again = again || __any_sync(0xffffffffu, j + lane < child && parent_of(j + lane) == cur && token_of(j + lane) == x);
+      return again;
+    };
+    for (; child >= 0; child = child_behind(child)) {
+      if (lazy) {                                 // make what the last test left the weights (nobody reads them for that test any more)
+        each4(true, lazy_mass, [&](int i, const uint4& y) {
+          if (i + 3 < w1) *reinterpret_cast<uint4*>(wt + i) = y;
+          else { wt[i] = y.x; if (i + 1 < w1) wt[i + 1] = y.y; if (i + 2 < w1) wt[i + 2] = y.z; }
+        });
         tau = 1; lazy = false;
         fa::cluster_sync();
       }
-      if (warp == 0) {
-        const int x = a.tokens[row0 + child];
-        const bool in = x >= 0 && x < V;
-        if (!in && lane == 0) atomicOr(a.status, STATUS_BAD_TOKEN);
-        uint64_t w = 0;
-        if (in) {
-          uint32_t y;
-          asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(y) : "r"(remote(wt + x % a.slice, x / a.slice)) : "memory");
-          w = y >= tau ? y : 0;
-        }
-        uint64_t d = mass;
-        if (q) d = in ? verify_scaled(q[x], (double)mass) : 0;
-        else {                                    // a token that was refused before has nothing left
-          bool again = false;
-          for (int j = cur + 1; j < child; j += 32)
-            again = again || __any_sync(0xffffffffu, j + lane < child && a.parents[row0 + j + lane] == cur && a.tokens[row0 + j + lane] == x);
-          if (again) w = 0;
-        }
-        const bool yes = mul_shift24(d, verify_u24(a.uniform[row0 + child])) < w;
-        if (lane == 0) { s_bcast[2] = w; s_bcast[3] = yes; s_token = x; }
+      const VerifyNode v = child < VF_NODES ? s_node[child] : gather(child);
+      const bool in = v.token >= 0 && v.token < V;
+      if (!in && tid == 0) atomicOr(a.status, STATUS_BAD_TOKEN);
+      uint64_t w = 0;
+      if (in) {
+        uint32_t y;
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(y) : "r"(remote(wt + v.token % a.slice, v.token / a.slice)) : "memory");
+        w = value(y);
       }
-      __syncthreads();
-      const uint64_t w = s_bcast[2];
-      if (s_bcast[3]) { accepted = child; token = s_token; }
-      __syncthreads();
-      if (accepted >= 0) break;
+      if (!q && same_before(child, v.token)) w = 0;                        // a token that was refused before has nothing left
+      if (mul_shift24(q ? verify_scaled(v.q, (double)mass) : mass, v.u24) < w) { accepted = child; accepted_logit = v.logit; break; }
       if (!q) {
-        if (w < mass) mass -= w;                  // (all of it is never refused)
+        if (w < mass) {                           // (all of it is never refused)
+          mass -= w;
+          const int i = v.token - c0;
+          if (w && i >= w0 && i < w1) left -= w;  // (zeroed below)
+        }
         refused = true;
       } else {
-        uint64_t left = 0;
         const double m = (double)mass;
-        for (int i = w0 + lane; i < w1; i += 32) left += less(i, m);
-        left = exchange(block_sum(left), 0, false, nullptr);
-        if (left) { mass = left; lazy = true; lazy_mass = m; sums = true; }
+        uint64_t rest = 0;
+        each4(true, m, [&](int, const uint4& y) { rest += (uint64_t)y.x + y.y + y.z + y.w; });
+        rest = warp_sum_u64(rest);
+        tell(rest, 0, xs, ys);
+        const uint64_t all = sum_of(xs);
+        if (all) { mass = all; lazy = true; lazy_mass = m; left = rest; sums = true; }
         else sums = false;
       }
     }
     // ---- without an accepted child: the next token
     if (accepted < 0 && mass) {
-      if (refused) {
-        fa::cluster_sync();                       // nobody reads the refused tokens' weights any more
-        for (int j = cur + 1 + tid; j < rows; j += VF_THREADS)
-          if (a.parents[row0 + j] == cur) { const int x = a.tokens[row0 + j] - c0; if (x >= 0 && x < n) wt[x] = 0; }
-        __syncthreads();
-        sums = false;
-      }
-      uint64_t local = 0;
-      auto left = [&](int i) { return lazy ? less(i, lazy_mass) : value(i); };
+      auto drop_refused = [&]() {                 // this warp's words of refused tokens, once nobody reads them any more
+        for (int j = cur + 1 + lane; j < rows; j += 32)
+          if (parent_of(j) == cur) { const int x = token_of(j) - c0; if (x >= w0 && x < w1) wt[x] = 0; }
+        __syncwarp();
+      };
       if (!sums) {
-        for (int i = w0 + lane; i < w1; i += 32) local += left(i);
-        local = block_sum(local);
-      } else if (tid == 0) {
-        for (int w = 0; w < VF_WARPS; ++w) local += s_wsum[w];
+        if (refused) { fa::cluster_sync(); drop_refused(); refused = false; }
+        left = 0;
+        each4(lazy, lazy_mass, [&](int, const uint4& y) { left += (uint64_t)y.x + y.y + y.z + y.w; });
+        left = warp_sum_u64(left);
       }
-      // mass in the CTAs before mine
-      const int b = turn++ & 1;
-      if (tid == 0) { s_slot[b][0] = local; s_token = -1; }
-      fa::cluster_sync();
-      uint64_t base = 0, r = mul_shift24(mass, verify_u24(a.uniform[row0]));
-      for (int k = 0; k < rank; ++k) base += ld_cluster_u64(remote(&s_slot[b][0], k));
-      for (int w = 0; w < warp; ++w) base += s_wsum[w];
-      if (r >= base && r < base + s_wsum[warp]) {          // one warp of the cluster
+      tell(left, 0, xs, ys);
+      if (refused) drop_refused();
+      // mass in the parts before mine
+      const uint64_t r = mul_shift24(mass, rows <= VF_NODES ? s_node[0].u24 : verify_u24(a.uniform[row0]));
+      uint64_t base = 0;
+#pragma unroll
+      for (int i = 0; i < PPL; ++i) base += i * 32 + lane < rank * VF_WARPS + warp ? xs[i] : 0;
+      base = warp_sum_u64(base);
+      if (r >= base && r < base + left) {         // one warp of the cluster
         for (int i = w0; i < w1; i += 128) {
           uint32_t x[4];
           uint64_t sum = 0;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) { x[k] = i + lane * 4 + k < w1 ? left(i + lane * 4 + k) : 0u; sum += x[k]; }
+          for (int k = 0; k < 4; ++k) {
+            const int j = i + lane * 4 + k;
+            x[k] = j < w1 ? value(wt[j]) : 0u;
+            if (lazy && x[k]) x[k] = less(x[k], q[c0 + j], lazy_mass);
+            sum += x[k];
+          }
           const uint64_t incl = warp_incl_scan_u64(sum, lane);
           const unsigned hit = __ballot_sync(0xffffffffu, base + incl > r);
           if (hit) {
             if (lane == __ffs(hit) - 1) {
               uint64_t run = base + incl - sum;
-              int k = 0;
-              while (k < 3 && run + x[k] <= r) run += x[k++];
-              const int tok = c0 + i + lane * 4 + k;
+              int tok = c0 + i + lane * 4;
+#pragma unroll
+              for (int k = 0; k < 3; ++k) { run += x[k]; if (run <= r) ++tok; else run = ~0ull >> 1; }
               a.next[s] = tok;
-              if (logp) logp[count] = radd(unit_T ? row[tok] : __fdiv_rn(row[tok], a.temperature), -zmax) - logf((float)sum_fixed * (1.f / 1099511627776.f));
+              if (logp) logp[count] = radd(scaled(row[tok]), -zmax) - log_total;
             }
             break;
           }
@@ -386,14 +462,17 @@ __global__ void __launch_bounds__(VF_THREADS) verify_kernel(VerifyArgs a) {
       }
       next = 0;                                   // written above
     } else if (rank == 0 && tid == 0) {
-      if (logp) logp[count] = accepted < 0 ? -INFINITY
-          : radd(unit_T ? row[token] : __fdiv_rn(row[token], a.temperature), -zmax) - logf((float)sum_fixed * (1.f / 1099511627776.f));
+      if (logp) logp[count] = accepted < 0 ? -INFINITY : radd(scaled(accepted_logit), -zmax) - log_total;
     }
     ++count;
-    live = accepted >= 0;
+    live = accepted >= 0 && count < a.max_path;
     cur = accepted;
-    if (live) fa::cluster_sync();                 // nobody reads this row's weights any more
+    if (live) {
+      fa::cluster_sync();                         // nobody reads this row's weights any more
+      fetch(cur);
+    }
   }
+  fa::cp_wait<0>();
   if (rank == 0) {
     if (tid == 0) { a.n_path[s] = count; if (next < 0) a.next[s] = -1; }
     for (int i = count + tid; i < a.max_path; i += VF_THREADS) { path[i] = -1; if (logp) logp[i] = 0.f; }
