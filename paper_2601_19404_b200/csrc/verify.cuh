@@ -35,21 +35,12 @@ struct VerifyArgs {
 };
 
 constexpr int VF_THREADS = 512, VF_WARPS = VF_THREADS / 32;
-constexpr int VF_B1 = 256, VF_COPIES = 8, VF_B2 = 512, VF_BITS = 9;
-constexpr int VF_HIST = VF_B1 * VF_COPIES * 8 + VF_B1 * 8 + 3 * VF_B2 * 8;
-constexpr int VF_NODES = 512;                     // what concerns so many nodes is gathered in shared memory at the start
+constexpr int VF_B1 = 256, VF_COPIES = 4, VF_B2 = 512, VF_BITS = 9;
+constexpr int VF_HIST = VF_B1 * VF_COPIES * 8 + VF_B1 * 8 + 2 * VF_B2 * 8;      // with the weights of 2^17 tokens and more two CTAs fit an SM
+constexpr int VF_NODES = 256;                     // what concerns so many nodes is gathered in shared memory at the start
 
 struct MassPair { uint32_t lo, hi; };             // sums of the lower 16 bits and of the others
 struct VerifyNode { int parent, token; uint32_t u24; float q, logit; };       // q, logit: of its token, in its parent's rows
-
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
-// Bucket of a weight >= 1: exponent and three bits below it (monotone).
-__device__ __forceinline__ int verify_bucket(uint32_t w) {
-  const int e = 31 - __clz(w);
-  return e * 8 + (e >= 3 ? (w >> (e - 3)) & 7 : (w << (3 - e)) & 7);
-}
 
 __device__ __forceinline__ uint32_t verify_u24(float u) {
   return u > 0.f ? min(__float2uint_rz(u * 16777216.f), (1u << 24) - 1) : 0u;
@@ -80,14 +71,20 @@ __device__ __forceinline__ float verify_exp(float x) {
   return __uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23));
 }
 
+// Adds a weight to a bucket where `in` says so, without a branch.
+__device__ __forceinline__ void mass_add(uint32_t addr, uint32_t w, bool in) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %3, 0;\n @p red.shared.add.u32 [%0], %1;\n @p red.shared.add.u32 [%0 + 4], %2;\n}"
+               ::"r"(addr), "r"(w & 0xFFFFu), "r"(w >> 16), "r"((uint32_t)in) : "memory");
+}
+
 template <int C>
 __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
   constexpr int PARTS = C * VF_WARPS, PPL = PARTS / 32;                  // sums of the cluster's warps, per lane
   extern __shared__ __align__(16) uint8_t vf_smem[];
   MassPair* h1 = reinterpret_cast<MassPair*>(vf_smem);                   // [bucket][copy]: this CTA's masses
   uint64_t* t1 = reinterpret_cast<uint64_t*>(h1 + VF_B1 * VF_COPIES);     // [bucket]: the cluster's
-  MassPair* h2 = reinterpret_cast<MassPair*>(t1 + VF_B1);                // of later rounds
-  uint64_t* t2 = reinterpret_cast<uint64_t*>(h2 + VF_B2);                // in turns
+  MassPair* h2 = h1;                                                     // of later rounds
+  uint64_t* t2 = t1 + VF_B1;                                             // in turns
   uint32_t* wt = reinterpret_cast<uint32_t*>(vf_smem + (a.top_p24 < (1u << 24) ? VF_HIST : 0));     // this CTA's weights
   const uint32_t wt_addr = (uint32_t)__cvta_generic_to_shared(wt);
   __shared__ __align__(16) ulonglong2 s_part[2][PARTS];      // what the cluster's warps tell, in turns
@@ -130,10 +127,8 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
 
   int turn = 0, pick = 0;                         // exchanges and selections so far: their shared memory is used in turns
   auto remote = [&](const void* p, int r) { return fa::map_rank((uint32_t)__cvta_generic_to_shared(p), r); };
-  auto warp_sum_u64 = [&](uint64_t v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+  auto warp_sum_u64 = [&](uint64_t v) {           // of numbers below 2^50
+    return (uint64_t)__reduce_add_sync(0xffffffffu, (uint32_t)v & 0xFFFFFFu) + ((uint64_t)__reduce_add_sync(0xffffffffu, (uint32_t)(v >> 24)) << 24);
   };
   // Every warp tells all CTAs two words; every warp learns, in x[i] and y[i] of lane l, those of part i * 32 + l (parts in
   // order of CTA and warp).  One cluster barrier.
@@ -142,7 +137,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     if (lane < C) asm volatile("st.shared::cluster.v2.u64 [%0], {%1, %2};" ::"r"(remote(&s_part[b][rank * VF_WARPS + warp], lane)), "l"(x), "l"(y) : "memory");
     fa::cluster_sync();
 #pragma unroll
-    for (int i = 0; i < PPL; ++i) { const ulonglong2 v = s_part[b][i * 32 + lane]; xs[i] = v.x; ys[i] = v.y; }
+    for (int i = 0; i < PPL; ++i) { const ulonglong2 v = s_part[b][i * 32 + lane]; xs[i] = v.x; ys[i] = v.y; }      // (what is not used is not read)
   };
   auto sum_of = [&](const uint64_t (&xs)[PPL]) {
     uint64_t v = 0;
@@ -163,16 +158,22 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     const int b = nb - 1 - tid, k = pick++ & 1;
     uint64_t m = 0;
     if (b >= 0) { m = total[b]; total[b] = 0; }
-    const uint64_t incl = warp_incl_scan_u64(m, lane);
-    if (lane == 31) s_scan[k][warp] = incl;
+    uint64_t before = 0;
+    const bool busy = warp * 32 < nb;
+    if (busy) {
+      const uint64_t incl = warp_incl_scan_u64(m, lane);
+      if (lane == 31) s_scan[k][warp] = incl;
+      before = incl - m;
+    }
     __syncthreads();
-    const uint64_t before = warp_sum_u64(lane < warp ? s_scan[k][lane & (VF_WARPS - 1)] : 0) + incl - m, run = *above + before;
+    if (busy) before += warp_sum_u64(lane < warp ? s_scan[k][lane & (VF_WARPS - 1)] : 0);
+    const uint64_t run = *above + before;
     if (m > 0 && run + m >= target && (run < target || before == 0)) { s_bin[k] = b; s_found[k][0] = run; s_found[k][1] = m; }
     __syncthreads();
     *above = s_found[k][0]; *at = s_found[k][1];
     return s_bin[k];
   };
-  // Weights below this never decide the nucleus: all of them together are less than what it leaves out (the largest is 2^30).
+  // Weights below this never decide the nucleus: all of them together are at most what it leaves out (the largest is 2^30).
   const uint32_t floor_w = max(1u, (uint32_t)(((uint64_t)((1u << 24) - a.top_p24) << 6) / (uint32_t)V));
 
   if (nucleus) {
@@ -231,13 +232,12 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     // ---- weights, their sum, and the sum of the exponentials (times 2^30) for the log-probability
     uint64_t tot = 0;
     float sume = 0.f;
-    auto put = [&](uint32_t w) {
-      if (w < floor_w) return;
-      MassPair* h = h1 + verify_bucket(w) * VF_COPIES + (lane & (VF_COPIES - 1));
-      atomicAdd(&h->lo, w & 0xFFFFu);
-      if (w >> 16) atomicAdd(&h->hi, w >> 16);
+    const uint32_t h1_addr = (uint32_t)__cvta_generic_to_shared(h1) + (lane & (VF_COPIES - 1)) * 8 - (127 << 3) * (VF_COPIES * 8);
+    auto put = [&](auto exact, float e, uint32_t w) {         // (from 8 on a weight's leading bits are those of its exponential)
+      const uint32_t b = __float_as_uint(exact.value ? __uint2float_rz(w) : e) >> 20;
+      mass_add(h1_addr + b * (VF_COPIES * 8), w, w >= floor_w);
     };
-    auto weigh = [&](auto unit, auto hist) {      // (what does not change within a row is decided outside the loop)
+    auto weigh = [&](auto unit, auto hist, auto exact) {      // (what does not change within a row is decided outside the loop)
       auto e_of = [&](float x) { return verify_exp(radd(unit.value ? x : __fdiv_rn(x, a.temperature), -zmax)); };
       for (int i = w0 + lane * 4; i < w4; i += 128) {
         const float4 y = *reinterpret_cast<const float4*>(wt + i);
@@ -247,24 +247,25 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
         tot += w.x + w.y;                         // (2^31 at most)
         tot += w.z + w.w;
         *reinterpret_cast<uint4*>(wt + i) = w;
-        if (hist.value) { put(w.x); put(w.y); put(w.z); put(w.w); }
+        if (hist.value) { put(exact, e0, w.x); put(exact, e1, w.y); put(exact, e2, w.z); put(exact, e3, w.w); }
       }
       if (w4 + lane < w1) {
         const float e = e_of(__uint_as_float(wt[w4 + lane]));
         const uint32_t w = __float2uint_rz(e);
         sume += e; tot += w; wt[w4 + lane] = w;
-        if (hist.value) put(w);
+        if (hist.value) put(exact, e, w);
       }
     };
     using yes = std::true_type; using no = std::false_type;
     if (!any) {
       for (int i = w0 + lane; i < w1; i += 32) wt[i] = 0;
     } else if (nucleus) {
-      if (unit_T) weigh(yes(), yes()); else weigh(no(), yes());
+      if (floor_w < 8) weigh(no(), yes(), yes());
+      else if (unit_T) weigh(yes(), yes(), no()); else weigh(no(), yes(), no());
     } else if (a.greedy) {                        // a weight of one at the lowest maximum
       int at = INT_MAX;
       for (int i = w0 + lane; i < w1; i += 32) if (__uint_as_float(wt[i]) == top) at = min(at, c0 + i);
-      if (unit_T) weigh(yes(), no()); else weigh(no(), no());
+      if (unit_T) weigh(yes(), no(), no()); else weigh(no(), no(), no());
       tell(__reduce_min_sync(0xffffffffu, at), 0, xs, ys);
       at = INT_MAX;
 #pragma unroll
@@ -273,22 +274,22 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       tot = 0;
       for (int i = w0 + lane; i < w1; i += 32) { wt[i] = i == at; tot += i == at; }
     } else {
-      if (unit_T) weigh(yes(), no()); else weigh(no(), no());
+      if (unit_T) weigh(yes(), no(), no()); else weigh(no(), no(), no());
     }
     uint64_t left = warp_sum_u64(tot);            // what is left in this warp's words, where `sums` says so
     if (nucleus) {
       __syncthreads();                            // the histogram is complete
       if (tid < VF_B1) {
-        MassPair p = {0, 0};                      // (a word sums pieces of 2^18 / 8 weights below 2^16 at most)
+        MassPair p = {0, 0};                      // (a word sums pieces of 2^18 / C weights below 2^16 at most)
 #pragma unroll
         for (int k = 0; k < VF_COPIES; ++k) { const MassPair y = h1[tid * VF_COPIES + ((k + tid) & (VF_COPIES - 1))]; p.lo += y.lo; p.hi += y.hi; }
         spread(t1 + tid, p);
       }
     }
-    // (the warps' sums of exponentials travel as whole multiples of 2^-10 x 2^-30, so that their order plays no part)
-    tell(left, (uint64_t)__float2ull_rn(warp_sum(sume) * 1024.f), xs, ys);
+    // (the warps' sums of exponentials travel as whole multiples of 2^-2 x 2^-30, so that their order plays no part; the sum is 2^30 at least)
+    tell(left, (uint64_t)__float2ull_rn(warp_sum(sume) * 4.f), xs, ys);
     uint64_t mass = sum_of(xs);
-    const float log_total = logf((float)sum_of(ys) * (1.f / 1099511627776.f));
+    const float log_total = logf((float)sum_of(ys) * (1.f / 4294967296.f));
     uint32_t tau = 1;
     if (nucleus && mass) {
       const uint64_t target = mul_shift24(mass, a.top_p24);
@@ -298,29 +299,27 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       const int e = b1 >> 3;
       int rest = max(e - 3, 0);
       uint32_t pre = e >= 3 ? 8u | (b1 & 7) : (8u | (b1 & 7)) >> (3 - e);       // the weight's leading bits so far
+      if (at < (uint64_t)pre << (rest + 1)) { pre = (uint32_t)at; rest = 0; }
       for (int round = 0; rest > 0; ++round) {
         const int bits = min(rest, VF_BITS);
-        h2[tid] = MassPair{0, 0};
-        static_assert(VF_B2 == VF_THREADS, "a bucket per thread");
+        for (int i = tid; i < VF_B2; i += VF_THREADS) h2[i] = MassPair{0, 0};
         __syncthreads();
-        auto add = [&](uint32_t w) {
-          if (w >> rest != pre) return;
-          MassPair* p = h2 + ((w >> (rest - bits)) & ((1u << bits) - 1));
-          atomicAdd(&p->lo, w & 0xFFFFu);
-          if (w >> 16) atomicAdd(&p->hi, w >> 16);
-        };
+        const uint32_t lowest = pre << rest, width = 1u << rest;
+        const uint32_t h2_addr = (uint32_t)__cvta_generic_to_shared(h2);
+        auto add = [&](uint32_t w) { mass_add(h2_addr + ((w - lowest) >> (rest - bits)) * 8, w, w - lowest < width); };
         for (int i = w0 + lane * 4; i < w4; i += 128) {
           const uint4 y = *reinterpret_cast<const uint4*>(wt + i);
-          add(y.x); add(y.y); add(y.z); add(y.w);
+          if (min(min(y.x - lowest, y.y - lowest), min(y.z - lowest, y.w - lowest)) < width) { add(y.x); add(y.y); add(y.z); add(y.w); }
         }
         if (w4 + lane < w1) add(wt[w4 + lane]);
         __syncthreads();
         uint64_t* t = t2 + (round & 1) * VF_B2;
-        spread(t + tid, h2[tid]);
+        for (int i = tid; i < VF_B2; i += VF_THREADS) spread(t + i, h2[i]);
         fa::cluster_sync();
         const int bin = select(t, 1 << bits, target, &above, &at);
         pre = (pre << bits) | bin;
         rest -= bits;
+        if (at < (uint64_t)pre << (rest + 1)) { pre = (uint32_t)at; rest = 0; }      // less than two of the bucket's lowest: one weight
       }
       tau = pre;
       mass = above + at;
@@ -336,9 +335,9 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       const uint64_t d = verify_scaled(prob, m);
       return d < w ? w - (uint32_t)d : 0u;
     };
-    // f(i, x) for this warp's words, four at a time: what is left of words i .. i + 3 after the test with mass m (or all of them, without
-    // q); probabilities are read where something is left to take from.
-    auto each4 = [&](bool test, double m, auto f) {
+    // f(i, x) for this warp's words, four at a time: what is left of words i .. i + 3 after the test with mass m.  Probabilities are
+    // read where there is something to take from.
+    auto each4 = [&](double m, auto f) {
       for (int i0 = w0 + lane * 4; i0 < w1; i0 += 128 * 4) {
         uint4 y[4];
         float4 p[4];
@@ -350,7 +349,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
           y[u] = *reinterpret_cast<const uint4*>(wt + i);                  // (words behind w1 are another warp's, or padding)
           y[u].x = value(y[u].x);
           y[u].y = i + 1 < w1 ? value(y[u].y) : 0u; y[u].z = i + 2 < w1 ? value(y[u].z) : 0u; y[u].w = i + 3 < w1 ? value(y[u].w) : 0u;
-          if (!test || !(y[u].x | y[u].y | y[u].z | y[u].w)) continue;
+          if (!(y[u].x | y[u].y | y[u].z | y[u].w)) continue;
           if (vec_q && i + 3 < w1) p[u] = *reinterpret_cast<const float4*>(q + c0 + i);
           else { p[u].x = q[c0 + i]; if (y[u].y) p[u].y = q[c0 + i + 1]; if (y[u].z) p[u].z = q[c0 + i + 2]; if (y[u].w) p[u].w = q[c0 + i + 3]; }
         }
@@ -358,12 +357,10 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
         for (int u = 0; u < 4; ++u) {
           const int i = i0 + 128 * u;
           if (i >= w1) continue;
-          if (test) {
-            if (y[u].x) y[u].x = less(y[u].x, p[u].x, m);
-            if (y[u].y) y[u].y = less(y[u].y, p[u].y, m);
-            if (y[u].z) y[u].z = less(y[u].z, p[u].z, m);
-            if (y[u].w) y[u].w = less(y[u].w, p[u].w, m);
-          }
+          if (y[u].x) y[u].x = less(y[u].x, p[u].x, m);
+          if (y[u].y) y[u].y = less(y[u].y, p[u].y, m);
+          if (y[u].z) y[u].z = less(y[u].z, p[u].z, m);
+          if (y[u].w) y[u].w = less(y[u].w, p[u].w, m);
           f(i, y[u]);
         }
       }
@@ -376,7 +373,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     };
     for (; child >= 0; child = child_behind(child)) {
       if (lazy) {                                 // make what the last test left the weights (nobody reads them for that test any more)
-        each4(true, lazy_mass, [&](int i, const uint4& y) {
+        each4(lazy_mass, [&](int i, const uint4& y) {
           if (i + 3 < w1) *reinterpret_cast<uint4*>(wt + i) = y;
           else { wt[i] = y.x; if (i + 1 < w1) wt[i + 1] = y.y; if (i + 2 < w1) wt[i + 2] = y.z; }
         });
@@ -404,7 +401,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       } else {
         const double m = (double)mass;
         uint64_t rest = 0;
-        each4(true, m, [&](int, const uint4& y) { rest += (uint64_t)y.x + y.y + y.z + y.w; });
+        each4(m, [&](int, const uint4& y) { rest += (uint64_t)y.x + y.y + y.z + y.w; });
         rest = warp_sum_u64(rest);
         tell(rest, 0, xs, ys);
         const uint64_t all = sum_of(xs);
@@ -421,8 +418,13 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       };
       if (!sums) {
         if (refused) { fa::cluster_sync(); drop_refused(); refused = false; }
-        left = 0;
-        each4(lazy, lazy_mass, [&](int, const uint4& y) { left += (uint64_t)y.x + y.y + y.z + y.w; });
+        left = 0;                                 // (nothing was taken lazily: then the sums are known)
+        for (int i = w0 + lane * 4; i < w4; i += 128) {
+          const uint4 y = *reinterpret_cast<const uint4*>(wt + i);
+          left += value(y.x) + value(y.y);
+          left += value(y.z) + value(y.w);
+        }
+        if (w4 + lane < w1) left += value(wt[w4 + lane]);
         left = warp_sum_u64(left);
       }
       tell(left, 0, xs, ys);
