@@ -34,9 +34,10 @@ struct VerifyArgs {
   int* status;
 };
 
-constexpr int VF_THREADS = 512, VF_WARPS = VF_THREADS / 32;
-constexpr int VF_B1 = 256, VF_COPIES = 4, VF_B2 = 512, VF_BITS = 9;
-constexpr int VF_HIST = VF_B1 * VF_COPIES * 8 + VF_B1 * 8 + 2 * VF_B2 * 8;      // with the weights of 2^17 tokens and more two CTAs fit an SM
+constexpr int VF_THREADS = 256, VF_WARPS = VF_THREADS / 32;
+constexpr int VF_B1 = 256, VF_COPIES = 4, VF_B2 = 512, VF_BITS = 9, VF_COLUMN = 8, VF_KEPT = VF_COLUMN * 32;
+// With the weights of 2^17 tokens and more two CTAs still fit an SM.
+constexpr int VF_HIST = VF_B1 * VF_COPIES * 8 + VF_B1 * 8 + 2 * VF_B2 * 8 + VF_WARPS * VF_KEPT * 4;
 constexpr int VF_NODES = 256;                     // what concerns so many nodes is gathered in shared memory at the start
 
 struct MassPair { uint32_t lo, hi; };             // sums of the lower 16 bits and of the others
@@ -46,10 +47,9 @@ __device__ __forceinline__ uint32_t verify_u24(float u) {
   return u > 0.f ? min(__float2uint_rz(u * 16777216.f), (1u << 24) - 1) : 0u;
 }
 
-// floor(q A), 0 for what is no probability.
-__device__ __forceinline__ uint64_t verify_scaled(float q, double mass) {
-  return q > 0.f ? (uint64_t)__double2ull_rz(fmin(__dmul_rn((double)q, mass), 4.0e18)) : 0ull;
-}
+// q A of a probability, 0 for what is none; its whole part is what a test takes (2^62 at most: more than any weight, whatever it
+// is multiplied by).
+__device__ __forceinline__ double verify_scaled(float q, double mass) { return __dmul_rn((double)(q > 0.f ? fminf(q, 16384.f) : 0.f), mass); }
 
 // exp_nonpos(x) 2^30 with the same roundings in fewer instructions: rint by adding 1.5 x 2^23 (and 30), whose low bits then are the
 // exponent that the polynomial's result is raised by.  Numbers below -40 count as -40: between there and -24 the sampler's
@@ -71,12 +71,6 @@ __device__ __forceinline__ float verify_exp(float x) {
   return __uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23));
 }
 
-// Adds a weight to a bucket where `in` says so, without a branch.
-__device__ __forceinline__ void mass_add(uint32_t addr, uint32_t w, bool in) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %3, 0;\n @p red.shared.add.u32 [%0], %1;\n @p red.shared.add.u32 [%0 + 4], %2;\n}"
-               ::"r"(addr), "r"(w & 0xFFFFu), "r"(w >> 16), "r"((uint32_t)in) : "memory");
-}
-
 template <int C>
 __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
   constexpr int PARTS = C * VF_WARPS, PPL = PARTS / 32;                  // sums of the cluster's warps, per lane
@@ -85,6 +79,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
   uint64_t* t1 = reinterpret_cast<uint64_t*>(h1 + VF_B1 * VF_COPIES);     // [bucket]: the cluster's
   MassPair* h2 = h1;                                                     // of later rounds
   uint64_t* t2 = t1 + VF_B1;                                             // in turns
+  uint32_t* s_list = reinterpret_cast<uint32_t*>(t2 + 2 * VF_B2) + (threadIdx.x >> 5) * VF_KEPT;       // the warp's: columns of weights on their way into a histogram, then the kept words' places
   uint32_t* wt = reinterpret_cast<uint32_t*>(vf_smem + (a.top_p24 < (1u << 24) ? VF_HIST : 0));     // this CTA's weights
   const uint32_t wt_addr = (uint32_t)__cvta_generic_to_shared(wt);
   __shared__ __align__(16) ulonglong2 s_part[2][PARTS];      // what the cluster's warps tell, in turns
@@ -93,8 +88,10 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
   __shared__ VerifyNode s_node[VF_NODES];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x % C, s = blockIdx.x / C, V = a.V;
   const int c0 = min(V, rank * a.slice), n = min(V, c0 + a.slice) - c0;   // my words [c0, c0 + n)
-  const int chunk = ((a.slice + VF_WARPS - 1) / VF_WARPS + 3) & ~3;       // of a warp
+  const int strip = ((a.slice + VF_THREADS * 4 - 1) / (VF_THREADS * 4) | 1) * 4;      // of a lane: an odd number of 16-byte words (no bank conflicts)
+  const int chunk = strip * 32;                   // of a warp
   const int w0 = min(n, warp * chunk), w1 = min(n, w0 + chunk), w4 = w0 + (w1 - w0) / 4 * 4;
+  const int l0 = w0 + lane * strip, l1 = w0 < w1 ? min(l0 + strip, (w1 + 3) & ~3) : l0;      // of this lane, where its words are to be consecutive
   int32_t* path = a.path + (int64_t)s * a.max_path;
   float* logp = a.logprobs ? a.logprobs + (int64_t)s * a.max_path : nullptr;
 
@@ -152,29 +149,66 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
 #pragma unroll
     for (int r = 0; r < C; ++r) asm volatile("red.relaxed.cluster.shared::cluster.add.u64 [%0], %1;" ::"r"(remote(total, r)), "l"(m) : "memory");
   };
-  // Among nb <= VF_THREADS buckets of masses total[b]: the highest with *above + (mass of the buckets from it on) >= target (the
+  // Among nb <= VF_B2 buckets of masses total[b]: the highest with *above + (mass of the buckets from it on) >= target (the
   // highest that is not empty, for a target of 0).  *above grows by the mass above it.  Leaves zeros behind.
   auto select = [&](uint64_t* total, int nb, uint64_t target, uint64_t* above, uint64_t* at) {
-    const int b = nb - 1 - tid, k = pick++ & 1;
-    uint64_t m = 0;
-    if (b >= 0) { m = total[b]; total[b] = 0; }
-    uint64_t before = 0;
-    const bool busy = warp * 32 < nb;
+    constexpr int K = VF_B2 / VF_THREADS;
+    const int b0 = nb - 1 - tid * K, k = pick++ & 1;
+    uint64_t m[K], sum = 0, before = 0;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      m[i] = 0;
+      if (b0 - i >= 0) { m[i] = total[b0 - i]; total[b0 - i] = 0; }
+      sum += m[i];
+    }
+    const bool busy = warp * 32 * K < nb;
     if (busy) {
-      const uint64_t incl = warp_incl_scan_u64(m, lane);
+      const uint64_t incl = warp_incl_scan_u64(sum, lane);
       if (lane == 31) s_scan[k][warp] = incl;
-      before = incl - m;
+      before = incl - sum;
     }
     __syncthreads();
-    if (busy) before += warp_sum_u64(lane < warp ? s_scan[k][lane & (VF_WARPS - 1)] : 0);
-    const uint64_t run = *above + before;
-    if (m > 0 && run + m >= target && (run < target || before == 0)) { s_bin[k] = b; s_found[k][0] = run; s_found[k][1] = m; }
+    if (busy) {
+      before += warp_sum_u64(lane < warp ? s_scan[k][lane & (VF_WARPS - 1)] : 0);
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const uint64_t run = *above + before;
+        if (m[i] > 0 && run + m[i] >= target && (run < target || before == 0)) { s_bin[k] = b0 - i; s_found[k][0] = run; s_found[k][1] = m[i]; }
+        before += m[i];
+      }
+    }
     __syncthreads();
     *above = s_found[k][0]; *at = s_found[k][1];
     return s_bin[k];
   };
-  // Weights below this never decide the nucleus: all of them together are at most what it leaves out (the largest is 2^30).
-  const uint32_t floor_w = max(1u, (uint32_t)(((uint64_t)((1u << 24) - a.top_p24) << 6) / (uint32_t)V));
+  // A lane's column: appends x where w - lo < width, without a branch.
+  const uint32_t column = (uint32_t)__cvta_generic_to_shared(s_list + lane), column_end = column + VF_COLUMN * 128;
+  auto append = [&](uint32_t& at, uint32_t w, uint32_t lo, uint32_t width, uint32_t x) {
+    asm volatile("{\n .reg .pred p;\n setp.lt.u32 p, %1, %2;\n @p st.shared.u32 [%0], %3;\n @p add.u32 %0, %0, 128;\n}" : "+r"(at) : "r"(w - lo), "r"(width), "r"(x) : "memory");
+  };
+  // Adds the words of this warp with lo <= w < lo + width to the buckets that bucket(w) gives.  Few words qualify, and a histogram's
+  // additions cost a warp the same for one lane as for 32: each lane collects its own first.
+  auto histogram = [&](uint32_t lo, uint32_t width, auto bucket) {
+    uint32_t at = column;
+    auto drain = [&]() {
+      const int most = __reduce_max_sync(0xffffffffu, (at - column) >> 7);
+      for (int j = 0; j < most; ++j)
+        if (column + j * 128 < at) {
+          const uint32_t w = s_list[j * 32 + lane];
+          MassPair* p = bucket(w);
+          atomicAdd(&p->lo, w & 0xFFFFu);
+          atomicAdd(&p->hi, w >> 16);
+        }
+      at = column;
+    };
+#pragma unroll 4
+    for (int k = 0; k < strip; k += 4) {
+      const uint4 y = l0 + k < l1 ? *reinterpret_cast<const uint4*>(wt + l0 + k) : make_uint4(0, 0, 0, 0);
+      append(at, y.x, lo, width, y.x); append(at, y.y, lo, width, y.y); append(at, y.z, lo, width, y.z); append(at, y.w, lo, width, y.w);
+      if (__any_sync(0xffffffffu, at > column_end - 4 * 128)) drain();
+    }
+    drain();
+  };
 
   if (nucleus) {
     for (int i = tid; i < VF_B1; i += VF_THREADS) t1[i] = 0;
@@ -202,7 +236,6 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     int child = count + 1 < a.max_path ? child_behind(cur) : -1;
     // ---- the row's logits are in shared memory: their maximum
     const float* row = a.logits + (int64_t)(row0 + cur) * a.logits_stride;
-    if (nucleus) for (int i = tid; i < VF_B1 * VF_COPIES; i += VF_THREADS) h1[i] = MassPair{0, 0};
     fa::cp_wait<0>();
     __syncwarp();
     if (child >= 0)
@@ -232,12 +265,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     // ---- weights, their sum, and the sum of the exponentials (times 2^30) for the log-probability
     uint64_t tot = 0;
     float sume = 0.f;
-    const uint32_t h1_addr = (uint32_t)__cvta_generic_to_shared(h1) + (lane & (VF_COPIES - 1)) * 8 - (127 << 3) * (VF_COPIES * 8);
-    auto put = [&](auto exact, float e, uint32_t w) {         // (from 8 on a weight's leading bits are those of its exponential)
-      const uint32_t b = __float_as_uint(exact.value ? __uint2float_rz(w) : e) >> 20;
-      mass_add(h1_addr + b * (VF_COPIES * 8), w, w >= floor_w);
-    };
-    auto weigh = [&](auto unit, auto hist, auto exact) {      // (what does not change within a row is decided outside the loop)
+    auto weigh = [&](auto unit) {      // (what does not change within a row is decided outside the loop)
       auto e_of = [&](float x) { return verify_exp(radd(unit.value ? x : __fdiv_rn(x, a.temperature), -zmax)); };
       for (int i = w0 + lane * 4; i < w4; i += 128) {
         const float4 y = *reinterpret_cast<const float4*>(wt + i);
@@ -247,25 +275,19 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
         tot += w.x + w.y;                         // (2^31 at most)
         tot += w.z + w.w;
         *reinterpret_cast<uint4*>(wt + i) = w;
-        if (hist.value) { put(exact, e0, w.x); put(exact, e1, w.y); put(exact, e2, w.z); put(exact, e3, w.w); }
       }
       if (w4 + lane < w1) {
         const float e = e_of(__uint_as_float(wt[w4 + lane]));
         const uint32_t w = __float2uint_rz(e);
         sume += e; tot += w; wt[w4 + lane] = w;
-        if (hist.value) put(exact, e, w);
       }
     };
-    using yes = std::true_type; using no = std::false_type;
     if (!any) {
       for (int i = w0 + lane; i < w1; i += 32) wt[i] = 0;
-    } else if (nucleus) {
-      if (floor_w < 8) weigh(no(), yes(), yes());
-      else if (unit_T) weigh(yes(), yes(), no()); else weigh(no(), yes(), no());
     } else if (a.greedy) {                        // a weight of one at the lowest maximum
       int at = INT_MAX;
       for (int i = w0 + lane; i < w1; i += 32) if (__uint_as_float(wt[i]) == top) at = min(at, c0 + i);
-      if (unit_T) weigh(yes(), no(), no()); else weigh(no(), no(), no());
+      if (unit_T) weigh(std::true_type()); else weigh(std::false_type());
       tell(__reduce_min_sync(0xffffffffu, at), 0, xs, ys);
       at = INT_MAX;
 #pragma unroll
@@ -274,44 +296,48 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       tot = 0;
       for (int i = w0 + lane; i < w1; i += 32) { wt[i] = i == at; tot += i == at; }
     } else {
-      if (unit_T) weigh(yes(), no(), no()); else weigh(no(), no(), no());
+      if (unit_T) weigh(std::true_type()); else weigh(std::false_type());
     }
-    uint64_t left = warp_sum_u64(tot);            // what is left in this warp's words, where `sums` says so
-    if (nucleus) {
-      __syncthreads();                            // the histogram is complete
-      if (tid < VF_B1) {
-        MassPair p = {0, 0};                      // (a word sums pieces of 2^18 / C weights below 2^16 at most)
-#pragma unroll
-        for (int k = 0; k < VF_COPIES; ++k) { const MassPair y = h1[tid * VF_COPIES + ((k + tid) & (VF_COPIES - 1))]; p.lo += y.lo; p.hi += y.hi; }
-        spread(t1 + tid, p);
-      }
-    }
+    if (w1 == n && lane < 3 && w1 + lane < ((w1 + 3) & ~3)) wt[w1 + lane] = 0;      // (padding)
+    uint64_t left = warp_sum_u64(tot);            // what is left in this warp's words
     // (the warps' sums of exponentials travel as whole multiples of 2^-2 x 2^-30, so that their order plays no part; the sum is 2^30 at least)
     tell(left, (uint64_t)__float2ull_rn(warp_sum(sume) * 4.f), xs, ys);
     uint64_t mass = sum_of(xs);
     const float log_total = logf((float)sum_of(ys) * (1.f / 4294967296.f));
+    // ---- the nucleus: the least weight in it and its mass (found when something depends on it)
     uint32_t tau = 1;
-    if (nucleus && mass) {
-      const uint64_t target = mul_shift24(mass, a.top_p24);
+    bool whole = !nucleus || mass == 0;           // weights and mass are the nucleus's
+    const uint64_t target = mul_shift24(mass, a.top_p24);
+    int n_kept = -1;                              // words of this lane in the nucleus, listed in order; -1 in all lanes: any may hold something
+    auto find_nucleus = [&]() {
+      // Weights below this never decide it: all of them together are at most what it leaves out.
+      const uint32_t least = max((uint32_t)((mass - target) / (uint32_t)V), 1u);
+      for (int i = tid; i < VF_B1 * VF_COPIES; i += VF_THREADS) h1[i] = MassPair{0, 0};
+      __syncthreads();
+      // (a weight's leading bits are those of its float, rounded down)
+      histogram(least, (1u << 30) + 1 - least, [&](uint32_t w) { return h1 + ((__float_as_uint(__uint2float_rz(w)) >> 20) - (127 << 3)) * VF_COPIES + (lane & (VF_COPIES - 1)); });
+      __syncthreads();
+      for (int i = tid; i < VF_B1; i += VF_THREADS) {
+        MassPair p = {0, 0};                      // (a word sums pieces of 2^18 / C weights below 2^16 at most)
+#pragma unroll
+        for (int k = 0; k < VF_COPIES; ++k) { const MassPair y = h1[i * VF_COPIES + ((k + i) & (VF_COPIES - 1))]; p.lo += y.lo; p.hi += y.hi; }
+        spread(t1 + i, p);
+      }
+      fa::cluster_sync();
       uint64_t above = 0, at = 0;
       const int b1 = select(t1, VF_B1, target, &above, &at);
       // b1: exponent e and three bits; the bits below in steps of nine
       const int e = b1 >> 3;
       int rest = max(e - 3, 0);
       uint32_t pre = e >= 3 ? 8u | (b1 & 7) : (8u | (b1 & 7)) >> (3 - e);       // the weight's leading bits so far
-      if (at < (uint64_t)pre << (rest + 1)) { pre = (uint32_t)at; rest = 0; }
-      for (int round = 0; rest > 0; ++round) {
+      for (int round = 0; ; ++round) {
+        if (at < (uint64_t)pre << (rest + 1)) { pre = (uint32_t)at; rest = 0; }      // less than two of the bucket's lowest: one weight
+        if (rest == 0) break;
         const int bits = min(rest, VF_BITS);
         for (int i = tid; i < VF_B2; i += VF_THREADS) h2[i] = MassPair{0, 0};
         __syncthreads();
-        const uint32_t lowest = pre << rest, width = 1u << rest;
-        const uint32_t h2_addr = (uint32_t)__cvta_generic_to_shared(h2);
-        auto add = [&](uint32_t w) { mass_add(h2_addr + ((w - lowest) >> (rest - bits)) * 8, w, w - lowest < width); };
-        for (int i = w0 + lane * 4; i < w4; i += 128) {
-          const uint4 y = *reinterpret_cast<const uint4*>(wt + i);
-          if (min(min(y.x - lowest, y.y - lowest), min(y.z - lowest, y.w - lowest)) < width) { add(y.x); add(y.y); add(y.z); add(y.w); }
-        }
-        if (w4 + lane < w1) add(wt[w4 + lane]);
+        const uint32_t lowest = pre << rest;
+        histogram(lowest, 1u << rest, [&](uint32_t w) { return h2 + ((w - lowest) >> (rest - bits)); });
         __syncthreads();
         uint64_t* t = t2 + (round & 1) * VF_B2;
         for (int i = tid; i < VF_B2; i += VF_THREADS) spread(t + i, h2[i]);
@@ -319,116 +345,139 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
         const int bin = select(t, 1 << bits, target, &above, &at);
         pre = (pre << bits) | bin;
         rest -= bits;
-        if (at < (uint64_t)pre << (rest + 1)) { pre = (uint32_t)at; rest = 0; }      // less than two of the bucket's lowest: one weight
       }
       tau = pre;
       mass = above + at;
-    }
+      whole = true;
+      // What is outside becomes 0; few words stay, as a rule: where they are, lane by lane.  (Nobody reads these weights before the
+      // next cluster barrier.)
+      left = 0;
+      uint32_t at_word = column;
+      bool full = false;
+#pragma unroll 4
+      for (int i = l0; i < l1; i += 4) {
+        uint4 y = *reinterpret_cast<const uint4*>(wt + i);
+        full = full || at_word > column_end - 4 * 128;
+        if (full) at_word = column;
+        append(at_word, y.x, tau, 0x80000000u, i); append(at_word, y.y, tau, 0x80000000u, i + 1);
+        append(at_word, y.z, tau, 0x80000000u, i + 2); append(at_word, y.w, tau, 0x80000000u, i + 3);
+        y.x = y.x >= tau ? y.x : 0u; y.y = y.y >= tau ? y.y : 0u; y.z = y.z >= tau ? y.z : 0u; y.w = y.w >= tau ? y.w : 0u;
+        left += y.x + y.y;
+        left += y.z + y.w;
+        *reinterpret_cast<uint4*>(wt + i) = y;
+      }
+      left = warp_sum_u64(left);
+      n_kept = __any_sync(0xffffffffu, full) ? -1 : (int)((at_word - column) >> 7);
+      __syncwarp();
+    };
     // ---- children (every warp by itself, all with the same result)
     int accepted = -1;
     float accepted_logit = 0.f;
-    bool lazy = false, sums = !nucleus;           // lazy: a - d with the last test's mass is what is left
+    bool lazy = false;                            // a - d with the last test's mass is what is left
     double lazy_mass = 0;
-    auto value = [&](uint32_t w) -> uint32_t { return w >= tau ? w : 0u; };
     const float* q = a.probs ? a.probs + (int64_t)(row0 + cur) * a.probs_stride : nullptr;
     auto less = [&](uint32_t w, float prob, double m) -> uint32_t {
-      const uint64_t d = verify_scaled(prob, m);
-      return d < w ? w - (uint32_t)d : 0u;
+      const uint32_t d = __double2uint_rz(verify_scaled(prob, m));         // (the largest number, for more)
+      return w > d ? w - d : 0u;
     };
-    // f(i, x) for this warp's words, four at a time: what is left of words i .. i + 3 after the test with mass m.  Probabilities are
-    // read where there is something to take from.
-    auto each4 = [&](double m, auto f) {
-      for (int i0 = w0 + lane * 4; i0 < w1; i0 += 128 * 4) {
-        uint4 y[4];
-        float4 p[4];
+    // What the test with mass m leaves of this warp's words, their sum; `store` puts it in their places.
+    auto take = [&](double m, bool store) {
+      uint64_t sum = 0;
+      if (n_kept >= 0) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int j = 0; j < VF_COLUMN; j += 4) {
+          if (!__any_sync(0xffffffffu, j < n_kept)) break;
+          int at[4];
+          float prob[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) { at[k] = j + k < n_kept ? s_list[(j + k) * 32 + lane] : -1; prob[k] = at[k] >= 0 ? q[c0 + at[k]] : 0.f; }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (at[k] < 0) continue;
+            const uint32_t x = less(wt[at[k]], prob[k], m);
+            sum += x;
+            if (store) wt[at[k]] = x;
+          }
+        }
+        return warp_sum_u64(sum);
+      }
+      constexpr int U = 4;
+      for (int i0 = w0 + lane * 4; i0 < w4; i0 += 128 * U) {
+        float4 p[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
           const int i = i0 + 128 * u;
-          y[u] = make_uint4(0, 0, 0, 0); p[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (i >= w1) continue;
-          y[u] = *reinterpret_cast<const uint4*>(wt + i);                  // (words behind w1 are another warp's, or padding)
-          y[u].x = value(y[u].x);
-          y[u].y = i + 1 < w1 ? value(y[u].y) : 0u; y[u].z = i + 2 < w1 ? value(y[u].z) : 0u; y[u].w = i + 3 < w1 ? value(y[u].w) : 0u;
-          if (!(y[u].x | y[u].y | y[u].z | y[u].w)) continue;
-          if (vec_q && i + 3 < w1) p[u] = *reinterpret_cast<const float4*>(q + c0 + i);
-          else { p[u].x = q[c0 + i]; if (y[u].y) p[u].y = q[c0 + i + 1]; if (y[u].z) p[u].z = q[c0 + i + 2]; if (y[u].w) p[u].w = q[c0 + i + 3]; }
+          if (i >= w4) p[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          else if (vec_q) p[u] = *reinterpret_cast<const float4*>(q + c0 + i);
+          else p[u] = make_float4(q[c0 + i], q[c0 + i + 1], q[c0 + i + 2], q[c0 + i + 3]);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
           const int i = i0 + 128 * u;
-          if (i >= w1) continue;
-          if (y[u].x) y[u].x = less(y[u].x, p[u].x, m);
-          if (y[u].y) y[u].y = less(y[u].y, p[u].y, m);
-          if (y[u].z) y[u].z = less(y[u].z, p[u].z, m);
-          if (y[u].w) y[u].w = less(y[u].w, p[u].w, m);
-          f(i, y[u]);
+          if (i >= w4) continue;
+          uint4 y = *reinterpret_cast<const uint4*>(wt + i);
+          y.x = less(y.x, p[u].x, m); y.y = less(y.y, p[u].y, m); y.z = less(y.z, p[u].z, m); y.w = less(y.w, p[u].w, m);
+          sum += y.x + y.y;
+          sum += y.z + y.w;
+          if (store) *reinterpret_cast<uint4*>(wt + i) = y;
         }
       }
+      if (w4 + lane < w1) {
+        const uint32_t x = less(wt[w4 + lane], q[c0 + w4 + lane], m);
+        sum += x;
+        if (store) wt[w4 + lane] = x;
+      }
+      return warp_sum_u64(sum);
     };
     bool refused = false;                         // drafts without probabilities: some child was refused
+    bool written = false;                         // weights were written since the last cluster barrier
     auto same_before = [&](int child, int x) {    // has an earlier child the same token?
       bool again = false;
       for (int j = cur + 1; j < child; j += 32) again = again || __any_sync(0xffffffffu, j + lane < child && parent_of(j + lane) == cur && token_of(j + lane) == x);
       return again;
     };
     for (; child >= 0; child = child_behind(child)) {
-      if (lazy) {                                 // make what the last test left the weights (nobody reads them for that test any more)
-        each4(lazy_mass, [&](int i, const uint4& y) {
-          if (i + 3 < w1) *reinterpret_cast<uint4*>(wt + i) = y;
-          else { wt[i] = y.x; if (i + 1 < w1) wt[i + 1] = y.y; if (i + 2 < w1) wt[i + 2] = y.z; }
-        });
-        tau = 1; lazy = false;
-        fa::cluster_sync();
-      }
+      if (lazy) { take(lazy_mass, true); lazy = false; written = true; }   // (nobody reads them for that test any more)
+      if (written) { fa::cluster_sync(); written = false; }
       const VerifyNode v = child < VF_NODES ? s_node[child] : gather(child);
       const bool in = v.token >= 0 && v.token < V;
       if (!in && tid == 0) atomicOr(a.status, STATUS_BAD_TOKEN);
-      uint64_t w = 0;
-      if (in) {
-        uint32_t y;
-        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(y) : "r"(remote(wt + v.token % a.slice, v.token / a.slice)) : "memory");
-        w = value(y);
+      uint32_t w = 0;
+      if (in) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(w) : "r"(remote(wt + v.token % a.slice, v.token / a.slice)) : "memory");
+      auto passes = [&]() { return mul_shift24(q ? __double2ull_rz(verify_scaled(v.q, (double)mass)) : mass, v.u24) < w; };
+      if (!whole) {
+        // The nucleus's mass lies between target and the row's, and what weighs more than all that it leaves out is in it: a first
+        // child that would be accepted at the row's mass is accepted at the nucleus's.
+        if (w > mass - target && passes()) { accepted = child; accepted_logit = v.logit; break; }
+        find_nucleus();
+        written = true;
+        if (w < tau) w = 0;
       }
       if (!q && same_before(child, v.token)) w = 0;                        // a token that was refused before has nothing left
-      if (mul_shift24(q ? verify_scaled(v.q, (double)mass) : mass, v.u24) < w) { accepted = child; accepted_logit = v.logit; break; }
+      if (passes()) { accepted = child; accepted_logit = v.logit; break; }
       if (!q) {
-        if (w < mass) {                           // (all of it is never refused)
-          mass -= w;
-          const int i = v.token - c0;
-          if (w && i >= w0 && i < w1) left -= w;  // (zeroed below)
-        }
+        mass -= w;                                // (all of it is never refused)
+        const int i = v.token - c0;
+        if (w && i >= w0 && i < w1) left -= w;    // (zeroed below)
         refused = true;
       } else {
         const double m = (double)mass;
-        uint64_t rest = 0;
-        each4(m, [&](int, const uint4& y) { rest += (uint64_t)y.x + y.y + y.z + y.w; });
-        rest = warp_sum_u64(rest);
-        tell(rest, 0, xs, ys);
+        const uint64_t part = take(m, false);
+        tell(part, 0, xs, ys);
+        written = false;
         const uint64_t all = sum_of(xs);
-        if (all) { mass = all; lazy = true; lazy_mass = m; left = rest; sums = true; }
-        else sums = false;
+        if (all) { mass = all; lazy = true; lazy_mass = m; left = part; }
       }
     }
     // ---- without an accepted child: the next token
+    if (accepted < 0 && !whole) find_nucleus();
     if (accepted < 0 && mass) {
-      auto drop_refused = [&]() {                 // this warp's words of refused tokens, once nobody reads them any more
+      tell(left, 0, xs, ys);
+      if (refused) {                              // this warp's words of refused tokens, which nobody reads any more
         for (int j = cur + 1 + lane; j < rows; j += 32)
           if (parent_of(j) == cur) { const int x = token_of(j) - c0; if (x >= w0 && x < w1) wt[x] = 0; }
         __syncwarp();
-      };
-      if (!sums) {
-        if (refused) { fa::cluster_sync(); drop_refused(); refused = false; }
-        left = 0;                                 // (nothing was taken lazily: then the sums are known)
-        for (int i = w0 + lane * 4; i < w4; i += 128) {
-          const uint4 y = *reinterpret_cast<const uint4*>(wt + i);
-          left += value(y.x) + value(y.y);
-          left += value(y.z) + value(y.w);
-        }
-        if (w4 + lane < w1) left += value(wt[w4 + lane]);
-        left = warp_sum_u64(left);
       }
-      tell(left, 0, xs, ys);
-      if (refused) drop_refused();
       // mass in the parts before mine
       const uint64_t r = mul_shift24(mass, rows <= VF_NODES ? s_node[0].u24 : verify_u24(a.uniform[row0]));
       uint64_t base = 0;
@@ -436,30 +485,38 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       for (int i = 0; i < PPL; ++i) base += i * 32 + lane < rank * VF_WARPS + warp ? xs[i] : 0;
       base = warp_sum_u64(base);
       if (r >= base && r < base + left) {         // one warp of the cluster
-        for (int i = w0; i < w1; i += 128) {
-          uint32_t x[4];
+        auto at = [&](int j, uint32_t w) { return lazy && w ? less(w, q[c0 + j], lazy_mass) : w; };
+        auto found = [&](int j) {
+          const int tok = c0 + j;
+          a.next[s] = tok;
+          if (logp) logp[count] = radd(scaled(row[tok]), -zmax) - log_total;
+        };
+        if (n_kept >= 0) {
           uint64_t sum = 0;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int j = i + lane * 4 + k;
-            x[k] = j < w1 ? value(wt[j]) : 0u;
-            if (lazy && x[k]) x[k] = less(x[k], q[c0 + j], lazy_mass);
-            sum += x[k];
-          }
-          const uint64_t incl = warp_incl_scan_u64(sum, lane);
-          const unsigned hit = __ballot_sync(0xffffffffu, base + incl > r);
-          if (hit) {
-            if (lane == __ffs(hit) - 1) {
-              uint64_t run = base + incl - sum;
-              int tok = c0 + i + lane * 4;
-#pragma unroll
-              for (int k = 0; k < 3; ++k) { run += x[k]; if (run <= r) ++tok; else run = ~0ull >> 1; }
-              a.next[s] = tok;
-              if (logp) logp[count] = radd(scaled(row[tok]), -zmax) - log_total;
+          for (int j = 0; j < n_kept; ++j) { const int i = s_list[j * 32 + lane]; sum += at(i, wt[i]); }
+          uint64_t run = base + warp_incl_scan_u64(sum, lane) - sum;
+          if (r >= run && r < run + sum)
+            for (int j = 0; j < n_kept; ++j) {
+              const int i = s_list[j * 32 + lane];
+              run += at(i, wt[i]);
+              if (run > r) { found(i); break; }
             }
+        } else {
+          for (int i = w0; i < w1; i += 128) {
+            uint32_t x[4];
+            uint64_t sum = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { const int j = i + lane * 4 + k; x[k] = j < w1 ? at(j, wt[j]) : 0u; sum += x[k]; }
+            const uint64_t all = warp_sum_u64(sum);
+            if (base + all <= r) { base += all; continue; }
+            uint64_t run = base + warp_incl_scan_u64(sum, lane) - sum;
+            int tok = -1;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { run += x[k]; if (tok < 0 && run > r) tok = i + lane * 4 + k; }
+            const unsigned hit = __ballot_sync(0xffffffffu, tok >= 0);
+            if (lane == __ffs(hit) - 1) found(tok);
             break;
           }
-          base += __shfl_sync(0xffffffffu, incl, 31);
         }
       }
       next = 0;                                   // written above
