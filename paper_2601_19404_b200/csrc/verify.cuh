@@ -35,10 +35,10 @@ struct VerifyArgs {
 };
 
 constexpr int VF_THREADS = 256, VF_WARPS = VF_THREADS / 32;
-constexpr int VF_B1 = 256, VF_COPIES = 4, VF_B2 = 512, VF_BITS = 9, VF_COLUMN = 8, VF_KEPT = VF_COLUMN * 32;
+constexpr int VF_B1 = 256, VF_COPIES = 4, VF_B2 = 512, VF_BITS = 9, VF_COLUMN = 12, VF_KEPT = VF_COLUMN * 32;
 // With the weights of 2^17 tokens and more two CTAs still fit an SM.
 constexpr int VF_HIST = VF_B1 * VF_COPIES * 8 + VF_B1 * 8 + 2 * VF_B2 * 8 + VF_WARPS * VF_KEPT * 4;
-constexpr int VF_NODES = 256;                     // what concerns so many nodes is gathered in shared memory at the start
+constexpr int VF_NODES = 128;                     // what concerns so many nodes is gathered in shared memory at the start
 
 struct MassPair { uint32_t lo, hi; };             // sums of the lower 16 bits and of the others
 struct VerifyNode { int parent, token; uint32_t u24; float q, logit; };       // q, logit: of its token, in its parent's rows
@@ -181,11 +181,12 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     *above = s_found[k][0]; *at = s_found[k][1];
     return s_bin[k];
   };
-  // A lane's column: appends x where w - lo < width, without a branch.
+  // A lane's column: appends x where w - lo < width, without a branch.  (Reads of the column are volatile, too: they stay behind.)
   const uint32_t column = (uint32_t)__cvta_generic_to_shared(s_list + lane), column_end = column + VF_COLUMN * 128;
   auto append = [&](uint32_t& at, uint32_t w, uint32_t lo, uint32_t width, uint32_t x) {
-    asm volatile("{\n .reg .pred p;\n setp.lt.u32 p, %1, %2;\n @p st.shared.u32 [%0], %3;\n @p add.u32 %0, %0, 128;\n}" : "+r"(at) : "r"(w - lo), "r"(width), "r"(x) : "memory");
+    asm volatile("{\n .reg .pred p;\n setp.lt.u32 p, %1, %2;\n @p st.shared.u32 [%0], %3;\n @p add.u32 %0, %0, 128;\n}" : "+r"(at) : "r"(w - lo), "r"(width), "r"(x));
   };
+  auto listed = [&](int j) { uint32_t x; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(column + j * 128)); return x; };
   // Adds the words of this warp with lo <= w < lo + width to the buckets that bucket(w) gives.  Few words qualify, and a histogram's
   // additions cost a warp the same for one lane as for 32: each lane collects its own first.
   auto histogram = [&](uint32_t lo, uint32_t width, auto bucket) {
@@ -194,18 +195,23 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       const int most = __reduce_max_sync(0xffffffffu, (at - column) >> 7);
       for (int j = 0; j < most; ++j)
         if (column + j * 128 < at) {
-          const uint32_t w = s_list[j * 32 + lane];
+          const uint32_t w = listed(j);
           MassPair* p = bucket(w);
           atomicAdd(&p->lo, w & 0xFFFFu);
           atomicAdd(&p->hi, w >> 16);
         }
       at = column;
     };
-#pragma unroll 4
-    for (int k = 0; k < strip; k += 4) {
-      const uint4 y = l0 + k < l1 ? *reinterpret_cast<const uint4*>(wt + l0 + k) : make_uint4(0, 0, 0, 0);
-      append(at, y.x, lo, width, y.x); append(at, y.y, lo, width, y.y); append(at, y.z, lo, width, y.z); append(at, y.w, lo, width, y.w);
-      if (__any_sync(0xffffffffu, at > column_end - 4 * 128)) drain();
+    auto words = [&](int k) { return l0 + k < l1 ? *reinterpret_cast<const uint4*>(wt + l0 + k) : make_uint4(0, 0, 0, 0); };
+    for (int k = 0; k < strip; k += 16) {
+      uint4 y[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) y[g] = words(k + 4 * g);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        append(at, y[g].x, lo, width, y[g].x); append(at, y[g].y, lo, width, y[g].y); append(at, y[g].z, lo, width, y[g].z); append(at, y[g].w, lo, width, y[g].w);
+        if ((g & 1) && __any_sync(0xffffffffu, at > column_end - 8 * 128)) drain();
+      }
     }
     drain();
   };
@@ -354,17 +360,22 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       left = 0;
       uint32_t at_word = column;
       bool full = false;
-#pragma unroll 4
-      for (int i = l0; i < l1; i += 4) {
-        uint4 y = *reinterpret_cast<const uint4*>(wt + i);
-        full = full || at_word > column_end - 4 * 128;
-        if (full) at_word = column;
-        append(at_word, y.x, tau, 0x80000000u, i); append(at_word, y.y, tau, 0x80000000u, i + 1);
-        append(at_word, y.z, tau, 0x80000000u, i + 2); append(at_word, y.w, tau, 0x80000000u, i + 3);
-        y.x = y.x >= tau ? y.x : 0u; y.y = y.y >= tau ? y.y : 0u; y.z = y.z >= tau ? y.z : 0u; y.w = y.w >= tau ? y.w : 0u;
-        left += y.x + y.y;
-        left += y.z + y.w;
-        *reinterpret_cast<uint4*>(wt + i) = y;
+      for (int i0 = l0; i0 < l1; i0 += 16) {
+        uint4 y[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) y[g] = i0 + 4 * g < l1 ? *reinterpret_cast<const uint4*>(wt + i0 + 4 * g) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int i = i0 + 4 * g;
+          full = full || at_word > column_end - 4 * 128;
+          if (full) at_word = column;
+          append(at_word, y[g].x, tau, 0x80000000u, i); append(at_word, y[g].y, tau, 0x80000000u, i + 1);
+          append(at_word, y[g].z, tau, 0x80000000u, i + 2); append(at_word, y[g].w, tau, 0x80000000u, i + 3);
+          y[g].x = y[g].x >= tau ? y[g].x : 0u; y[g].y = y[g].y >= tau ? y[g].y : 0u; y[g].z = y[g].z >= tau ? y[g].z : 0u; y[g].w = y[g].w >= tau ? y[g].w : 0u;
+          left += y[g].x + y[g].y;
+          left += y[g].z + y[g].w;
+          if (i < l1) *reinterpret_cast<uint4*>(wt + i) = y[g];
+        }
       }
       left = warp_sum_u64(left);
       n_kept = __any_sync(0xffffffffu, full) ? -1 : (int)((at_word - column) >> 7);
@@ -390,7 +401,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
           int at[4];
           float prob[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) { at[k] = j + k < n_kept ? s_list[(j + k) * 32 + lane] : -1; prob[k] = at[k] >= 0 ? q[c0 + at[k]] : 0.f; }
+          for (int k = 0; k < 4; ++k) { at[k] = j + k < n_kept ? (int)listed(j + k) : -1; prob[k] = at[k] >= 0 ? q[c0 + at[k]] : 0.f; }
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             if (at[k] < 0) continue;
@@ -493,11 +504,11 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
         };
         if (n_kept >= 0) {
           uint64_t sum = 0;
-          for (int j = 0; j < n_kept; ++j) { const int i = s_list[j * 32 + lane]; sum += at(i, wt[i]); }
+          for (int j = 0; j < n_kept; ++j) { const int i = (int)listed(j); sum += at(i, wt[i]); }
           uint64_t run = base + warp_incl_scan_u64(sum, lane) - sum;
           if (r >= run && r < run + sum)
             for (int j = 0; j < n_kept; ++j) {
-              const int i = s_list[j * 32 + lane];
+              const int i = (int)listed(j);
               run += at(i, wt[i]);
               if (run > r) { found(i); break; }
             }
