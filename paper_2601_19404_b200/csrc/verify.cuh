@@ -457,9 +457,23 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       if (in) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(w) : "r"(remote(wt + v.token % a.slice, v.token / a.slice)) : "memory");
       auto passes = [&]() { return mul_shift24(q ? __double2ull_rz(verify_scaled(v.q, (double)mass)) : mass, v.u24) < w; };
       if (!whole) {
-        // The nucleus's mass lies between target and the row's, and what weighs more than all that it leaves out is in it: a first
-        // child that would be accepted at the row's mass is accepted at the nucleus's.
-        if (w > mass - target && passes()) { accepted = child; accepted_logit = v.logit; break; }
+        // The nucleus's mass lies between target and the row's, and a weight is in it when all above it are less than target: a first
+        // child that would be accepted at the row's mass, with such a weight, is accepted.  (Most are: no nucleus is needed.)
+        if (passes()) {
+          bool inside = w > mass - target;
+          if (!inside) {
+            uint64_t above = 0;
+            for (int i = w0 + lane * 4; i < w4; i += 128) {
+              const uint4 y = *reinterpret_cast<const uint4*>(wt + i);
+              above += (y.x > w ? y.x : 0u) + (y.y > w ? y.y : 0u);
+              above += (y.z > w ? y.z : 0u) + (y.w > w ? y.w : 0u);
+            }
+            if (w4 + lane < w1 && wt[w4 + lane] > w) above += wt[w4 + lane];
+            tell(warp_sum_u64(above), 0, xs, ys);
+            inside = sum_of(xs) < target;
+          }
+          if (inside) { accepted = child; accepted_logit = v.logit; break; }
+        }
         find_nucleus();
         written = true;
         if (w < tau) w = 0;
