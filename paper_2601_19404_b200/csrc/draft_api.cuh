@@ -18,8 +18,16 @@ static int launch_clusters(rpo_ctx* c, const char* label, void (*kern)(KArgs...)
   return RPO_OK;
 }
 
+// Clusters of more than eight CTAs have to be asked for, once per device.
+template <auto KERNEL>
+static cudaError_t allow_large_clusters(rpo_ctx* c) {
+  static OncePerDevice once;
+  return once.run(c->device, [&] { return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); });
+}
+
 template <int C>
 static int verify_launch(rpo_ctx* c, VerifyArgs a, int n_seqs) {
+  if (C > 8) CUDA_TRY((allow_large_clusters<verify_kernel<C>>(c)));
   CUDA_TRY((allow_smem<verify_kernel<C>>(c, VF_HIST + (((1 << 18) / C + 3) & ~3) * 4)));
   a.slice = (ceil_div(a.V, C) + 3) & ~3;
   return launch_clusters(c, "verify_kernel", verify_kernel<C>, n_seqs * C, C, VF_THREADS, (a.top_p24 < (1u << 24) ? VF_HIST : 0) + (size_t)a.slice * 4, a);
@@ -43,7 +51,9 @@ extern "C" int rpo_verify_drafts(rpo_ctx* c, int32_t n_seqs, int32_t n_rows, int
   a.path = d_path_out; a.n_path = d_n_path_out; a.next = d_next_out; a.logprobs = d_logprobs_out;
   a.V = vocab; a.n_rows = n_rows; a.max_path = max_path; a.greedy = sampler->greedy != 0; a.eos_id = sampler->eos_id;
   a.temperature = sampler->temperature; a.top_p24 = (uint32_t)floorf(sampler->top_p * 16777216.0f); a.status = c->d_status;
-  return verify_launch<8>(c, a, n_seqs);
+  // Few sequences: clusters of sixteen (4 trees of 24 nodes over 151 936 tokens, five levels at most: 36 us; clusters of eight 44).
+  // Many: eight, two of whose CTAs share an SM (16 chains of three accepted tokens over 152 064: 42 us; clusters of sixteen 44, 128: 164 and 229).
+  return n_seqs * 16 <= c->sm_count ? verify_launch<16>(c, a, n_seqs) : verify_launch<8>(c, a, n_seqs);
 }
 
 // All layers share pool size, tables and lengths; `l` describes their planes.

@@ -244,9 +244,9 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     const float* row = a.logits + (int64_t)(row0 + cur) * a.logits_stride;
     fa::cp_wait<0>();
     __syncwarp();
-    if (child >= 0)
+    for (int j = child, k = 0; j >= 0 && k < (C > 8 ? 4 : 1); j = child_behind(j), ++k)      // few sequences: the bandwidth is there
       for (int i = w0 + lane * 32; i < w1; i += 1024)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(a.logits + (int64_t)(row0 + child) * a.logits_stride + c0 + i));
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(a.logits + (int64_t)(row0 + j) * a.logits_stride + c0 + i));
     auto row_max = [&]() {                        // (what is no number counts as excluded)
       float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       for (int i = w0 + lane * 4; i < w4; i += 128) {
