@@ -93,8 +93,16 @@ static int page_cluster(int n_items) {
   return cluster;
 }
 
-static int plane_grid(const rpo_ctx* c, const PageLayers& l, int64_t items) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>((items * 2 * l.n_layers * l.hkv + 7) / 8, 8 * (int64_t)c->sm_count));
+// Planes that a CTA takes of each item: all SMs have work, and an item's look-ups are shared by at least `least` planes.
+static int planes_per_cta(const rpo_ctx* c, const PageLayers& l, int64_t items, int least) {
+  return std::max<int64_t>(least, ceil_div(items * 2 * l.n_layers * l.hkv, 8 * (int64_t)c->sm_count));
+}
+static int plane_grid(const PageLayers& l, int64_t items, int per) { return (int)std::min<int64_t>(items * ceil_div(2 * (int64_t)l.n_layers * l.hkv, per), 1 << 20); }
+
+static int copy_pages(rpo_ctx* c, const PageLayers& l, const PageWs& ws, int n) {
+  const int per = planes_per_cta(c, l, n, 8);
+  LAUNCH_OP(c, copy_pages_kernel, plane_grid(l, n, per), PG_MOVE_THREADS, 0, l, ws.copies, n, per);
+  return RPO_OK;
 }
 
 extern "C" int rpo_fork_pages(rpo_ctx* c, const rpo_page_pool* pool, const rpo_paged_kv* h_layers, int32_t n_layers, int32_t n_forks,
@@ -108,8 +116,7 @@ extern "C" int rpo_fork_pages(rpo_ctx* c, const rpo_page_pool* pool, const rpo_p
   a.src = d_src; a.dst = d_dst; a.lens = d_fork_lens; a.lens_out = d_lens_out; a.n = n_forks;
   const int cluster = page_cluster(n_forks);
   RPO_TRY(launch_clusters(c, "fork_pages_kernel", fork_pages_kernel, cluster, cluster, PG_THREADS, 0, a));
-  LAUNCH_OP(c, copy_pages_kernel, plane_grid(c, l, n_forks), 256, 0, l, a.p.ws.copies, n_forks);
-  return RPO_OK;
+  return copy_pages(c, l, a.p.ws, n_forks);
 }
 
 extern "C" int rpo_reserve_pages(rpo_ctx* c, const rpo_page_pool* pool, const rpo_paged_kv* h_layers, int32_t n_layers, const int32_t* d_lens,
@@ -122,8 +129,7 @@ extern "C" int rpo_reserve_pages(rpo_ctx* c, const rpo_page_pool* pool, const rp
   a.lens = d_lens; a.target = d_target_lens;
   const int cluster = page_cluster(a.p.n_seqs);
   RPO_TRY(launch_clusters(c, "reserve_pages_kernel", reserve_pages_kernel, cluster, cluster, PG_THREADS, 0, a));
-  LAUNCH_OP(c, copy_pages_kernel, plane_grid(c, l, a.p.n_seqs), 256, 0, l, a.p.ws.copies, a.p.n_seqs);
-  return RPO_OK;
+  return copy_pages(c, l, a.p.ws, a.p.n_seqs);
 }
 
 extern "C" int rpo_commit_path(rpo_ctx* c, const rpo_paged_kv* h_layers, int32_t n_layers, const int32_t* d_q_offsets, const int32_t* d_path,
@@ -136,6 +142,7 @@ extern "C" int rpo_commit_path(rpo_ctx* c, const rpo_paged_kv* h_layers, int32_t
   a.table = h_layers->d_block_table; a.lens = h_layers->d_lens; a.offsets = d_q_offsets; a.path = d_path; a.n_path = d_n_path; a.lens_out = d_lens_out;
   a.n_seqs = h_layers->n_seqs; a.stride = h_layers->table_stride; a.path_stride = path_stride; a.status = c->d_status;
   a.ticket = (int*)((PageCopy*)c->ws.op_pages + PG_MAX_ITEMS) + PG_MAX_ITEMS;
-  LAUNCH_OP(c, commit_path_kernel, plane_grid(c, l, a.n_seqs), 256, 0, l, a);
+  const int per = planes_per_cta(c, l, a.n_seqs, 8);
+  LAUNCH_OP(c, commit_path_kernel, plane_grid(l, a.n_seqs, per), PG_MOVE_THREADS, 0, l, a, per);
   return RPO_OK;
 }

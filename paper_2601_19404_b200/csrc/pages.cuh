@@ -37,7 +37,7 @@ struct PageLayers {                       // all layers of a cache: same pool, t
 
 struct PageCopy { int from, to, rows, pad; };            // rows 0: nothing to copy
 
-struct PageWs { PageCopy* copies; int *counts, *ticket; };      // [PG_MAX_ITEMS], [PG_MAX_ITEMS], one (zero between calls)
+struct PageWs { PageCopy* copies; int *counts, *ticket; };      // [PG_MAX_ITEMS], [PG_MAX_ITEMS], two (zero between calls)
 
 struct PagePoolArgs {
   int32_t *refs, *free, *n_free, *table, *held;
@@ -62,26 +62,37 @@ struct PagePoolArgs {
 struct ForkArgs { PagePoolArgs p; const int32_t *src, *dst, *lens; int32_t* lens_out; int n; };
 struct ReserveArgs { PagePoolArgs p; const int32_t *lens, *target; };
 
-struct PageShared { int64_t scan[32]; int first[PG_MAX_ITEMS + 1], taken; };   // first: pages needed, then released, before item i
+struct PageShared { int scan[PG_WARPS]; int first[PG_MAX_ITEMS + 1], taken; };   // first: pages needed, then released, before item i
+
+__device__ __forceinline__ int warp_before(int v, int lane) {                 // sum of the lower lanes' values
+  int incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int n = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += n; }
+  return incl - v;
+}
 
 // sh.first[i] = sum of count(i') over i' < i, for i <= n; all threads of the CTA.
 template <typename F>
 __device__ __forceinline__ void page_prefix(int n, PageShared& sh, F count) {
-  const int per = (n + PG_THREADS - 1) / PG_THREADS, i0 = threadIdx.x * per;
+  static_assert(PG_WARPS == 32, "a warp scans the warps' sums");
+  const int per = (n + PG_THREADS - 1) / PG_THREADS, i0 = threadIdx.x * per, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int c[PG_PER_THREAD], sum = 0;
 #pragma unroll
   for (int k = 0; k < PG_PER_THREAD; ++k) {
     c[k] = k < per && i0 + k < n ? count(i0 + k) : 0;
     sum += c[k];
   }
-  int64_t before, all;
-  plan_scan(sum, before, all, sh.scan);
+  int before = warp_before(sum, lane);
+  if (lane == 31) sh.scan[warp] = before + sum;
+  __syncthreads();
+  const int w = sh.scan[lane];
+  before += (int)__reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
 #pragma unroll
   for (int k = 0; k < PG_PER_THREAD; ++k) {
-    if (k < per && i0 + k < n) sh.first[i0 + k] = (int)before;
+    if (k < per && i0 + k < n) sh.first[i0 + k] = before;
     before += c[k];
   }
-  if (threadIdx.x == 0) sh.first[n] = (int)all;
+  if (threadIdx.x == PG_THREADS - 1) sh.first[n] = before;
   __syncthreads();
 }
 
@@ -114,55 +125,96 @@ struct ItemBits {
   }
 };
 
-// f(slot, page) for the slots [lo, hi) of a table row, 32 at a time, one per lane; page -1: no slot, or none of the pool.
-// MARKS: entries may carry PG_MARK.
+// f(slot, page) for the slots [lo, hi) of a table row, 32 PG_ROWS at a time: slot and page of each of a lane's PG_ROWS; page -1: no
+// slot, or none of the pool.  MARKS: entries may carry PG_MARK.
+constexpr int PG_ROWS = 4;
+
 template <bool MARKS = false, typename F>
 __device__ __forceinline__ void page_slots(const PagePoolArgs& p, int s, int lo, int hi, F f) {
   const int lane = threadIdx.x & 31;
   int32_t* row = p.table + (int64_t)s * p.stride;
-  for (int j = lo; j < hi; j += 32) {
-    int page = -1;
-    if (j + lane < hi) { page = row[j + lane]; if (!p.in_pool(MARKS ? page & ~PG_MARK : page)) page = -1; }
-    f(j + lane, page);
+  for (int j = lo; j < hi; j += 32 * PG_ROWS) {
+    int slot[PG_ROWS], page[PG_ROWS];
+#pragma unroll
+    for (int k = 0; k < PG_ROWS; ++k) { slot[k] = j + 32 * k + lane; page[k] = slot[k] < hi ? row[slot[k]] : 0; }
+#pragma unroll
+    for (int k = 0; k < PG_ROWS; ++k) if (slot[k] >= hi || !p.in_pool(MARKS ? page[k] & ~PG_MARK : page[k])) page[k] = -1;
+    f(slot, page);
   }
 }
 
-// The releasing half of a call.  dropped(i, f) calls f(slot, page) for the pages that item i gives up, slots ascending, a
-// warp together (page -1: none in this lane); finish(i) runs last, when the item's old table row is not needed any more.
+// The releasing half of a call.  dropped(i, f) calls f(slot, page) (as page_slots) for the pages that item i gives up, a warp
+// together; finish(i) runs last, when the item's old table row is not needed any more.
+//
+// A page that this item alone holds is claimed at once: its count becomes PG_CLAIM plus the item's place.  Other counts fall; where
+// several items of one call give up the last references to a page, which is rare, two more passes find the first of them.
 template <typename D, typename F>
 __device__ __forceinline__ void page_release(const PagePoolArgs& p, int n, int n_free, int n_taken, PageShared& sh, D dropped, F finish) {
   const int lane = threadIdx.x & 31, warp = blockIdx.x * PG_WARPS + (threadIdx.x >> 5), warps = gridDim.x * PG_WARPS;
+  auto place = [&](int i, int slot) { return PG_CLAIM + i * p.stride + slot; };
+  volatile int* several = p.ws.ticket + 1;               // a page lost its last reference to several items (zero between calls)
   fa::cluster_sync();                                    // counts grow before they fall
-  for (int i = warp; i < n; i += warps) dropped(i, [&](int, int page) { if (page >= 0) atomicSub(p.refs + page, 1); });
-  fa::cluster_sync();
-  for (int i = warp; i < n; i += warps)
-    dropped(i, [&](int slot, int page) {
-      if (page < 0) return;
-      const int r = p.count_of(page);
-      if (r == 0 || r < PG_CLAIM / 2) atomicMin(p.refs + page, PG_CLAIM + i * p.stride + slot);
-    });
-  fa::cluster_sync();
-  auto claimed = [&](int i, int slot, int page) { return page >= 0 && p.count_of(page) == PG_CLAIM + i * p.stride + slot; };
   for (int i = warp; i < n; i += warps) {
     int c = 0;
-    dropped(i, [&](int slot, int page) { c += __popc(__ballot_sync(0xffffffffu, claimed(i, slot, page))); });
+    dropped(i, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+      int r[PG_ROWS];
+#pragma unroll
+      for (int k = 0; k < PG_ROWS; ++k) r[k] = page[k] >= 0 ? p.count_of(page[k]) : 0;
+#pragma unroll
+      for (int k = 0; k < PG_ROWS; ++k) {
+        if (page[k] < 0) continue;
+        if (r[k] == 1) { p.refs[page[k]] = place(i, slot[k]); ++c; }
+        else if (atomicSub(p.refs + page[k], 1) == 1) *several = 1;
+      }
+    });
+    c = (int)__reduce_add_sync(0xffffffffu, c);
     if (lane == 0) p.ws.counts[i] = c;
   }
   fa::cluster_sync();
+  auto claimed = [&](int i, int slot, int page) { return page >= 0 && p.count_of(page) == place(i, slot); };
+  const bool again = *several != 0;
+  if (again) {
+    for (int i = warp; i < n; i += warps)
+      dropped(i, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+#pragma unroll
+        for (int k = 0; k < PG_ROWS; ++k) {
+          if (page[k] < 0) continue;
+          const int r = p.count_of(page[k]);
+          if (r == 0 || r < PG_CLAIM / 2) atomicMin(p.refs + page[k], place(i, slot[k]));
+        }
+      });
+    fa::cluster_sync();
+    for (int i = warp; i < n; i += warps) {
+      int c = 0;
+      dropped(i, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+#pragma unroll
+        for (int k = 0; k < PG_ROWS; ++k) c += claimed(i, slot[k], page[k]);
+      });
+      c = (int)__reduce_add_sync(0xffffffffu, c);
+      if (lane == 0) p.ws.counts[i] = c;
+    }
+    fa::cluster_sync();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *several = 0;
+  }
   page_prefix(n, sh, [&](int i) { return *(volatile int*)(p.ws.counts + i); });
   const int base = n_free - n_taken;
   for (int i = warp; i < n; i += warps) {
     int at = base + sh.first[i];
     if (sh.first[i + 1] > sh.first[i])
-      dropped(i, [&](int slot, int page) {
-        const bool mine = claimed(i, slot, page);
-        const unsigned who = __ballot_sync(0xffffffffu, mine);
-        const int to = at + __popc(who & ((1u << lane) - 1));
-        if (mine) {
-          p.refs[page] = 0;
-          if (to < p.n_blocks) p.free[to] = page; else p.bad_length();
+      dropped(i, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+        bool mine[PG_ROWS];
+#pragma unroll
+        for (int k = 0; k < PG_ROWS; ++k) mine[k] = claimed(i, slot[k], page[k]);
+#pragma unroll
+        for (int k = 0; k < PG_ROWS; ++k) {
+          const unsigned who = __ballot_sync(0xffffffffu, mine[k]);
+          const int to = at + __popc(who & ((1u << lane) - 1));
+          if (mine[k]) {
+            p.refs[page[k]] = 0;
+            if (to < p.n_blocks) p.free[to] = page[k]; else p.bad_length();
+          }
+          at += __popc(who);
         }
-        at += __popc(who);
       });
     __syncwarp();
     finish(i);
@@ -196,7 +248,10 @@ __global__ void __launch_bounds__(PG_THREADS) fork_pages_kernel(ForkArgs a) {
     if (valid(i) && page_served(p, sh, i, n_free)) {
       ok.set(k);
       const int len = a.lens[i], whole = len / KV_BLOCK, s = a.src[i];
-      page_slots(p, s, 0, whole, [&](int, int page) { if (page >= 0) atomicAdd(p.refs + page, 1); });
+      page_slots(p, s, 0, whole, [&](const int (&)[PG_ROWS], const int (&page)[PG_ROWS]) {
+#pragma unroll
+        for (int k = 0; k < PG_ROWS; ++k) if (page[k] >= 0) atomicAdd(p.refs + page[k], 1);
+      });
       if (len % KV_BLOCK) {
         copy.from = p.table[(int64_t)s * p.stride + whole];
         copy.to = p.free[n_free - 1 - sh.first[i]];
@@ -246,12 +301,18 @@ __global__ void __launch_bounds__(PG_THREADS) reserve_pages_kernel(ReserveArgs a
     const ReserveSeq x = seq(s);
     int32_t* row = p.table + (int64_t)s * p.stride;
     int need = max(0, x.want - x.held);
-    page_slots(p, s, x.len / KV_BLOCK, min(x.held, x.want), [&](int slot, int page) {
-      const bool others = page >= 0 && p.count_of(page) > 1;
-      if (others) row[slot] = page | PG_MARK;
-      else if (page < 0 && slot < min(x.held, x.want) && row[slot] >= 0) row[slot] = -1;      // (a number that could pass for a mark)
-      need += __popc(__ballot_sync(0xffffffffu, others));
+    int replaced = 0;
+    page_slots(p, s, x.len / KV_BLOCK, min(x.held, x.want), [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+      int r[PG_ROWS];
+#pragma unroll
+      for (int k = 0; k < PG_ROWS; ++k) r[k] = page[k] >= 0 ? p.count_of(page[k]) : 0;
+#pragma unroll
+      for (int k = 0; k < PG_ROWS; ++k) {
+        if (r[k] > 1) { row[slot[k]] = page[k] | PG_MARK; ++replaced; }
+        else if (page[k] < 0 && slot[k] < min(x.held, x.want) && row[slot[k]] >= 0) row[slot[k]] = -1;      // (a number that could pass for a mark)
+      }
     });
+    need += (int)__reduce_add_sync(0xffffffffu, replaced);
     if (lane == 0) p.ws.counts[s] = need;
   }
   fa::cluster_sync();
@@ -290,55 +351,64 @@ __global__ void __launch_bounds__(PG_THREADS) reserve_pages_kernel(ReserveArgs a
                [&](int s, auto f) {
                  if (!ok.get((s - warp) / warps)) return;
                  const ReserveSeq x = seq(s);
-                 page_slots<true>(p, s, x.len / KV_BLOCK, x.held, [&](int slot, int page) {
-                   int old = -1;
-                   if (page >= 0 && (page & PG_MARK)) {
-                     old = p.count_of(page & ~PG_MARK) - PG_OLD;
-                     if (old < 0 || old >= p.n_blocks) old = -1;
-                   } else if (slot >= x.want) old = page;
+                 page_slots<true>(p, s, x.len / KV_BLOCK, x.held, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+                   int old[PG_ROWS];
+#pragma unroll
+                   for (int k = 0; k < PG_ROWS; ++k) {
+                     old[k] = -1;
+                     if (page[k] >= 0 && (page[k] & PG_MARK)) {
+                       old[k] = p.count_of(page[k] & ~PG_MARK) - PG_OLD;
+                       if (old[k] < 0 || old[k] >= p.n_blocks) old[k] = -1;
+                     } else if (slot[k] >= x.want) old[k] = page[k];
+                   }
                    f(slot, old);
                  });
                },
                [&](int s) {
                  if (!ok.get((s - warp) / warps)) return;
                  const ReserveSeq x = seq(s);
-                 page_slots<true>(p, s, x.len / KV_BLOCK, min(x.held, x.want), [&](int slot, int page) {
-                   if (page < 0 || !(page & PG_MARK)) return;
-                   p.table[(int64_t)s * p.stride + slot] = page & ~PG_MARK;
-                   p.refs[page & ~PG_MARK] = 1;
+                 page_slots<true>(p, s, x.len / KV_BLOCK, min(x.held, x.want), [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+#pragma unroll
+                   for (int k = 0; k < PG_ROWS; ++k) {
+                     if (page[k] < 0 || !(page[k] & PG_MARK)) continue;
+                     p.table[(int64_t)s * p.stride + slot[k]] = page[k] & ~PG_MARK;
+                     p.refs[page[k] & ~PG_MARK] = 1;
+                   }
                  });
                  __syncwarp();
                  if (lane == 0) p.held[s] = x.want;
                });
 }
 
-// The first rows of pages, in every plane.
-constexpr int PG_LOADS = 8;
+// The first rows of pages, in every plane: a CTA takes one page and `per` planes, every thread the same 16 bytes of several planes.
+constexpr int PG_LOADS = 8, PG_MOVE_THREADS = 256;
 
-__global__ void __launch_bounds__(256) copy_pages_kernel(const __grid_constant__ PageLayers l, const PageCopy* copies, int n) {
-  const int lane = threadIdx.x & 31, planes = l.planes();
-  const int64_t total = (int64_t)n * planes, warps = (int64_t)gridDim.x * 8;
-  for (int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); w < total; w += warps) {
-    const PageCopy c = copies[w / planes];
-    if (c.rows == 0) continue;
-    uint8_t* base = l.plane((int)(w % planes));
+__global__ void __launch_bounds__(PG_MOVE_THREADS) copy_pages_kernel(const __grid_constant__ PageLayers l, const PageCopy* copies, int n, int per) {
+  const int parts = (l.planes() + per - 1) / per;
+  for (int64_t w = blockIdx.x; w < (int64_t)n * parts; w += gridDim.x) {
+    const PageCopy c = copies[w / parts];
+    const int pieces = c.rows * l.row_bytes / 16, p0 = (int)(w % parts) * per, p1 = min(l.planes(), p0 + per);
     const int64_t page_bytes = (int64_t)KV_BLOCK * l.row_bytes;
-    const uint4* from = reinterpret_cast<const uint4*>(base + c.from * page_bytes);
-    uint4* to = reinterpret_cast<uint4*>(base + c.to * page_bytes);
-    const int pieces = c.rows * l.row_bytes / 16;
-    for (int i0 = lane; i0 < pieces; i0 += 32 * PG_LOADS) {
-      uint4 x[PG_LOADS];
+    const int together = pieces > 0 && pieces <= PG_MOVE_THREADS / 2 ? PG_MOVE_THREADS / pieces : 1;      // planes side by side
+    const int sub = together > 1 ? threadIdx.x / pieces : 0;
+    if (sub >= together) continue;
+    for (int i = together > 1 ? threadIdx.x % pieces : threadIdx.x; i < pieces; i += PG_MOVE_THREADS)
+      for (int p = p0 + sub; p < p1; p += together * PG_LOADS) {
+        uint4 x[PG_LOADS];
 #pragma unroll
-      for (int u = 0; u < PG_LOADS; ++u) if (i0 + 32 * u < pieces) x[u] = from[i0 + 32 * u];
+        for (int u = 0; u < PG_LOADS; ++u) if (p + u * together < p1) x[u] = reinterpret_cast<const uint4*>(l.plane(p + u * together) + c.from * page_bytes)[i];
 #pragma unroll
-      for (int u = 0; u < PG_LOADS; ++u) if (i0 + 32 * u < pieces) to[i0 + 32 * u] = x[u];
-    }
+        for (int u = 0; u < PG_LOADS; ++u) if (p + u * together < p1) reinterpret_cast<uint4*>(l.plane(p + u * together) + c.to * page_bytes)[i] = x[u];
+      }
   }
 }
 
-// Commit: the rows of the accepted nodes, in ascending order, to the front of the tree's slots.  A warp moves those of one
-// sequence and plane in order, PG_LOADS pieces per lane at once; a row's source never lies before its destination, so what
-// is read later has not been overwritten.  The CTA that ends last writes the lengths, which the others have read.
+// Commit: the rows of the accepted nodes, in ascending order, to the front of the tree's slots.  A CTA takes a sequence and `per`
+// planes: it looks the rows' places up once, then every warp moves a plane's rows in order, PG_LOADS pieces per lane at once; a
+// row's source never lies before its destination, so what is read later has not been overwritten.  The CTA that ends last writes
+// the lengths, which the others have read.
+constexpr int PG_MOVES = 256;                             // rows whose places are kept at once
+
 struct CommitArgs {
   const int32_t *table, *lens, *offsets, *path, *n_path; int32_t* lens_out;
   int n_seqs, stride, path_stride;
@@ -367,39 +437,49 @@ __device__ __forceinline__ CommitSeq commit_seq(const CommitArgs& a, int s) {   
   return x;
 }
 
-__global__ void __launch_bounds__(256) commit_path_kernel(const __grid_constant__ PageLayers l, CommitArgs a) {
+__global__ void __launch_bounds__(PG_MOVE_THREADS) commit_path_kernel(const __grid_constant__ PageLayers l, CommitArgs a, int per) {
   __shared__ int s_last;
-  const int lane = threadIdx.x & 31, planes = l.planes(), lanes = l.row_bytes / 16, per = 32 / lanes;      // lanes of a row, rows at once
-  const int64_t total = (int64_t)a.n_seqs * planes, warps = (int64_t)gridDim.x * 8;
-  for (int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); w < total; w += warps) {
-    const int s = (int)(w / planes);
+  __shared__ int2 s_move[PG_MOVES];                      // rows inside a plane, from and to; to -1: stays
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lanes = l.row_bytes / 16, group = 32 / lanes;      // lanes of a row, rows at once
+  const int parts = (l.planes() + per - 1) / per;
+  for (int64_t w = blockIdx.x; w < (int64_t)a.n_seqs * parts; w += gridDim.x) {
+    const int s = (int)(w / parts), p0 = (int)(w % parts) * per, p1 = min(l.planes(), p0 + per);
     const CommitSeq q = commit_seq(a, s);
-    if (q.n <= 0) continue;
-    uint8_t* base = l.plane((int)(w % planes)) + (lane % lanes) * 16;
     const int32_t* path = a.path + (int64_t)s * a.path_stride;
     const int32_t* row = a.table + (int64_t)s * a.stride;
-    auto place = [&](int slot) -> int64_t {
+    auto place = [&](int slot) {
       const int page = row[slot / KV_BLOCK];
       if (page < 0 || page >= l.n_blocks) { atomicOr(a.status, STATUS_BAD_BLOCK); return -1; }
-      return ((int64_t)page * KV_BLOCK + slot % KV_BLOCK) * l.row_bytes;
+      return page * KV_BLOCK + slot % KV_BLOCK;
     };
-    for (int i0 = lane / lanes; i0 - lane / lanes < q.n; i0 += per * PG_LOADS) {
-      uint4 x[PG_LOADS];
-      int64_t to[PG_LOADS];
+    for (int first = 0; first < q.n; first += PG_MOVES) {
+      const int n = min(PG_MOVES, q.n - first);
+      __syncthreads();                                   // the last rows' places are read
+      for (int i = threadIdx.x; i < n; i += PG_MOVE_THREADS) {
+        const int node = path[first + i];
+        int2 m = make_int2(0, -1);
+        if (node != first + i) { m.x = place(q.past + node); m.y = place(q.past + first + i); if (m.x < 0) m.y = -1; }
+        s_move[i] = m;
+      }
+      __syncthreads();
+      for (int p = p0 + warp; p < p1; p += PG_MOVE_THREADS / 32) {
+        uint8_t* base = l.plane(p) + (lane % lanes) * 16;
+        for (int i0 = lane / lanes; i0 - lane / lanes < n; i0 += group * PG_LOADS) {
+          uint4 x[PG_LOADS];
+          int to[PG_LOADS];
 #pragma unroll
-      for (int u = 0; u < PG_LOADS; ++u) {
-        const int i = i0 + per * u, node = i < q.n ? path[i] : i;
-        to[u] = -1;
-        if (node != i) {
-          const int64_t from = place(q.past + node);
-          to[u] = place(q.past + i);
-          if (from < 0) to[u] = -1; else x[u] = *reinterpret_cast<const uint4*>(base + from);
+          for (int u = 0; u < PG_LOADS; ++u) {
+            const int i = i0 + group * u;
+            const int2 m = i < n ? s_move[i] : make_int2(0, -1);
+            to[u] = m.y;
+            if (m.y >= 0) x[u] = *reinterpret_cast<const uint4*>(base + (int64_t)m.x * l.row_bytes);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int u = 0; u < PG_LOADS; ++u) if (to[u] >= 0) *reinterpret_cast<uint4*>(base + (int64_t)to[u] * l.row_bytes) = x[u];
+          __syncwarp();
         }
       }
-      __syncwarp();
-#pragma unroll
-      for (int u = 0; u < PG_LOADS; ++u) if (to[u] >= 0) *reinterpret_cast<uint4*>(base + to[u]) = x[u];
-      __syncwarp();
     }
   }
   __syncthreads();
@@ -410,7 +490,7 @@ __global__ void __launch_bounds__(256) commit_path_kernel(const __grid_constant_
   __syncthreads();
   if (!s_last) return;
   if (threadIdx.x == 0) *a.ticket = 0;
-  for (int s = threadIdx.x >> 5; s < a.n_seqs; s += 8) {
+  for (int s = warp; s < a.n_seqs; s += PG_MOVE_THREADS / 32) {
     const CommitSeq q = commit_seq(a, s);
     if (lane == 0) a.lens_out[s] = q.n < 0 ? q.len : q.past + q.n;
   }
