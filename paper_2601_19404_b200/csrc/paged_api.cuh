@@ -63,6 +63,15 @@ static SplitWs split_ws(rpo_ctx* c, int rows_cap) {
   return w;
 }
 
+// The parts of items that several CTAs worked on: n_recs CTAs left records.
+template <typename T, int DH, bool TREE>
+static int merge_parts(rpo_ctx* c, const SplitWs& ws, const AttnOut<T>& o, int n_recs, int blocks_y, int subs = 1, int sub_rows = 0) {
+  static_assert(!TREE || OP_GRID * 148 <= MERGE_MAX_RECS, "records of a call");
+  if (TREE && n_recs <= MERGE_MAX_RECS) LAUNCH_OP(c, (tree_merge_kernel<T, DH>), 4 * c->sm_count, MERGE_WARPS * 32, 0, ws, o, n_recs, subs, sub_rows);
+  else LAUNCH_OP(c, (split_merge_kernel<T, DH>), dim3(n_recs, blocks_y), MERGE_WARPS * 32, 0, ws, o);
+  return RPO_OK;
+}
+
 // Few rows per sequence (decode steps): one CTA pair per SM over an equal share of all pages.
 template <int DH, bool TREE>
 static int chunk_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const bf16* k_new, const bf16* v_new,
@@ -74,8 +83,7 @@ static int chunk_steps(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   s.kv = view; s.c = a; s.q = q; s.q_stride = q_stride; s.k_new = k_new; s.v_new = v_new; s.new_stride = new_stride; s.scale_log2 = scale * 1.4426950408889634f;
   s.o.out = out; s.o.lse = lse; s.o.hq = a.hq; s.o.rep = a.hq / view.hkv; s.ws = split_ws(c, Cfg::ROWS); s.min_share = 4;
   LAUNCH_OP(c, (paged_step_kernel<DH, TREE>), grid, 128, Cfg::SMEM + (view.n_seqs + 1) * 4, s);
-  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(grid, std::min(a.max_chunk * s.o.rep, Cfg::ROWS)), MERGE_WARPS * 32, 0, s.ws, s.o);
-  return RPO_OK;
+  return merge_parts<bf16, DH, TREE>(c, s.ws, s.o, grid, std::min(a.max_chunk * s.o.rep, Cfg::ROWS));
 }
 
 // Tensor map over rows of head_dim 16-bit values in 128-byte swizzled boxes: 2 or 3 dimensions.
@@ -132,8 +140,7 @@ static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   LAUNCH_OP(c, (chunk_prepare_kernel<bf16, DH, CH_BN / KV_BLOCK, TREE>), (prepare_grid<bf16, DH, TREE>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4,
             2, items, plan, k_new, v_new, new_stride);
   LAUNCH_OP(c, (paged_chunk_kernel<DH, TREE>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
-  LAUNCH_OP(c, (split_merge_kernel<bf16, DH>), dim3(c->sm_count, OP_PART_ROWS / (MERGE_WARPS * MERGE_ROWS)), MERGE_WARPS * 32, 0, t.ws, t.o);
-  return RPO_OK;
+  return merge_parts<bf16, DH, TREE>(c, t.ws, t.o, c->sm_count, OP_PART_ROWS / (MERGE_WARPS * MERGE_ROWS));
 }
 
 // 32-bit storage: BM rows of an item against tiles of keys on CUDA cores.
@@ -154,8 +161,7 @@ static int chunk_f32(rpo_ctx* c, const PagedView<float>& view, const ChunkArgs& 
   LAUNCH_OP(c, (chunk_prepare_kernel<float, DH, Cfg::BN / KV_BLOCK, TREE>), (prepare_grid<float, DH, TREE>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, f.tok, grid, 2, 1, items,
             plan, k_new, v_new, new_stride);
   LAUNCH_OP(c, (paged_f32_kernel<DH, BM, TREE>), grid, 256, Cfg::SMEM, f);
-  LAUNCH_OP(c, (split_merge_kernel<float, DH>), dim3(grid, BM == 64 ? BM / (MERGE_WARPS * MERGE_ROWS) : std::min(a.max_chunk * f.o.rep, BM)), MERGE_WARPS * 32, 0, f.ws, f.o);
-  return RPO_OK;
+  return merge_parts<float, DH, TREE>(c, f.ws, f.o, grid, BM == 64 ? BM / (MERGE_WARPS * MERGE_ROWS) : std::min(a.max_chunk * f.o.rep, BM));
 }
 
 template <typename T, int DH, bool TREE>

@@ -157,6 +157,147 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) split_merge_kernel(SplitWs w
   }
 }
 
+// The same for trees: there are few items, cut into many parts, so the rows of all of them are spread over the whole grid.  Every
+// CTA reads all records; a warp takes a row, or, where some item has more than MERGE_MANY parts, a CTA does.  `subs` results lie in every
+// part, sub_rows rows apart (two where a kernel shared an item's keys among its two row tiles).
+// (2 trees of 48 nodes on 40000 .. 60001, 28 on 4 heads of 128, nine parts an item: 6 us; with split_merge_kernel 45.)
+constexpr int MERGE_MANY = 24, MERGE_MAX_RECS = 512;
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(SplitWs ws, AttnOut<T> a, int n_recs, int subs, int sub_rows) {
+  constexpr int DPL = DH / 32, W = MERGE_WARPS, THREADS = W * 32, PER = MERGE_MAX_RECS / THREADS;
+  __shared__ int s_first[MERGE_MAX_RECS + 1], s_scan[W], s_most;
+  __shared__ float s_o[W][DH];
+  __shared__ float s_l[W];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) s_most = 0;
+  int rows[PER], sum = 0, most = 0;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int c = tid * PER + k;
+    const SplitRec rec = c < n_recs ? ws.rec[c] : SplitRec{0, 0, 0, 0};
+    rows[k] = rec.n_parts > 0 ? rec.rows : 0;
+    most = max(most, rec.n_parts);
+    sum += rows[k];
+  }
+  int incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int n = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += n; }
+  if (lane == 31) s_scan[warp] = incl;
+  __syncthreads();
+  atomicMax(&s_most, most);
+  int before = incl - sum, total = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) { if (w < warp) before += s_scan[w]; total += s_scan[w]; }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) { if (tid * PER + k < n_recs) s_first[tid * PER + k] = before; before += rows[k]; }
+  __syncthreads();
+  struct Row { int64_t dst; int first, n, r; };              // where it goes; its record, results and place in them
+  auto row_of = [&](int u) {
+    int lo = 0, hi = n_recs - 1;                             // the last record that begins at or before row u (empty ones hold none)
+    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (s_first[mid] <= u) lo = mid; else hi = mid - 1; }
+    const SplitRec rec = ws.rec[lo];
+    const int r = u - s_first[lo];
+    return Row{(int64_t)(rec.row0 + r / a.rep) * a.hq + rec.head0 + r % a.rep, lo, rec.n_parts * subs, r};
+  };
+  auto place = [&](const Row& row, int q) -> int64_t {       // of result q: part q / subs, its (q % subs)-th
+    const int p = q / subs;
+    return (int64_t)(p == 0 ? 2 * row.first + 1 : 2 * (row.first + p)) * ws.rows_cap + (q % subs) * sub_rows + row.r;
+  };
+  auto load = [&](int64_t at, float (&x)[DPL]) {
+#pragma unroll
+    for (int i = 0; i < DPL; i += 2) { const float2 y = *reinterpret_cast<const float2*>(ws.o + at * DH + lane * DPL + i); x[i] = y.x; x[i + 1] = y.y; }
+  };
+  if (s_most * subs <= MERGE_FEW) {
+    for (int u0 = (blockIdx.x * W + warp) * MERGE_ROWS; u0 < total; u0 += gridDim.x * W * MERGE_ROWS) {
+      Row row[MERGE_ROWS];
+      float2 ml[MERGE_ROWS][MERGE_FEW];
+      float x[MERGE_ROWS][MERGE_FEW][DPL];
+#pragma unroll
+      for (int k = 0; k < MERGE_ROWS; ++k) row[k] = row_of(min(u0 + k, total - 1));
+#pragma unroll
+      for (int q = 0; q < MERGE_FEW; ++q)
+#pragma unroll
+        for (int k = 0; k < MERGE_ROWS; ++k) {
+          ml[k][q] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+          for (int i = 0; i < DPL; ++i) x[k][q][i] = 0.f;
+          if (q < row[k].n) { const int64_t at = place(row[k], q); ml[k][q] = ws.ml[at]; load(at, x[k][q]); }
+        }
+#pragma unroll
+      for (int k = 0; k < MERGE_ROWS; ++k) {
+        if (u0 + k >= total) break;
+        float m = -INFINITY, l = 0.f, acc[DPL];
+#pragma unroll
+        for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
+#pragma unroll
+        for (int q = 0; q < MERGE_FEW; ++q) m = fmaxf(m, ml[k][q].x);
+        const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int q = 0; q < MERGE_FEW; ++q) {
+          const float w = fa::ex2(ml[k][q].x - mu);
+          l = fmaf(w, ml[k][q].y, l);
+#pragma unroll
+          for (int i = 0; i < DPL; ++i) acc[i] = fmaf(w, x[k][q][i], acc[i]);
+        }
+        merge_store(a.out + row[k].dst * DH + lane * DPL, acc, l > 0.f ? 1.0f / l : 0.f);
+        if (lane == 0 && a.lse) a.lse[row[k].dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
+      }
+    }
+    return;
+  }
+  const bool by_cta = s_most * subs > MERGE_MANY;
+  const int step = by_cta ? gridDim.x : gridDim.x * W;
+  for (int u = by_cta ? blockIdx.x : blockIdx.x * W + warp; u < total; u += step) {
+    const Row row = row_of(u);
+    float m = -INFINITY;
+    for (int q = lane; q < row.n; q += 32) m = fmaxf(m, ws.ml[place(row, q)].x);
+    m = warp_max(m);
+    const float mu = m == -INFINITY ? 0.f : m;
+    float l = 0.f, acc[DPL];
+#pragma unroll
+    for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
+    const int w0 = by_cta ? warp : 0, ws_step = by_cta ? W : 1;
+    for (int q0 = w0; q0 < row.n; q0 += MERGE_LOADS * ws_step) {
+      float x[MERGE_LOADS][DPL];
+      float2 ml[MERGE_LOADS];
+#pragma unroll
+      for (int k = 0; k < MERGE_LOADS; ++k) {
+        const bool v = q0 + k * ws_step < row.n;
+        const int64_t at = place(row, v ? q0 + k * ws_step : q0);
+        ml[k] = v ? ws.ml[at] : make_float2(-INFINITY, 0.f);
+        load(at, x[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < MERGE_LOADS; ++k) {
+        const float w = fa::ex2(ml[k].x - mu);
+        l = fmaf(w, ml[k].y, l);
+#pragma unroll
+        for (int i = 0; i < DPL; ++i) acc[i] = fmaf(w, x[k][i], acc[i]);
+      }
+    }
+    if (by_cta) {
+#pragma unroll
+      for (int i = 0; i < DPL; ++i) s_o[warp][lane * DPL + i] = acc[i];
+      if (lane == 0) s_l[warp] = l;
+      __syncthreads();
+      l = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) l += s_l[w];
+      if (tid < DH) {
+        float o = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) o += s_o[w][tid];
+        a.out[row.dst * DH + tid] = from_f32<T>(l > 0.f ? o / l : 0.f);
+      }
+      __syncthreads();
+    } else {
+      merge_store(a.out + row.dst * DH + lane * DPL, acc, l > 0.f ? 1.0f / l : 0.f);
+    }
+    if (lane == 0 && (!by_cta || warp == 0) && a.lse) a.lse[row.dst] = l > 0.f ? m * LN2_F + logf(l) : -INFINITY;
+  }
+}
+
 // ---- the keys a run of rows can see -------------------------------------------------------------------------------
 // Positions [p0, p1] (p0 may be negative: rows before the first token).  Pages [0, n_first) hold the sinks (all pages
 // when there is no window or it reaches them), pages [lo_page, end_page) the window; keys below `lo` that are no sinks
