@@ -65,9 +65,9 @@ static SplitWs split_ws(rpo_ctx* c, int rows_cap) {
 
 // The parts of items that several CTAs worked on: n_recs CTAs left records.
 template <typename T, int DH, bool TREE>
-static int merge_parts(rpo_ctx* c, const SplitWs& ws, const AttnOut<T>& o, int n_recs, int blocks_y, int subs = 1, int sub_rows = 0) {
+static int merge_parts(rpo_ctx* c, const SplitWs& ws, const AttnOut<T>& o, int n_recs, int blocks_y) {
   static_assert(!TREE || OP_GRID * 148 <= MERGE_MAX_RECS, "records of a call");
-  if (TREE && n_recs <= MERGE_MAX_RECS) LAUNCH_OP(c, (tree_merge_kernel<T, DH>), 4 * c->sm_count, MERGE_WARPS * 32, 0, ws, o, n_recs, subs, sub_rows);
+  if (TREE && n_recs <= MERGE_MAX_RECS) LAUNCH_OP(c, (tree_merge_kernel<T, DH>), 4 * c->sm_count, MERGE_WARPS * 32, 0, ws, o, n_recs);
   else LAUNCH_OP(c, (split_merge_kernel<T, DH>), dim3(n_recs, blocks_y), MERGE_WARPS * 32, 0, ws, o);
   return RPO_OK;
 }
@@ -124,7 +124,10 @@ template <int DH, bool TREE>
 static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs& a, const bf16* q, int64_t q_stride, const bf16* k_new, const bf16* v_new,
                       int64_t new_stride, float scale, bf16* out, float* lse) {
   using Cfg = ChunkCfg<DH>;
-  CUDA_TRY((allow_smem<paged_chunk_kernel<DH, TREE>>(c, Cfg::SMEM)));
+  if constexpr (TREE) {
+    CUDA_TRY((allow_smem<tree_tile_kernel<DH, true>>(c, TreeCfg<DH, true>::SMEM)));
+    CUDA_TRY((allow_smem<tree_tile_kernel<DH, false>>(c, TreeCfg<DH, false>::SMEM)));
+  } else CUDA_TRY((allow_smem<paged_chunk_kernel<DH>>(c, Cfg::SMEM)));
   ChunkTcArgs t;
   t.kv = view; t.c = a; t.scale_log2 = scale * 1.4426950408889634f;
   t.o.out = out; t.o.lse = lse; t.o.hq = a.hq; t.o.rep = a.hq / view.hkv; t.ws = split_ws(c, OP_PART_ROWS);
@@ -139,7 +142,10 @@ static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   RPO_TRY(op_map_pages(c, &vm, view, view.v, DH));
   LAUNCH_OP(c, (chunk_prepare_kernel<bf16, DH, CH_BN / KV_BLOCK, TREE>), (prepare_grid<bf16, DH, TREE>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count, 4,
             2, items, plan, k_new, v_new, new_stride);
-  LAUNCH_OP(c, (paged_chunk_kernel<DH, TREE>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
+  if constexpr (TREE) {
+    if (a.max_chunk <= t.tq) LAUNCH_OP(c, (tree_tile_kernel<DH, true>), c->sm_count, (TreeCfg<DH, true>::THREADS), (TreeCfg<DH, true>::SMEM), qm, km, vm, t);
+    else LAUNCH_OP(c, (tree_tile_kernel<DH, false>), c->sm_count, (TreeCfg<DH, false>::THREADS), (TreeCfg<DH, false>::SMEM), qm, km, vm, t);
+  } else LAUNCH_OP(c, (paged_chunk_kernel<DH>), c->sm_count, Cfg::THREADS, Cfg::SMEM, qm, km, vm, t);
   return merge_parts<bf16, DH, TREE>(c, t.ws, t.o, c->sm_count, OP_PART_ROWS / (MERGE_WARPS * MERGE_ROWS));
 }
 

@@ -121,7 +121,9 @@ __global__ void __launch_bounds__(1024) chunk_prepare_kernel(PagedView<T> kv, Ch
       const int t0 = (i - pl_first[lo]) * tok;
       it.seq = lo; it.n_tok = min(tok, sp.rows - t0); it.row0 = sp.row0 + t0; it.p0 = sp.len - sp.rows + t0;
       it.key0 = TREE ? sp.len - sp.rows : it.p0;
-      it.n_tiles = KeyTiles<PAGES>(c, it.key0, it.p0 + it.n_tok - 1).n;
+      // (16-bit trees: a tile is one half where the item has two sub-tiles of rows)
+      if (TREE && sizeof(T) == 2 && it.n_tok > tok / 2) it.n_tiles = KeyTiles<PAGES / 2>(c, it.key0, it.p0 + it.n_tok - 1).n;
+      else it.n_tiles = KeyTiles<PAGES>(c, it.key0, it.p0 + it.n_tok - 1).n;
       n = (int64_t)(it.n_tiles + over) * kv.hkv;
     }
     int64_t before, all;
@@ -273,8 +275,7 @@ __device__ __forceinline__ bool chunk_wait_warp(uint64_t* bar, uint32_t parity, 
   return __all_sync(0xffffffffu, ok);
 }
 
-// TREE: the chunks are trees (paged_tree.cuh).
-template <int DH, bool TREE>
+template <int DH>
 __global__ void __launch_bounds__(ChunkCfg<DH>::THREADS, 1)
 paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                    ChunkTcArgs a) {
@@ -332,7 +333,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     bool ok = true;
     int kt = 0;                                              // tiles sent: ring position of K and V
     for (int seg = 0; ok && walk.next(); ++seg) {
-      const KeyTiles<CH_BN / KV_BLOCK> kt_of(a.c, walk.it.key0, walk.it.p0 + walk.it.n_tok - 1);
+      const KeyTiles<CH_BN / KV_BLOCK> kt_of(a.c, walk.it.p0, walk.it.p0 + walk.it.n_tok - 1);
       const bool two = walk.it.n_tok > a.tq;
       if (lane == 0) ok = tc::mbar_wait(q_free, (seg & 1) ^ 1, abort_flag);
       ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -373,17 +374,16 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     int kt = 0;
     while (ok && walk.next()) {
       const int p1 = walk.it.p0 + walk.it.n_tok - 1;
-      const KeyTiles<CH_BN / KV_BLOCK> kt_of(a.c, walk.it.key0, p1);
-      const TreeRow* nodes = TREE ? a.c.tree + (walk.it.row0 - (walk.it.p0 - walk.it.key0)) : nullptr;
+      const KeyTiles<CH_BN / KV_BLOCK> kt_of(a.c, walk.it.p0, p1);
       for (int t = walk.t0; t < walk.t1; ++t, ++kt) {
         const int sv = kt % NSV;
         ok = tc::mbar_wait_warp(&v_full[sv], (kt / NSV) & 1, abort_flag);
         if (!ok) break;
         const int key0 = kt_of.page0(t) * KV_BLOCK, seen_end = t < kt_of.n1 ? min(a.c.sinks, p1 + 1) : p1 + 1;
-        if (key0 + CH_BN > seen_end || (t >= kt_of.n1 && key0 < kt_of.kp.lo) || (TREE && key0 + CH_BN > walk.it.key0)) {
+        if (key0 + CH_BN > seen_end || (t >= kt_of.n1 && key0 < kt_of.kp.lo)) {
           for (int r = lane; r < CH_BN; r += 32) {
             const int j = key0 + r;
-            if (j < seen_end && (j >= kt_of.kp.lo || j < a.c.sinks) && !(TREE && j >= walk.it.key0 && nodes[j - walk.it.key0].depth < 0)) continue;
+            if (j < seen_end && (j >= kt_of.kp.lo || j < a.c.sinks)) continue;
             const uint32_t at = sV + sv * Cfg::KV_BYTES + (r >> 4) * PAGE + (r & 15) * 128;
 #pragma unroll
             for (int hf = 0; hf < HALVES; ++hf)
@@ -491,18 +491,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         skipped = false;
       }
       const int p_item = walk.it.p0, p1 = p_item + walk.it.n_tok - 1;
-      const KeyTiles<CH_BN / KV_BLOCK> kt_of(a.c, walk.it.key0, p1);
+      const KeyTiles<CH_BN / KV_BLOCK> kt_of(a.c, p_item, p1);
       const bool row_valid = in_tile && x * a.tq + tok < walk.it.n_tok;
-      int p_lo = p_item + x * a.tq, p_hi = min(p1, p_lo + a.tq - 1);     // positions of my sub-tile
-      int p = min(p_lo + tok, p_hi);
-      const TreeRow* node = nullptr;
-      bool live = row_valid;                                 // a row that takes part
-      if (TREE) {
-        node = a.c.tree + walk.it.row0 + x * a.tq + (p - p_lo);
-        live = live && node->depth >= 0;
-        p = walk.it.key0 + node->depth;
-        p_lo = walk.it.key0 - 1;                             // the last slot that may be seen without a look at the masks
-      }
+      const int p_lo = p_item + x * a.tq, p_hi = min(p1, p_lo + a.tq - 1);     // positions of my sub-tile
+      const int p = min(p_lo + tok, p_hi);
       float m = -INFINITY, l = 0.f;
       bool have_m = false;                                   // every row of the warp has a reference maximum
       // Halves [u_whole0, u_whole1) hold only keys that every row of the sub-tile sees (of the window's tiles; halves of
@@ -528,7 +520,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
         bool done = false;
         if (whole && have_m) {
           const float ps = chunk_exp(v, a.scale_log2, m);
-          done = __all_sync(0xffffffffu, ps < CH_MOST || !live);
+          done = __all_sync(0xffffffffu, ps < CH_MOST || !row_valid);
           if (done) l += ps;
           else {
             tc::tmem_ld32_nowait(ts, v);
@@ -540,12 +532,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
           if (!whole) {
             const int key0 = kt_of.page0(u >> 1) * KV_BLOCK + h * CH_HALF;
             const bool first_range = (u >> 1) < kt_of.n1;
-            const int last = TREE ? (live ? walk.it.key0 - 1 : -1) : p;
-            const int hi = (first_range ? min(last, a.c.sinks - 1) : last) - key0;
+            const int hi = (first_range ? min(p, a.c.sinks - 1) : p) - key0;
             const int lo = a.c.window > 0 ? p - a.c.window + 1 - key0 : -key0, sk = a.c.sinks - key0;
-            const uint64_t own = TREE && live && !first_range ? tree_bits(node->seen, key0 - walk.it.key0) : 0;
 #pragma unroll
-            for (int c = 0; c < CH_HALF; ++c) if ((c > hi || (c < lo && c >= sk)) && !(TREE && ((own >> c) & 1))) v[c] = 0xFF800000u;
+            for (int c = 0; c < CH_HALF; ++c) if (c > hi || (c < lo && c >= sk)) v[c] = 0xFF800000u;
           }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -570,7 +560,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
               }
             }
             if (move) { l *= factor; m = mt; }
-            have_m = __all_sync(0xffffffffu, m > -INFINITY || !live);
+            have_m = __all_sync(0xffffffffu, m > -INFINITY || !row_valid);
           }
           l += chunk_exp(v, a.scale_log2, m == -INFINITY ? 0.f : m);
         }
@@ -586,7 +576,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
       o_phase ^= 1;
       tc::tmem_fence_after();
       const bool begins = walk.t0 == 0, ends = walk.t1 == walk.it.n_tiles, split = !(begins && ends);
-      if (TREE && !live) { m = -INFINITY; l = 0.f; }          // whatever the halves without masks gave
       const float inv = l > 0.f ? 1.0f / l : 0.f;
       const int64_t dst = (int64_t)(walk.it.row0 + x * a.tq + tok) * a.o.hq + walk.head * rep + r % rep;
       const int64_t part = (int64_t)(2 * blockIdx.x + (begins ? 1 : 0)) * a.ws.rows_cap + x * (a.tq * rep) + r;
@@ -594,9 +583,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
       for (int c = 0; c < DH; c += 32) {
         uint32_t w[32];
         tc::tmem_ld32(t_o + c, w);                          // the whole warp loads, valid rows store
-        if (TREE && !(l > 0.f))                              // (a row whose V was not checked by any row may hold NaN)
-#pragma unroll
-          for (int i = 0; i < 32; ++i) w[i] = 0;
         if (row_valid && split) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(a.ws.o + part * DH + c + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);

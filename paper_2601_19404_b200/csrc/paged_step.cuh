@@ -158,13 +158,13 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) split_merge_kernel(SplitWs w
 }
 
 // The same for trees: there are few items, cut into many parts, so the rows of all of them are spread over the whole grid.  Every
-// CTA reads all records; a warp takes a row, or, where some item has more than MERGE_MANY parts, a CTA does.  `subs` results lie in every
-// part, sub_rows rows apart (two where a kernel shared an item's keys among its two row tiles).
+// CTA reads all records; a warp takes two rows where no item has more than MERGE_FEW parts, else one, or, where some item has more than
+// MERGE_MANY, a CTA does.
 // (2 trees of 48 nodes on 40000 .. 60001, 28 on 4 heads of 128, nine parts an item: 6 us; with split_merge_kernel 45.)
 constexpr int MERGE_MANY = 24, MERGE_MAX_RECS = 512;
 
 template <typename T, int DH>
-__global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(SplitWs ws, AttnOut<T> a, int n_recs, int subs, int sub_rows) {
+__global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(SplitWs ws, AttnOut<T> a, int n_recs) {
   constexpr int DPL = DH / 32, W = MERGE_WARPS, THREADS = W * 32, PER = MERGE_MAX_RECS / THREADS;
   __shared__ int s_first[MERGE_MAX_RECS + 1], s_scan[W], s_most;
   __shared__ float s_o[W][DH];
@@ -192,23 +192,20 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(SplitWs ws
 #pragma unroll
   for (int k = 0; k < PER; ++k) { if (tid * PER + k < n_recs) s_first[tid * PER + k] = before; before += rows[k]; }
   __syncthreads();
-  struct Row { int64_t dst; int first, n, r; };              // where it goes; its record, results and place in them
+  struct Row { int64_t dst; int first, n, r; };              // where it goes; its record, parts and place in them
   auto row_of = [&](int u) {
     int lo = 0, hi = n_recs - 1;                             // the last record that begins at or before row u (empty ones hold none)
     while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (s_first[mid] <= u) lo = mid; else hi = mid - 1; }
     const SplitRec rec = ws.rec[lo];
     const int r = u - s_first[lo];
-    return Row{(int64_t)(rec.row0 + r / a.rep) * a.hq + rec.head0 + r % a.rep, lo, rec.n_parts * subs, r};
+    return Row{(int64_t)(rec.row0 + r / a.rep) * a.hq + rec.head0 + r % a.rep, lo, rec.n_parts, r};
   };
-  auto place = [&](const Row& row, int q) -> int64_t {       // of result q: part q / subs, its (q % subs)-th
-    const int p = q / subs;
-    return (int64_t)(p == 0 ? 2 * row.first + 1 : 2 * (row.first + p)) * ws.rows_cap + (q % subs) * sub_rows + row.r;
-  };
+  auto place = [&](const Row& row, int p) -> int64_t { return (int64_t)(p == 0 ? 2 * row.first + 1 : 2 * (row.first + p)) * ws.rows_cap + row.r; };
   auto load = [&](int64_t at, float (&x)[DPL]) {
 #pragma unroll
     for (int i = 0; i < DPL; i += 2) { const float2 y = *reinterpret_cast<const float2*>(ws.o + at * DH + lane * DPL + i); x[i] = y.x; x[i + 1] = y.y; }
   };
-  if (s_most * subs <= MERGE_FEW) {
+  if (s_most <= MERGE_FEW) {
     for (int u0 = (blockIdx.x * W + warp) * MERGE_ROWS; u0 < total; u0 += gridDim.x * W * MERGE_ROWS) {
       Row row[MERGE_ROWS];
       float2 ml[MERGE_ROWS][MERGE_FEW];
@@ -246,7 +243,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(SplitWs ws
     }
     return;
   }
-  const bool by_cta = s_most * subs > MERGE_MANY;
+  const bool by_cta = s_most > MERGE_MANY;
   const int step = by_cta ? gridDim.x : gridDim.x * W;
   for (int u = by_cta ? blockIdx.x : blockIdx.x * W + warp; u < total; u += step) {
     const Row row = row_of(u);

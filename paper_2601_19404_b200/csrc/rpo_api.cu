@@ -26,6 +26,7 @@
 #include "paged_mass.cuh"
 #include "paged_step.cuh"
 #include "paged_tree.cuh"
+#include "paged_treetile.cuh"
 #include "pages.cuh"
 #include "ref_kernels.cuh"
 #include "sampler.cuh"
