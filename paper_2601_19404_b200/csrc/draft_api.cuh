@@ -89,13 +89,13 @@ static int check_pool(rpo_ctx* c, const rpo_page_pool* pool, const rpo_paged_kv*
 
 static int page_cluster(int n_items) {
   int cluster = 1;
-  while (cluster < PG_MAX_CLUSTER && n_items > cluster * PG_WARPS) cluster *= 2;
+  while (cluster < PG_MAX_CLUSTER && n_items > cluster * PG_WARPS / 2) cluster *= 2;      // (half of the warps: their accesses spread over more SMs)
   return cluster;
 }
 
-// Planes that a CTA takes of each item: all SMs have work, and an item's look-ups are shared by at least `least` planes.
-static int planes_per_cta(const rpo_ctx* c, const PageLayers& l, int64_t items, int least) {
-  return std::max<int64_t>(least, ceil_div(items * 2 * l.n_layers * l.hkv, 8 * (int64_t)c->sm_count));
+// Planes that a CTA takes of each item: all SMs have work, and an item's look-ups are shared by eight planes at least.
+static int planes_per_cta(const rpo_ctx* c, const PageLayers& l, int64_t items, int ctas_per_sm) {
+  return (int)std::min<int64_t>(PG_PLANES, std::max<int64_t>(8, ceil_div(items * 2 * l.n_layers * l.hkv, ctas_per_sm * (int64_t)c->sm_count)));
 }
 static int plane_grid(const PageLayers& l, int64_t items, int per) { return (int)std::min<int64_t>(items * ceil_div(2 * (int64_t)l.n_layers * l.hkv, per), 1 << 20); }
 
@@ -142,7 +142,7 @@ extern "C" int rpo_commit_path(rpo_ctx* c, const rpo_paged_kv* h_layers, int32_t
   a.table = h_layers->d_block_table; a.lens = h_layers->d_lens; a.offsets = d_q_offsets; a.path = d_path; a.n_path = d_n_path; a.lens_out = d_lens_out;
   a.n_seqs = h_layers->n_seqs; a.stride = h_layers->table_stride; a.path_stride = path_stride; a.status = c->d_status;
   a.ticket = (int*)((PageCopy*)c->ws.op_pages + PG_MAX_ITEMS) + PG_MAX_ITEMS;
-  const int per = planes_per_cta(c, l, a.n_seqs, 8);
+  const int per = planes_per_cta(c, l, a.n_seqs, 4);
   LAUNCH_OP(c, commit_path_kernel, plane_grid(l, a.n_seqs, per), PG_MOVE_THREADS, 0, l, a, per);
   return RPO_OK;
 }

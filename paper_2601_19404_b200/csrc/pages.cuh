@@ -146,16 +146,20 @@ __device__ __forceinline__ void page_slots(const PagePoolArgs& p, int s, int lo,
 // The releasing half of a call.  dropped(i, f) calls f(slot, page) (as page_slots) for the pages that item i gives up, a warp
 // together; finish(i) runs last, when the item's old table row is not needed any more.
 //
-// A page that this item alone holds is claimed at once: its count becomes PG_CLAIM plus the item's place.  Other counts fall; where
-// several items of one call give up the last references to a page, which is rare, two more passes find the first of them.
+// A page that this item alone holds is claimed at once: its count becomes PG_CLAIM plus the item's place, or, where a warp has one
+// item of at most 1024 pages, 0, and a bit of the lane's remembers it (random 4-byte accesses of a few SMs are what this costs: 256
+// sequences of 3600 pages on average given back 42 us with marks, 23 us with bits).  Other counts fall; where several items of one call
+// give up the last references to a page, which is rare, two more passes find the first of them.
 template <typename D, typename F>
 __device__ __forceinline__ void page_release(const PagePoolArgs& p, int n, int n_free, int n_taken, PageShared& sh, D dropped, F finish) {
   const int lane = threadIdx.x & 31, warp = blockIdx.x * PG_WARPS + (threadIdx.x >> 5), warps = gridDim.x * PG_WARPS;
   auto place = [&](int i, int slot) { return PG_CLAIM + i * p.stride + slot; };
   volatile int* several = p.ws.ticket + 1;               // a page lost its last reference to several items (zero between calls)
+  const bool bits = n <= warps && p.stride <= 32 / PG_ROWS * 32 * PG_ROWS;
+  uint32_t sole = 0;                                     // with bits: PG_ROWS for every call of f
   fa::cluster_sync();                                    // counts grow before they fall
   for (int i = warp; i < n; i += warps) {
-    int c = 0;
+    int c = 0, call = 0;
     dropped(i, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
       int r[PG_ROWS];
 #pragma unroll
@@ -163,9 +167,13 @@ __device__ __forceinline__ void page_release(const PagePoolArgs& p, int n, int n
 #pragma unroll
       for (int k = 0; k < PG_ROWS; ++k) {
         if (page[k] < 0) continue;
-        if (r[k] == 1) { p.refs[page[k]] = place(i, slot[k]); ++c; }
-        else if (atomicSub(p.refs + page[k], 1) == 1) *several = 1;
+        if (r[k] == 1) {
+          p.refs[page[k]] = bits ? 0 : place(i, slot[k]);
+          if (bits) sole |= 1u << (call * PG_ROWS + k);
+          ++c;
+        } else if (atomicSub(p.refs + page[k], 1) == 1) *several = 1;
       }
+      ++call;
     });
     c = (int)__reduce_add_sync(0xffffffffu, c);
     if (lane == 0) p.ws.counts[i] = c;
@@ -199,18 +207,19 @@ __device__ __forceinline__ void page_release(const PagePoolArgs& p, int n, int n
   page_prefix(n, sh, [&](int i) { return *(volatile int*)(p.ws.counts + i); });
   const int base = n_free - n_taken;
   for (int i = warp; i < n; i += warps) {
-    int at = base + sh.first[i];
+    int at = base + sh.first[i], call = 0;
     if (sh.first[i + 1] > sh.first[i])
       dropped(i, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
         bool mine[PG_ROWS];
 #pragma unroll
-        for (int k = 0; k < PG_ROWS; ++k) mine[k] = claimed(i, slot[k], page[k]);
+        for (int k = 0; k < PG_ROWS; ++k) mine[k] = bits && !again ? (sole >> (call * PG_ROWS + k)) & 1 : claimed(i, slot[k], page[k]);
+        ++call;
 #pragma unroll
         for (int k = 0; k < PG_ROWS; ++k) {
           const unsigned who = __ballot_sync(0xffffffffu, mine[k]);
           const int to = at + __popc(who & ((1u << lane) - 1));
           if (mine[k]) {
-            p.refs[page[k]] = 0;
+            if (!bits || again) p.refs[page[k]] = 0;
             if (to < p.n_blocks) p.free[to] = page[k]; else p.bad_length();
           }
           at += __popc(who);
@@ -381,32 +390,36 @@ __global__ void __launch_bounds__(PG_THREADS) reserve_pages_kernel(ReserveArgs a
 }
 
 // The first rows of pages, in every plane: a CTA takes one page and `per` planes, every thread the same 16 bytes of several planes.
-constexpr int PG_LOADS = 8, PG_MOVE_THREADS = 256;
+constexpr int PG_LOADS = 8, PG_MOVE_THREADS = 256, PG_PLANES = 64;
 
-__global__ void __launch_bounds__(PG_MOVE_THREADS) copy_pages_kernel(const __grid_constant__ PageLayers l, const PageCopy* copies, int n, int per) {
+__global__ void __launch_bounds__(PG_MOVE_THREADS, 4) copy_pages_kernel(const __grid_constant__ PageLayers l, const PageCopy* copies, int n, int per) {
+  __shared__ uint8_t* s_plane[PG_PLANES];                // `per` is at most that
   const int parts = (l.planes() + per - 1) / per;
   for (int64_t w = blockIdx.x; w < (int64_t)n * parts; w += gridDim.x) {
     const PageCopy c = copies[w / parts];
-    const int pieces = c.rows * l.row_bytes / 16, p0 = (int)(w % parts) * per, p1 = min(l.planes(), p0 + per);
-    const int64_t page_bytes = (int64_t)KV_BLOCK * l.row_bytes;
-    const int together = pieces > 0 && pieces <= PG_MOVE_THREADS / 2 ? PG_MOVE_THREADS / pieces : 1;      // planes side by side
-    const int sub = together > 1 ? threadIdx.x / pieces : 0;
+    const int pieces = c.rows * l.row_bytes / 16, p0 = (int)(w % parts) * per, planes = min(l.planes() - p0, per);
+    if (pieces == 0) continue;
+    const int64_t page_bytes = (int64_t)KV_BLOCK * l.row_bytes, from = c.from * page_bytes, to = c.to * page_bytes;
+    __syncthreads();                                     // the last planes are read
+    for (int p = threadIdx.x; p < planes; p += PG_MOVE_THREADS) s_plane[p] = l.plane(p0 + p);
+    __syncthreads();
+    const int together = max(1, PG_MOVE_THREADS / pieces), sub = pieces <= PG_MOVE_THREADS ? threadIdx.x / pieces : 0;      // planes side by side
     if (sub >= together) continue;
-    for (int i = together > 1 ? threadIdx.x % pieces : threadIdx.x; i < pieces; i += PG_MOVE_THREADS)
-      for (int p = p0 + sub; p < p1; p += together * PG_LOADS) {
+    for (int i = pieces <= PG_MOVE_THREADS ? threadIdx.x - sub * pieces : threadIdx.x; i < pieces; i += PG_MOVE_THREADS)
+      for (int p = sub; p < planes; p += together * PG_LOADS) {
         uint4 x[PG_LOADS];
 #pragma unroll
-        for (int u = 0; u < PG_LOADS; ++u) if (p + u * together < p1) x[u] = reinterpret_cast<const uint4*>(l.plane(p + u * together) + c.from * page_bytes)[i];
+        for (int u = 0; u < PG_LOADS; ++u) if (p + u * together < planes) x[u] = reinterpret_cast<const uint4*>(s_plane[p + u * together] + from)[i];
 #pragma unroll
-        for (int u = 0; u < PG_LOADS; ++u) if (p + u * together < p1) reinterpret_cast<uint4*>(l.plane(p + u * together) + c.to * page_bytes)[i] = x[u];
+        for (int u = 0; u < PG_LOADS; ++u) if (p + u * together < planes) reinterpret_cast<uint4*>(s_plane[p + u * together] + to)[i] = x[u];
       }
   }
 }
 
 // Commit: the rows of the accepted nodes, in ascending order, to the front of the tree's slots.  A CTA takes a sequence and `per`
-// planes: it looks the rows' places up once, then every warp moves a plane's rows in order, PG_LOADS pieces per lane at once; a
-// row's source never lies before its destination, so what is read later has not been overwritten.  The CTA that ends last writes
-// the lengths, which the others have read.
+// planes: it looks the rows' places up once, then moves the rows in order, PG_LOADS pieces per thread at once, all of them read before
+// any is written; a row's source never lies before its destination, so what is read later has not been overwritten.  The CTA that ends
+// last writes the lengths, which the others have read.
 constexpr int PG_MOVES = 256;                             // rows whose places are kept at once
 
 struct CommitArgs {
@@ -437,10 +450,11 @@ __device__ __forceinline__ CommitSeq commit_seq(const CommitArgs& a, int s) {   
   return x;
 }
 
-__global__ void __launch_bounds__(PG_MOVE_THREADS) commit_path_kernel(const __grid_constant__ PageLayers l, CommitArgs a, int per) {
+__global__ void __launch_bounds__(PG_MOVE_THREADS, 4) commit_path_kernel(const __grid_constant__ PageLayers l, CommitArgs a, int per) {
   __shared__ int s_last;
   __shared__ int2 s_move[PG_MOVES];                      // rows inside a plane, from and to; to -1: stays
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lanes = l.row_bytes / 16, group = 32 / lanes;      // lanes of a row, rows at once
+  __shared__ uint8_t* s_plane[PG_PLANES];                // `per` is at most that
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lanes = l.row_bytes / 16;      // 16-byte pieces of a row
   const int parts = (l.planes() + per - 1) / per;
   for (int64_t w = blockIdx.x; w < (int64_t)a.n_seqs * parts; w += gridDim.x) {
     const int s = (int)(w / parts), p0 = (int)(w % parts) * per, p1 = min(l.planes(), p0 + per);
@@ -455,6 +469,7 @@ __global__ void __launch_bounds__(PG_MOVE_THREADS) commit_path_kernel(const __gr
     for (int first = 0; first < q.n; first += PG_MOVES) {
       const int n = min(PG_MOVES, q.n - first);
       __syncthreads();                                   // the last rows' places are read
+      for (int p = p0 + threadIdx.x; p < p1; p += PG_MOVE_THREADS) s_plane[p - p0] = l.plane(p);
       for (int i = threadIdx.x; i < n; i += PG_MOVE_THREADS) {
         const int node = path[first + i];
         int2 m = make_int2(0, -1);
@@ -462,22 +477,30 @@ __global__ void __launch_bounds__(PG_MOVE_THREADS) commit_path_kernel(const __gr
         s_move[i] = m;
       }
       __syncthreads();
-      for (int p = p0 + warp; p < p1; p += PG_MOVE_THREADS / 32) {
-        uint8_t* base = l.plane(p) + (lane % lanes) * 16;
-        for (int i0 = lane / lanes; i0 - lane / lanes < n; i0 += group * PG_LOADS) {
+      // as many rows, and planes, as PG_LOADS pieces of every thread hold: all are read before any is written
+      const int rows = min(n, PG_LOADS * PG_MOVE_THREADS / lanes);
+      for (int r0 = 0; r0 < n; r0 += rows) {
+        const int nr = min(rows, n - r0), together = PG_LOADS * PG_MOVE_THREADS / (lanes * nr);
+        const int first_q = threadIdx.x / lanes / nr, first_r = threadIdx.x / lanes % nr, step_q = PG_MOVE_THREADS / lanes / nr, step_r = PG_MOVE_THREADS / lanes % nr;
+        for (int p = p0; p < p1; p += together) {
+          const int planes = min(together, p1 - p);
           uint4 x[PG_LOADS];
-          int to[PG_LOADS];
+          // this thread's pieces: planes q, rows r of them
+          auto pieces = [&](auto f) {
+            int q = first_q, r = first_r;
 #pragma unroll
-          for (int u = 0; u < PG_LOADS; ++u) {
-            const int i = i0 + group * u;
-            const int2 m = i < n ? s_move[i] : make_int2(0, -1);
-            to[u] = m.y;
-            if (m.y >= 0) x[u] = *reinterpret_cast<const uint4*>(base + (int64_t)m.x * l.row_bytes);
-          }
-          __syncwarp();
-#pragma unroll
-          for (int u = 0; u < PG_LOADS; ++u) if (to[u] >= 0) *reinterpret_cast<uint4*>(base + (int64_t)to[u] * l.row_bytes) = x[u];
-          __syncwarp();
+            for (int u = 0; u < PG_LOADS; ++u) {
+              if (q < planes) {
+                const int2 m = s_move[r0 + r];
+                if (m.y >= 0) f(u, s_plane[p - p0 + q] + threadIdx.x % lanes * 16, m);
+              }
+              q += step_q; r += step_r;
+              if (r >= nr) { r -= nr; ++q; }
+            }
+          };
+          pieces([&](int u, uint8_t* base, const int2& m) { x[u] = *reinterpret_cast<const uint4*>(base + (int64_t)m.x * l.row_bytes); });
+          __syncthreads();
+          pieces([&](int u, uint8_t* base, const int2& m) { *reinterpret_cast<uint4*>(base + (int64_t)m.y * l.row_bytes) = x[u]; });
         }
       }
     }
