@@ -666,3 +666,104 @@ def test_a_rollout_with_drafted_tokens():
         counts = np.bincount([p for s, row in enumerate(c.pool.d_block_table.tolist()) for p in row[:held[s]]], minlength=120)
         assert c.pool.d_refs.tolist() == counts.tolist() and int(c.pool.d_n_free) == int((counts == 0).sum())
         del graph
+
+
+# ---- beside one another, and far into memory -----------------------------------------------------------------------
+def test_two_contexts_on_two_streams_at_once():
+    """Workspaces belong to a context: calls of two contexts that overlap give what they give alone."""
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    made = [make_context("bf16", s) for s in streams]
+    cases = [Tree("bf16", 12, 2, 128, [40, 60], [3000, 900], seed=k) for k in range(2)]
+    checks = [Drafts(5003, TREES, seed=k, top_p=0.9) for k in range(2)]
+    alone = [(c.attend(x), d.run(x)) for x, c, d in zip(made, cases, checks)]
+    outs = [[(torch.zeros_like(a[0][0]), torch.zeros_like(a[0][1])) for _ in range(10)] for a in alone]
+    torch.cuda.synchronize()
+    for i in range(10):
+        for x, c, o in zip(made, cases, outs):
+            x.tree_attention(c.q, c.kv, c.d_off, c.d_parents, c.max_nodes, *o[i])
+    torch.cuda.synchronize()
+    for a, o in zip(alone, outs):
+        assert all(torch.equal(y, a[0][0]) and torch.equal(z, a[0][1]) for y, z in o)
+    for x, d, a in zip(made, checks, alone):
+        assert all(torch.equal(y, z) for y, z in zip(d.run(x), a[1]))
+        assert x.device_status() == 0
+        x.close()
+
+
+@pytest.mark.parametrize("n", [2, 30])
+def test_a_captured_step_follows_parents_lengths_and_numbers(n):
+    """Attention and verification replayed from a graph with other trees, lengths, tokens and random numbers in the same buffers."""
+    s = torch.cuda.Stream()
+    with make_context("bf16", s) as ctx:
+        first, second = (Tree("bf16", 12, 2, 128, [n, n, n], past, seed=k, holes=0.2 * k) for k, past in ((0, [200, 3, 50]), (1, [90, 77, 0])))
+        stride = first.kv.d_block_table.shape[1]
+        c = Drafts(997, [t for t in ([list(range(-1, n - 1))] * 3)], seed=1, top_p=0.9)
+        d = Drafts(997, [random_tree(n, np.random.default_rng(k)) for k in range(3)], seed=2, top_p=0.9, max_path=c.max_path)
+        out, lse = torch.zeros_like(first.q.contiguous()), torch.zeros(first.q.shape[:2], device=DEV)
+        buf = [torch.from_numpy(np.array(x)).to(DEV) for x in (c.logits, c.probs, c.tokens, c.parents, c.uniform)]
+        off = i32(c.off)
+        path, n_path, nxt = (torch.zeros(x, dtype=torch.int32, device=DEV) for x in ((3, c.max_path), (3,), (3,)))
+        logp = torch.zeros(3, c.max_path, device=DEV)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            ctx.tree_attention(first.q, first.kv, first.d_off, first.d_parents, n, out, lse)
+            ctx.verify_drafts(buf[0], buf[2], buf[3], off, buf[4], rpo.Sampler(1.0, 0.9), path, n_path, nxt, logp, d_draft_probs=buf[1])
+        torch.cuda.synchronize()
+        for tree, drafted in ((first, c), (second, d), (first, c)):
+            if tree is second:                                            # into the buffers that were captured
+                keep = first.k.clone(), first.v.clone(), first.q.clone()
+                blocks = min(first.k.shape[1], second.k.shape[1])
+                used = second.table[second.table >= 0]
+                assert used.max() < blocks or second.k.shape[1] <= first.k.shape[1]
+                first.k[:, :blocks], first.v[:, :blocks] = second.k[:, :blocks], second.v[:, :blocks]
+                first.q.copy_(second.q)
+            elif tree is first and drafted is c and "keep" in dir():
+                first.k.copy_(keep[0]); first.v.copy_(keep[1]); first.q.copy_(keep[2])
+            width = min(stride, tree.table.shape[1])
+            first.kv.d_block_table.fill_(-1)
+            first.kv.d_block_table[:, :width] = i32(tree.table[:, :width])
+            first.kv.d_lens.copy_(i32(tree.lens))
+            first.d_parents.copy_(i32(tree.parents))
+            for b, x in zip(buf, (drafted.logits, drafted.probs, drafted.tokens, drafted.parents, drafted.uniform)):
+                b.copy_(torch.from_numpy(np.array(x)))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            tree.check(out, lse)
+            drafted.check(path, n_path, nxt, logp)
+        assert ctx.device_status() == 0
+        del graph
+
+
+def test_pools_beyond_32_bit_offsets(contexts):
+    """The last pages of a pool of more than 2^32 bytes: attention, copies and moves."""
+    ctx, hkv, blocks, dh = contexts["bf16"], 4, (1 << 18) + 40, 128
+    k, v = (torch.zeros(hkv, blocks, 16, dh, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    pool = rpo.PagePool.empty(blocks, 2, 8, DEV)
+    pool.d_free.copy_(torch.arange(blocks, dtype=torch.int32, device=DEV))          # the last pages on top
+    lens = torch.zeros(2, dtype=torch.int32, device=DEV)
+    kv = rpo.PagedKV(k, v, pool.d_block_table, lens)
+    layers = rpo.PagedLayers([kv])
+    ctx.reserve_pages(pool, layers, lens, i32([60, 0]))
+    g = torch.Generator(DEV).manual_seed(0)
+    new = torch.randn(60, 8 + 2 * hkv, dh, device=DEV, generator=g).to(torch.bfloat16)
+    q, kn, vn = new[:, :8], new[:, 8:8 + hkv], new[:, 8 + hkv:]
+    lens.copy_(i32([60, 0]))
+    out = torch.zeros(60, 8, dh, dtype=torch.bfloat16, device=DEV)
+    parents = i32(range(-1, 59))
+    ctx.tree_attention(q, kv, i32([0, 60, 60]), parents, 60, out, d_k_new=kn, d_v_new=vn)
+    ctx.fork_pages(pool, layers, i32([0]), i32([1]), i32([55]), lens)
+    ctx.commit_path(layers, i32([0, 4, 4]), i32([[0, 3], [0, 0]]), i32([2, 0]), lens)
+    torch.cuda.synchronize()
+    assert ctx.device_status() == 0 and lens.tolist() == [58, 55]
+    table = pool.d_block_table.tolist()
+    assert min(table[0][:4] + table[1][3:4]) > (1 << 18) and table[0][:3] == table[1][:3] and table[0][3] != table[1][3]
+    for cache, want in ((k, kn), (v, vn)):
+        assert torch.equal(cache[:, table[0][3], :8], want[48:56].transpose(0, 1)) and torch.equal(cache[:, table[0][3], 8], want[56]) and torch.equal(cache[:, table[0][3], 9], want[59])
+        assert torch.equal(cache[:, table[1][3], :7], want[48:55].transpose(0, 1)) and not cache[:, table[1][3], 7:].any()
+    z = torch.einsum("rhd,khd->hrk", q[:, ::2].double(), kn.double()) * dh ** -0.5
+    w = torch.softmax(z.masked_fill(~torch.tril(torch.ones(60, 60, dtype=torch.bool, device=DEV)), -float("inf")), -1)
+    want = torch.einsum("hrk,khd->rhd", w, vn.double())
+    scale = torch.einsum("hrk,khd->rhd", w, vn.double().abs())
+    assert torch.all((out[:, ::2].double() - want).abs() <= scale * (2.0 ** -8 + 2.0 ** -18) + 2.0 ** -8 * want.abs())
