@@ -51,24 +51,30 @@ __device__ __forceinline__ uint32_t verify_u24(float u) {
 // is multiplied by).
 __device__ __forceinline__ double verify_scaled(float q, double mass) { return __dmul_rn((double)(q > 0.f ? fminf(q, 16384.f) : 0.f), mass); }
 
-// exp_nonpos(x) 2^30 with the same roundings in fewer instructions: rint by adding 1.5 x 2^23 (and 30), whose low bits then are the
-// exponent that the polynomial's result is raised by.  Numbers below -40 count as -40: between there and -24 the sampler's
-// exponential is 0, this one below 2^-4, which is a weight of 0 too and nothing in a sum.
-__device__ __forceinline__ float verify_exp(float x) {
+// exp_nonpos(x) 2^30 of two numbers, with the same roundings in fewer instructions: packed additions and products, rint by adding
+// 1.5 x 2^23 (and 30), whose low bits then are the exponent that the polynomial's result is raised by.  Numbers below -40 count as -40:
+// between there and -24 the sampler's exponential is 0, this one below 2^-4, which is a weight of 0 too and nothing in a sum.
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ void verify_exp(float x0, float x1, float& e0, float& e1) {
   constexpr float shift = 12582912.0f + 30.0f;
-  x = fmaxf(x, -40.0f);
-  const float t = radd(rmul(x, (float)1.44269504088896340736), shift), n = radd(t, -shift);
-  float r = radd(x, rmul(n, -__uint_as_float(0x3F317200u)));
-  r = radd(r, rmul(n, -(float)(0.69314718055994530942 - 0.693145751953125)));
-  float p = (float)(1.0 / 5040.0);
-  p = radd(rmul(p, r), (float)(1.0 / 720.0));
-  p = radd(rmul(p, r), (float)(1.0 / 120.0));
-  p = radd(rmul(p, r), (float)(1.0 / 24.0));
-  p = radd(rmul(p, r), (float)(1.0 / 6.0));
-  p = radd(rmul(p, r), 0.5f);
-  p = radd(rmul(p, r), 1.0f);
-  p = radd(rmul(p, r), 1.0f);
-  return __uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23));
+  auto both = [](float x) { return t5::pack2(x, x); };
+  const uint64_t x = t5::pack2(fmaxf(x0, -40.0f), fmaxf(x1, -40.0f));
+  const uint64_t t = t5::add2(mul2(x, both((float)1.44269504088896340736)), both(shift)), n = t5::add2(t, both(-shift));
+  uint64_t r = t5::add2(x, mul2(n, both(-__uint_as_float(0x3F317200u))));
+  r = t5::add2(r, mul2(n, both(-(float)(0.69314718055994530942 - 0.693145751953125))));
+  uint64_t p = both((float)(1.0 / 5040.0));
+  p = t5::add2(mul2(p, r), both((float)(1.0 / 720.0)));
+  p = t5::add2(mul2(p, r), both((float)(1.0 / 120.0)));
+  p = t5::add2(mul2(p, r), both((float)(1.0 / 24.0)));
+  p = t5::add2(mul2(p, r), both((float)(1.0 / 6.0)));
+  p = t5::add2(mul2(p, r), both(0.5f));
+  p = t5::add2(mul2(p, r), both(1.0f));
+  p = t5::add2(mul2(p, r), both(1.0f));
+  float p0, p1, t0, t1;
+  t5::unpack2(p, p0, p1);
+  t5::unpack2(t, t0, t1);
+  e0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
+  e1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
 }
 
 template <int C>
@@ -272,10 +278,12 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     uint64_t tot = 0;
     float sume = 0.f;
     auto weigh = [&](auto unit) {      // (what does not change within a row is decided outside the loop)
-      auto e_of = [&](float x) { return verify_exp(radd(unit.value ? x : __fdiv_rn(x, a.temperature), -zmax)); };
+      auto z_of = [&](float x) { return radd(unit.value ? x : __fdiv_rn(x, a.temperature), -zmax); };
       for (int i = w0 + lane * 4; i < w4; i += 128) {
         const float4 y = *reinterpret_cast<const float4*>(wt + i);
-        const float e0 = e_of(y.x), e1 = e_of(y.y), e2 = e_of(y.z), e3 = e_of(y.w);
+        float e0, e1, e2, e3;
+        verify_exp(z_of(y.x), z_of(y.y), e0, e1);
+        verify_exp(z_of(y.z), z_of(y.w), e2, e3);
         const uint4 w = make_uint4(__float2uint_rz(e0), __float2uint_rz(e1), __float2uint_rz(e2), __float2uint_rz(e3));
         sume += (e0 + e1) + (e2 + e3);
         tot += w.x + w.y;                         // (2^31 at most)
@@ -283,7 +291,8 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
         *reinterpret_cast<uint4*>(wt + i) = w;
       }
       if (w4 + lane < w1) {
-        const float e = e_of(__uint_as_float(wt[w4 + lane]));
+        float e, unused;
+        verify_exp(z_of(__uint_as_float(wt[w4 + lane])), 0.f, e, unused);
         const uint32_t w = __float2uint_rz(e);
         sume += e; tot += w; wt[w4 + lane] = w;
       }
