@@ -99,9 +99,10 @@ static int planes_per_cta(const rpo_ctx* c, const PageLayers& l, int64_t items, 
 }
 static int plane_grid(const PageLayers& l, int64_t items, int per) { return (int)std::min<int64_t>(items * ceil_div(2 * (int64_t)l.n_layers * l.hkv, per), 1 << 20); }
 
-static int copy_pages(rpo_ctx* c, const PageLayers& l, const PageWs& ws, int n) {
+static int copy_pages(rpo_ctx* c, const PageLayers& l, const PageWs& ws, int n, bool rare) {
   const int per = planes_per_cta(c, l, n, 8);
-  LAUNCH_OP(c, copy_pages_kernel, plane_grid(l, n, per), PG_MOVE_THREADS, 0, l, ws.copies, n, per);
+  const int grid = plane_grid(l, n, per);
+  LAUNCH_OP(c, copy_pages_kernel, rare ? std::min(grid, 4 * c->sm_count) : grid, PG_MOVE_THREADS, 0, l, ws.copies, n, per, rare);
   return RPO_OK;
 }
 
@@ -116,7 +117,7 @@ extern "C" int rpo_fork_pages(rpo_ctx* c, const rpo_page_pool* pool, const rpo_p
   a.src = d_src; a.dst = d_dst; a.lens = d_fork_lens; a.lens_out = d_lens_out; a.n = n_forks;
   const int cluster = page_cluster(n_forks);
   RPO_TRY(launch_clusters(c, "fork_pages_kernel", fork_pages_kernel, cluster, cluster, PG_THREADS, 0, a));
-  return copy_pages(c, l, a.p.ws, n_forks);
+  return copy_pages(c, l, a.p.ws, n_forks, false);
 }
 
 extern "C" int rpo_reserve_pages(rpo_ctx* c, const rpo_page_pool* pool, const rpo_paged_kv* h_layers, int32_t n_layers, const int32_t* d_lens,
@@ -129,7 +130,7 @@ extern "C" int rpo_reserve_pages(rpo_ctx* c, const rpo_page_pool* pool, const rp
   a.lens = d_lens; a.target = d_target_lens;
   const int cluster = page_cluster(a.p.n_seqs);
   RPO_TRY(launch_clusters(c, "reserve_pages_kernel", reserve_pages_kernel, cluster, cluster, PG_THREADS, 0, a));
-  return copy_pages(c, l, a.p.ws, a.p.n_seqs);
+  return copy_pages(c, l, a.p.ws, a.p.n_seqs, true);
 }
 
 extern "C" int rpo_commit_path(rpo_ctx* c, const rpo_paged_kv* h_layers, int32_t n_layers, const int32_t* d_q_offsets, const int32_t* d_path,

@@ -103,6 +103,8 @@ __device__ __forceinline__ bool page_served(const PagePoolArgs& p, const PageSha
   return false;
 }
 __device__ __forceinline__ int page_taken(PageShared& sh, int n, int n_free) {          // pages that the served ones take
+  if (sh.first[n] <= n_free) return sh.first[n];
+  __syncthreads();
   if (threadIdx.x == 0) sh.taken = 0;
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += PG_THREADS) if (sh.first[i + 1] <= n_free) atomicMax(&sh.taken, sh.first[i + 1]);
@@ -392,8 +394,13 @@ __global__ void __launch_bounds__(PG_THREADS) reserve_pages_kernel(ReserveArgs a
 // The first rows of pages, in every plane: a CTA takes one page and `per` planes, every thread the same 16 bytes of several planes.
 constexpr int PG_LOADS = 8, PG_MOVE_THREADS = 256, PG_PLANES = 64;
 
-__global__ void __launch_bounds__(PG_MOVE_THREADS, 4) copy_pages_kernel(const __grid_constant__ PageLayers l, const PageCopy* copies, int n, int per) {
+__global__ void __launch_bounds__(PG_MOVE_THREADS, 4) copy_pages_kernel(const __grid_constant__ PageLayers l, const PageCopy* copies, int n, int per, bool rare) {
   __shared__ uint8_t* s_plane[PG_PLANES];                // `per` is at most that
+  if (rare) {                                            // as a rule there is nothing to copy: one look instead of one per page
+    bool any = false;
+    for (int i = threadIdx.x; i < n; i += PG_MOVE_THREADS) any = any || copies[i].rows != 0;
+    if (!__syncthreads_or(any)) return;
+  }
   const int parts = (l.planes() + per - 1) / per;
   for (int64_t w = blockIdx.x; w < (int64_t)n * parts; w += gridDim.x) {
     const PageCopy c = copies[w / parts];
