@@ -254,11 +254,19 @@ __global__ void __launch_bounds__(PG_THREADS) fork_pages_kernel(ForkArgs a) {
   });
   const int n_taken = page_taken(sh, a.n, n_free);
   ItemBits ok;
+  // what a warp's first fork is stays in registers: behind a cluster barrier each look is one to L2 again
+  struct Fork { int src, dst, len, held, copy; };
+  Fork mine = {0, 0, 0, 0, -1};
+  auto fork = [&](int i) {
+    if (i == warp) return mine;
+    return Fork{a.src[i], a.dst[i], a.lens[i], p.pages_held(a.dst[i]), p.ws.copies[i].to};
+  };
   for (int i = warp, k = 0; i < a.n; i += warps, ++k) {
     PageCopy copy = {-1, -1, 0, 0};
     if (valid(i) && page_served(p, sh, i, n_free)) {
       ok.set(k);
       const int len = a.lens[i], whole = len / KV_BLOCK, s = a.src[i];
+      if (k == 0) mine = Fork{s, a.dst[i], len, p.pages_held(a.dst[i]), -1};
       page_slots(p, s, 0, whole, [&](const int (&)[PG_ROWS], const int (&page)[PG_ROWS]) {
 #pragma unroll
         for (int k = 0; k < PG_ROWS; ++k) if (page[k] >= 0) atomicAdd(p.refs + page[k], 1);
@@ -271,20 +279,27 @@ __global__ void __launch_bounds__(PG_THREADS) fork_pages_kernel(ForkArgs a) {
         if (lane == 0 && copy.to >= 0) p.refs[copy.to] = 1;
       }
     }
+    if (k == 0) mine.copy = copy.to;
     if (lane == 0) p.ws.copies[i] = copy;
   }
   page_release(p, a.n, n_free, n_taken, sh,
-               [&](int i, auto f) { if (ok.get((i - warp) / warps)) page_slots(p, a.dst[i], 0, p.pages_held(a.dst[i]), f); },
+               [&](int i, auto f) {
+                 if (!ok.get((i - warp) / warps)) return;
+                 const Fork x = fork(i);
+                 page_slots(p, x.dst, 0, x.held, f);
+               },
                [&](int i) {
                  if (!ok.get((i - warp) / warps)) return;
-                 const int len = a.lens[i], whole = len / KV_BLOCK, part = len % KV_BLOCK ? 1 : 0;
-                 const int32_t* from = p.table + (int64_t)a.src[i] * p.stride;
-                 int32_t* to = p.table + (int64_t)a.dst[i] * p.stride;
+                 const Fork x = fork(i);
+                 const int whole = x.len / KV_BLOCK, part = x.len % KV_BLOCK ? 1 : 0;
+                 const int32_t* from = p.table + (int64_t)x.src * p.stride;
+                 int32_t* to = p.table + (int64_t)x.dst * p.stride;
+#pragma unroll 4
                  for (int j = lane; j < whole; j += 32) to[j] = from[j];
                  if (lane == 0) {
-                   if (part) to[whole] = p.ws.copies[i].to;
-                   p.held[a.dst[i]] = whole + part;
-                   if (a.lens_out) a.lens_out[a.dst[i]] = len;
+                   if (part) to[whole] = x.copy;
+                   p.held[x.dst] = whole + part;
+                   if (a.lens_out) a.lens_out[x.dst] = x.len;
                  }
                });
 }
@@ -300,7 +315,7 @@ __global__ void __launch_bounds__(PG_THREADS) reserve_pages_kernel(ReserveArgs a
   __shared__ PageShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = blockIdx.x * PG_WARPS + (tid >> 5), warps = gridDim.x * PG_WARPS;
   const int n_free = p.free_pages(), n = p.n_seqs, most = p.stride * KV_BLOCK;
-  auto seq = [&](int s) {
+  auto look = [&](int s) {
     ReserveSeq x;
     x.held = p.pages_held(s);
     const int target = p.clamped(a.target[s], most);
@@ -308,6 +323,9 @@ __global__ void __launch_bounds__(PG_THREADS) reserve_pages_kernel(ReserveArgs a
     x.want = (target + KV_BLOCK - 1) / KV_BLOCK;
     return x;
   };
+  // a warp's first sequence stays in registers: behind a cluster barrier each look is one to L2 again
+  const ReserveSeq mine = warp < n ? look(warp) : ReserveSeq{0, 0, 0};
+  auto seq = [&](int s) { return s == warp ? mine : look(s); };
   for (int s = warp; s < n; s += warps) {
     const ReserveSeq x = seq(s);
     int32_t* row = p.table + (int64_t)s * p.stride;
