@@ -3,9 +3,9 @@
 //
 // Bound by latency where little is copied (a few dependent look-ups and barriers), by HBM where much is (the copied rows
 // once each way).  Fork and reserve change tables, counts and the stack of free pages in one cluster, whose barriers order the
-// phases, and leave a list of pages to copy; a second kernel copies those in all layers, a warp per page and plane (a plane
-// is K or V of one KV head of one layer) with eight 16-byte pieces per lane in flight.  Which page goes where is a
-// matter of the order of forks or sequences alone, never of timing:
+// phases, and leave a list of pages to copy; a second kernel copies those in all layers, a CTA per page and group of planes (a
+// plane is K or V of one KV head of one layer) with eight 16-byte pieces per thread in flight.  128 forks of 28 layers of 4 heads of
+// 128: 41 us, half of it tables and counts.  Which page goes where is a matter of the order of forks or sequences alone, never of timing:
 //   taken    the k-th page that the call needs, in order of (fork or sequence, page of it), is free[n_free - 1 - k]
 //   released a page whose count falls to 0 is pushed once, at the place of the first (fork or sequence, page) that drops it
 #pragma once
@@ -37,7 +37,7 @@ struct PageLayers {                       // all layers of a cache: same pool, t
 
 struct PageCopy { int from, to, rows, pad; };            // rows 0: nothing to copy
 
-struct PageWs { PageCopy* copies; int *counts, *ticket; };      // [PG_MAX_ITEMS], [PG_MAX_ITEMS], two (zero between calls)
+struct PageWs { PageCopy* copies; int *counts, *ticket; };      // [PG_MAX_ITEMS], [PG_MAX_ITEMS], two (the first zero between calls)
 
 struct PagePoolArgs {
   int32_t *refs, *free, *n_free, *table, *held;
@@ -150,16 +150,20 @@ __device__ __forceinline__ void page_slots(const PagePoolArgs& p, int s, int lo,
 //
 // A page that this item alone holds is claimed at once: its count becomes PG_CLAIM plus the item's place, or, where a warp has one
 // item of at most 1024 pages, 0, and a bit of the lane's remembers it (random 4-byte accesses of a few SMs are what this costs: 256
-// sequences of 3600 pages on average given back 42 us with marks, 23 us with bits).  Other counts fall; where several items of one call
+// sequences of 240 pages on average taken and given back 72 us with marks, 60 us with bits).  Other counts fall once all have been
+// looked at (a count that is 1 because another item has given the page up is not this item's alone); where several items of one call
 // give up the last references to a page, which is rare, two more passes find the first of them.
 template <typename D, typename F>
 __device__ __forceinline__ void page_release(const PagePoolArgs& p, int n, int n_free, int n_taken, PageShared& sh, D dropped, F finish) {
   const int lane = threadIdx.x & 31, warp = blockIdx.x * PG_WARPS + (threadIdx.x >> 5), warps = gridDim.x * PG_WARPS;
   auto place = [&](int i, int slot) { return PG_CLAIM + i * p.stride + slot; };
-  volatile int* several = p.ws.ticket + 1;               // a page lost its last reference to several items (zero between calls)
+  volatile int* found = p.ws.ticket + 1;                 // 1: shared pages are given up; 2: one of them by all who held it
   const bool bits = n <= warps && p.stride <= 32 / PG_ROWS * 32 * PG_ROWS;
   uint32_t sole = 0;                                     // with bits: PG_ROWS for every call of f
+  bool shared = false;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *found = 0;
   fa::cluster_sync();                                    // counts grow before they fall
+  auto claimed = [&](int i, int slot, int page) { return page >= 0 && p.count_of(page) == place(i, slot); };
   for (int i = warp; i < n; i += warps) {
     int c = 0, call = 0;
     dropped(i, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
@@ -173,16 +177,31 @@ __device__ __forceinline__ void page_release(const PagePoolArgs& p, int n, int n
           p.refs[page[k]] = bits ? 0 : place(i, slot[k]);
           if (bits) sole |= 1u << (call * PG_ROWS + k);
           ++c;
-        } else if (atomicSub(p.refs + page[k], 1) == 1) *several = 1;
+        } else shared = true;
       }
       ++call;
     });
     c = (int)__reduce_add_sync(0xffffffffu, c);
     if (lane == 0) p.ws.counts[i] = c;
   }
+  shared = __any_sync(0xffffffffu, shared);
+  if (shared && lane == 0) *found = 1;
   fa::cluster_sync();
-  auto claimed = [&](int i, int slot, int page) { return page >= 0 && p.count_of(page) == place(i, slot); };
-  const bool again = *several != 0;
+  bool again = false;
+  if (*found) {
+    if (shared)
+      for (int i = warp; i < n; i += warps) {
+        int call = 0;
+        dropped(i, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+#pragma unroll
+          for (int k = 0; k < PG_ROWS; ++k)
+            if (page[k] >= 0 && !(bits ? (sole >> (call * PG_ROWS + k)) & 1 : claimed(i, slot[k], page[k])) && atomicSub(p.refs + page[k], 1) == 1) *found = 2;
+          ++call;
+        });
+      }
+    fa::cluster_sync();
+    again = *found == 2;
+  }
   if (again) {
     for (int i = warp; i < n; i += warps)
       dropped(i, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
@@ -204,7 +223,6 @@ __device__ __forceinline__ void page_release(const PagePoolArgs& p, int n, int n
       if (lane == 0) p.ws.counts[i] = c;
     }
     fa::cluster_sync();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *several = 0;
   }
   page_prefix(n, sh, [&](int i) { return *(volatile int*)(p.ws.counts + i); });
   const int base = n_free - n_taken;

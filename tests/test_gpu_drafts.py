@@ -455,6 +455,33 @@ def test_pages_of_many_sequences(contexts):
     assert int(c.pool.d_n_free) == blocks and ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("n,width,second,slot", [(2, 1000, 1, 990), (300, 40, 256, 0), (300, 40, 299, 39), (700, 1100, 512, 1000)])
+def test_a_shared_page_is_pushed_where_it_was_first_given_up(contexts, n, width, second, slot):
+    """Two sequences hold one page and give it up in one call, the second of them long after the first."""
+    ctx = contexts["bf16"]
+    c = Cache("bf16", 1, 1, 64, 2 * width + n, n, width)
+    lens = [0] * n
+    lens[0] = lens[second] = width * 16
+    ctx.reserve_pages(c.pool, c.layers, i32([0] * n), i32(lens))
+    c.twin.reserve([0] * n, lens)
+    c.same()
+    # the second's page in `slot` goes back to the stack by hand, the first's page 0 takes its place
+    t = c.twin
+    page, lost = t.table[0][0], t.table[second][slot]
+    t.table[second][slot] = page
+    t.refs[page], t.refs[lost], t.free[t.n_free] = 2, 0, lost
+    t.n_free += 1
+    c.pool.d_block_table.copy_(i32(t.table))
+    c.pool.d_refs.copy_(i32(t.refs))
+    c.pool.d_free.copy_(i32(t.free))
+    c.pool.d_n_free.fill_(t.n_free)
+    c.same()
+    ctx.reserve_pages(c.pool, c.layers, i32(lens), i32([0] * n))
+    t.reserve(lens, [0] * n)
+    c.same()
+    assert ctx.device_status() == 0
+
+
 def test_pages_of_one_long_sequence(contexts):
     ctx = contexts["bf16"]
     c = Cache("bf16", 1, 1, 64, 14000, 3, 6300)
