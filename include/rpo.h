@@ -271,7 +271,7 @@ int rpo_sample_rows_noalloc(int32_t n_rows, int32_t vocab, const float* d_logits
  * keep every key.)
  *
  * The calls enqueue work on the context's stream, allocate nothing, do not synchronise and can be
- * captured into a CUDA graph; split work goes through workspaces of the context (48 MB, taken at
+ * captured into a CUDA graph; split work goes through workspaces of the context (54 MB, taken at
  * rpo_create), so calls on one context (replays of graphs that hold them included) must not overlap
  * on the GPU.  Outputs must not overlap inputs except where said.  Results do not depend on the
  * order in which the GPU finishes things: the same call gives the same bits.
@@ -369,7 +369,7 @@ int rpo_evict_cache(rpo_ctx* ctx, const rpo_paged_kv* kv, const float* d_mass, c
  * A tree is a list of nodes: rows [d_offsets[s], d_offsets[s+1]) of sequence s, node i of it naming its parent
  * among the nodes before it, d_parents[row] < i.  -1: the node follows the last cached token.  -2: there is no
  * node in this row (padding); neither is there where the chain of parents ends in one.  Any other number is
- * taken for -2 and sets bit 3 of the status word. */
+ * taken for -2, and rpo_tree_attention sets bit 3 of the status word. */
 
 /* Attention of a tree of drafted tokens per sequence over the paged cache.  Node i of n lies in slot len - n + i
  * and sits at position p = len - n + depth (0 for a child of the last cached token).  It sees the len - n cached

@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) split_merge_kernel(SplitWs w
 // The same for trees: there are few items, cut into many parts, so the rows of all of them are spread over the whole grid.  Every
 // CTA reads all records; a warp takes two rows where no item has more than MERGE_FEW parts, else one, or, where some item has more than
 // MERGE_MANY, a CTA does.
-// (2 trees of 48 nodes on 40000 .. 60001, 28 on 4 heads of 128, nine parts an item: 6 us; with split_merge_kernel 45.)
+// (2 trees of 48 nodes on 40000 .. 60001, 28 on 4 heads of 128, nine parts an item: the whole call 139 us, with split_merge_kernel 178.)
 constexpr int MERGE_MANY = 24, MERGE_MAX_RECS = 512;
 
 template <typename T, int DH>

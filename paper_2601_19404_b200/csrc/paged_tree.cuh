@@ -6,9 +6,10 @@
 // positions below `sinks`.  A node whose chain of parents does not end at -1 is no node: it sees nothing, is seen by none,
 // and its K and V are not written.
 //
-// The attention kernels differ from those of causal chunks in the mask of the chunk's own slots alone, so they are the same
-// kernels with one more template parameter.  Up to 16 rows (paged_step.cuh) the warp that works on an item finds the masks
-// with shuffles; the tiled kernels read them from a list that tree_rows below writes, one bit per slot.
+// Attention differs from that of causal chunks in the mask of the chunk's own slots alone.  Up to 16 rows (paged_step.cuh) and in
+// 32 bits (paged_f32.cuh) it runs in the same kernels with one more template parameter; paged_treetile.cuh holds the 16-bit kernel
+// of larger trees.  Up to 16 rows the warp that works on an item finds the masks with shuffles; the others read them from a list
+// that tree_rows below writes, one bit per slot.
 #pragma once
 #include "paged_kv.cuh"
 

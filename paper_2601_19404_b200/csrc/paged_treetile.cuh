@@ -5,7 +5,8 @@
 // paged_tree.cuh.  What differs: a decode step with drafted tokens has few rows per sequence and many keys, so K and V are read
 // for one sub-tile of rows as a rule, and one sub-tile alone is bound by the chain S -> softmax -> P V of its 64-key units (2200
 // clocks a unit, 63 % of a copy's rate).  Here both softmax warpgroups and both issuers serve such an item: they take
-// alternate units, each with a sum and an output of its own, and join them through shared memory at the end of a piece.  Items of two
+// alternate units, each with a sum and an output of its own; at the end of a piece warpgroup 0 joins both outputs, which lie in the
+// same lanes of tensor memory.  Items of two
 // sub-tiles work as there, one for each warpgroup.  K and V come in rings of 64-key units, and both issuers follow every unit's
 // barriers, also those of units that are the other's.
 //
@@ -13,7 +14,8 @@
 // of them are in flight.  64 trees of 16 nodes on 1024 .. 6144 tokens, 28 on 4 heads of 128: 104 to 109 us of this kernel, 4.7 TB/s, 72 % of
 // a copy's rate (121 to 128 us with the list of items before and the join behind; in paged_chunk.cuh's way 136).  Steps: one producer for K
 // and V, 8 units 174 (K waits in line behind V); two producers 140; 12 units instead of 8 121; with the pages prefetched to L2 half a batch
-// ahead 129, not kept.  2 trees of 48 nodes on 40000 .. 60001: 133 to 141 us, where one sub-tile pair of 252 rows is bound by the softmax.
+// ahead 129, not kept.  2 trees of 48 nodes on 40000 .. 60001: 133 to 141 us, 123 of this kernel; their 336 rows
+// are an item of two sub-tiles and one of one, which read the keys once each (372 MB instead of 233), tensor pipe 46 %.
 #pragma once
 #include "paged_chunk.cuh"
 #include "paged_tree.cuh"
@@ -117,19 +119,17 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
     for (int seg = 0; ok && walk.next(); ++seg) {
       const bool two = two_of();
       const TreeTiles tiles = tiles_of();
-      const int p1 = walk.it.p0 + walk.it.n_tok - 1, past = walk.it.key0;
-      const TreeRow* nodes = a.c.tree + (walk.it.row0 - (walk.it.p0 - past));
-      if (is_k) {
-        if (lane == 0) ok = tc::mbar_wait(q_free, (seg & 1) ^ 1, abort_flag);
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
-        if (lane == 0) {
-          tc::mbar_expect_tx(q_full, (two ? 2 : 1) * HALVES * rep * a.tq * 128);
-          for (int x = 0; x < (two ? 2 : 1); ++x)
-            for (int hf = 0; hf < HALVES; ++hf)
-              t5::tma_load_3d(sQ + x * Cfg::Q_BYTES + hf * (CH_BM * 128), &q_map, hf * 64, walk.head * rep, walk.it.row0 + x * a.tq, q_full);
-        }
-      }
+      // Lane 0 sends the queries when the last piece's are done with, at the latest before the piece's unit NS: the first NS units only
+      // wait for earlier pieces, so that keys are on their way while those finish.
+      bool q_sent = !is_k;
+      auto send_q = [&](bool now) {
+        if (lane != 0 || q_sent || !(now ? tc::mbar_wait(q_free, (seg & 1) ^ 1, abort_flag) : tc::mbar_try_wait(q_free, (seg & 1) ^ 1))) return;
+        q_sent = true;
+        tc::mbar_expect_tx(q_full, (two ? 2 : 1) * HALVES * rep * a.tq * 128);
+        for (int x = 0; x < (two ? 2 : 1); ++x)
+          for (int hf = 0; hf < HALVES; ++hf)
+            t5::tma_load_3d(sQ + x * Cfg::Q_BYTES + hf * (CH_BM * 128), &q_map, hf * 64, walk.head * rep, walk.it.row0 + x * a.tq, q_full);
+      };
       const int32_t* tbl = a.kv.table + (int64_t)walk.it.seq * a.kv.table_stride;
       // The blocks of 32 pages at once, a batch ahead (a unit takes less time than a look-up): lane b holds page b % pages of tile
       // t + b / pages; behind the pages that are seen, the last of them (masked, V zeroed)
@@ -149,30 +149,17 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
         for (int u = 0; u < (two ? 1 : 2); ++u, ++ku) {
           const int st = ku % NS, b = lane % UP, hf = lane / UP;       // lanes 0 .. UP HALVES - 1: one 16 x 64 box each
           const int y = (walk.head * a.kv.n_blocks + __shfl_sync(0xffffffffu, blk, at + u * UP + b)) * KV_BLOCK;
+          send_q((t - walk.t0) * (two ? 1 : 2) + u >= NS);
           if (lane == 0) { ok = tc::mbar_wait(&empty[st], ((ku / NS) & 1) ^ 1, abort_flag); if (ok) tc::mbar_expect_tx(&full[st], Cfg::UNIT_BYTES); }
           ok = __shfl_sync(0xffffffffu, ok, 0);
           if (!ok) break;
           if (hf < HALVES)
             t5::tma_load_2d(ring + st * Cfg::UNIT_BYTES + (is_k ? hf * (Cfg::UNIT * 128) + b * 2048 : b * PAGE + hf * 2048), is_k ? (const void*)&k_map : (const void*)&v_map,
                             hf * 64, y, &full[st]);
-          if (is_k || !special(tiles, two, (t - walk.t0) * (two ? 1 : 2) + u)) continue;
-          ok = tc::mbar_wait_warp(&v_full[st], (ku / NS) & 1, abort_flag);
-          if (!ok) break;
-          const int key0 = tiles.page0(t) * KV_BLOCK + u * Cfg::UNIT, seen_end = t < tiles.n1 ? min(a.c.sinks, p1 + 1) : p1 + 1;
-          for (int r = lane; r < Cfg::UNIT; r += 32) {
-            const int j = key0 + r;
-            if (j < seen_end && (j >= tiles.kp.lo || j < a.c.sinks) && !(j >= past && nodes[j - past].depth < 0)) continue;
-            const uint32_t row = sV + st * Cfg::UNIT_BYTES + (r >> 4) * PAGE + (r & 15) * 128;
-#pragma unroll
-            for (int h2 = 0; h2 < HALVES; ++h2)
-#pragma unroll
-              for (int ch = 0; ch < 8; ++ch) fa::st_zero16(row + h2 * 2048 + ch * 16);
-          }
-          t5::fence_async_smem();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&v_ready[st]);
         }
       }
+      if (ok) send_q(true);
+      ok = __shfl_sync(0xffffffffu, ok && (q_sent || lane != 0), 0);
     }
   } else if (warp < 3) {
     // ------------------------------------------------------------------ MMA issuers: warp 1 for warpgroup 0, warp 2 for warpgroup 1
@@ -184,12 +171,29 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
     const uint32_t t_s = tm + x * CH_BN, t_o = tm + 2 * CH_BN + x * DH;
     bool ok = true;
     int ku = 0, step = 0;                                    // units of the pieces before; units of this warpgroup so far
-    uint32_t ready = 0;                                      // bit st: phase of v_ready[st], which special units alone complete
+    uint32_t ready = 0;                                      // bit st: phase of v_ready[st], which special units of two sub-tiles alone complete
     for (int seg = 0; ok && walk.next(); ++seg) {
       const bool two = two_of();
       const TreeTiles tiles = tiles_of();
       const int n_units = (walk.t1 - walk.t0) * (two ? 1 : 2), n_own = walk.t1 - walk.t0, own0 = two ? 0 : x, every = two ? 1 : 2;
       const uint32_t dq = dq0 + (two ? x * (Cfg::Q_BYTES >> 4) : 0);
+      const int p1 = walk.it.p0 + walk.it.n_tok - 1, past = walk.it.key0;
+      const TreeRow* nodes = a.c.tree + (walk.it.row0 - (walk.it.p0 - past));
+      // Zeros for the rows of V in unit i that no row of the item sees (the issuer does it while P is on its way).
+      auto zero_unseen = [&](int i, int st) {
+        const int t = walk.t0 + (two ? i : i >> 1), key0 = tiles.page0(t) * KV_BLOCK + (two ? 0 : (i & 1) * Cfg::UNIT), seen_end = t < tiles.n1 ? min(a.c.sinks, p1 + 1) : p1 + 1;
+        for (int r = lane; r < Cfg::UNIT; r += 32) {
+          const int j = key0 + r;
+          if (j < seen_end && (j >= tiles.kp.lo || j < a.c.sinks) && !(j >= past && nodes[j - past].depth < 0)) continue;
+          const uint32_t row = sV + st * Cfg::UNIT_BYTES + (r >> 4) * PAGE + (r & 15) * 128;
+#pragma unroll
+          for (int h2 = 0; h2 < HALVES; ++h2)
+#pragma unroll
+            for (int ch = 0; ch < 8; ++ch) fa::st_zero16(row + h2 * 2048 + ch * 16);
+        }
+        t5::fence_async_smem();
+        __syncwarp();
+      };
       int k_at = 0, v_at = 0;                                // units of this piece whose K, V this warp is done with
       // K of the units up to own unit j: the other's are passed on, of mine S = Q K^T is issued.
       auto qk = [&](int j) {
@@ -220,11 +224,14 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
           const int st = (ku + v_at) % NS;
           const uint32_t ready_parity = (ready >> st) & 1;
           const bool zeros = special(tiles, two, v_at);
-          if (zeros) ready ^= 1u << st;
+          if (zeros && two) ready ^= 1u << st;
           ok = tc::mbar_wait_warp(&v_full[st], ((ku + v_at) / NS) & 1, abort_flag);
           if (!ok) break;
           if (v_at < target) { if (t5::elect_one()) tc::mbar_arrive(&v_empty[st]); continue; }
-          if (zeros) ok = tc::mbar_wait_warp(&v_ready[st], ready_parity, abort_flag);
+          if (zeros && (!two || x == 0)) {
+            zero_unseen(v_at, st);
+            if (two && lane == 0) tc::mbar_arrive(&v_ready[st]);
+          } else if (zeros) ok = tc::mbar_wait_warp(&v_ready[st], ready_parity, abort_flag);
           if (!ok) break;
           ok = tc::mbar_wait_warp(&p_full[x * 2 + h], ((step + j) >> 1) & 1, abort_flag);
           if (!ok) break;
@@ -247,7 +254,6 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
       }
       for (; ok && v_at < n_units; ++v_at) {
         const int st = (ku + v_at) % NS;
-        if (special(tiles, two, v_at)) ready ^= 1u << st;
         ok = tc::mbar_wait_warp(&v_full[st], ((ku + v_at) / NS) & 1, abort_flag);
         if (ok && t5::elect_one()) tc::mbar_arrive(&v_empty[st]);
       }
