@@ -51,8 +51,8 @@ extern "C" int rpo_verify_drafts(rpo_ctx* c, int32_t n_seqs, int32_t n_rows, int
   a.path = d_path_out; a.n_path = d_n_path_out; a.next = d_next_out; a.logprobs = d_logprobs_out;
   a.V = vocab; a.n_rows = n_rows; a.max_path = max_path; a.greedy = sampler->greedy != 0; a.eos_id = sampler->eos_id;
   a.temperature = sampler->temperature; a.top_p24 = (uint32_t)floorf(sampler->top_p * 16777216.0f); a.status = c->d_status;
-  // Few sequences: clusters of sixteen (4 trees of 24 nodes over 151 936 tokens, five levels at most: 36 us; clusters of eight 44).
-  // Many: eight, two of whose CTAs share an SM (16 chains of three accepted tokens over 152 064: 42 us; clusters of sixteen 44, 128: 164 and 229).
+  // Few sequences: clusters of sixteen (4 trees of 24 nodes over 151 936 tokens 32.9 us, clusters of eight 37.9; 8 chains of 9 with
+  // probabilities 51, eight 59).  Many: eight, two of whose CTAs share an SM (16 such chains 80 us, sixteen 86; 128: 248 and 417).
   return n_seqs * 16 <= c->sm_count ? verify_launch<16>(c, a, n_seqs) : verify_launch<8>(c, a, n_seqs);
 }
 

@@ -10,12 +10,14 @@
 // sub-tiles work as there, one for each warpgroup.  K and V come in rings of 64-key units, and both issuers follow every unit's
 // barriers, also those of units that are the other's.
 //
-// Bound by what is on its way from DRAM: a CTA holds 12 units (192 KB) and consumes K two of its units before V, so that about half
-// of them are in flight.  64 trees of 16 nodes on 1024 .. 6144 tokens, 28 on 4 heads of 128: 104 to 109 us of this kernel, 4.7 TB/s, 72 % of
-// a copy's rate (121 to 128 us with the list of items before and the join behind; in paged_chunk.cuh's way 136).  Steps: one producer for K
-// and V, 8 units 174 (K waits in line behind V); two producers 140; 12 units instead of 8 121; with the pages prefetched to L2 half a batch
-// ahead 129, not kept.  2 trees of 48 nodes on 40000 .. 60001: 133 to 141 us, 123 of this kernel; their 336 rows
-// are an item of two sub-tiles and one of one, which read the keys once each (372 MB instead of 233), tensor pipe 46 %.
+// 64 trees of 16 nodes on 1024 .. 6144 tokens, 28 on 4 heads of 128: 121 to 125 us with the list of items before (7) and the join behind
+// (8), in paged_chunk.cuh's way 136.  Long runs go at a copy's rate (2 trees of 18 nodes on three times 40000 .. 60001 tokens: 64 us
+// more for 410 MB more, 6.4 TB/s); what a call costs beyond its bytes is filling and draining the rings, 12 units (192 KB) a CTA, and the
+// kernels around.  Steps: one producer for K and V and 8 units 174 (K waits in line behind V); two producers 140; 12 units 121 to 129;
+// keys of the next piece sent before its queries, rows of V zeroed by the issuers instead of the producer 125 where it was 129.  Not
+// kept: pages prefetched to L2 half a batch ahead, 129 where it was 123.
+// 2 trees of 48 nodes on 40000 .. 60001: 133 to 141 us, 123 of this kernel; their 336 rows are an item of two sub-tiles and one of one,
+// which read the keys once each (372 MB instead of 233).
 #pragma once
 #include "paged_chunk.cuh"
 #include "paged_tree.cuh"
