@@ -140,8 +140,9 @@ static int chunk_tiles(rpo_ctx* c, const PagedView<bf16>& view, const ChunkArgs&
   RPO_TRY(op_map_rows(c, &qm, q, q_stride, a.n_rows, a.hq, DH, t.o.rep, t.tq));
   RPO_TRY(op_map_pages(c, &km, view, view.k, DH));
   RPO_TRY(op_map_pages(c, &vm, view, view.v, DH));
+  const bool weighed = TREE && a.max_chunk > t.tq;           // tiles count 3 or 4
   LAUNCH_OP(c, (chunk_prepare_kernel<bf16, DH, CH_BN / KV_BLOCK, TREE>), (prepare_grid<bf16, DH, TREE>(view, a, k_new)), 1024, view.n_seqs * 4, view, a, 2 * t.tq, c->sm_count,
-            TREE ? 1 : 4, TREE ? 4 : 2, items, plan, k_new, v_new, new_stride);
+            weighed ? 4 : TREE ? 1 : 4, weighed ? 14 : TREE ? 4 : 2, items, plan, k_new, v_new, new_stride);
   if constexpr (TREE) {
     if (a.max_chunk <= t.tq) LAUNCH_OP(c, (tree_tile_kernel<DH, true>), c->sm_count, (TreeCfg<DH, true>::THREADS), (TreeCfg<DH, true>::SMEM), qm, km, vm, t);
     else LAUNCH_OP(c, (tree_tile_kernel<DH, false>), c->sm_count, (TreeCfg<DH, false>::THREADS), (TreeCfg<DH, false>::SMEM), qm, km, vm, t);

@@ -42,9 +42,10 @@ constexpr float CH_MOST = 2.0f * CH_HALF;      // largest sum of a half's P that
 
 // p0: slot of the item's first token (its position, unless the chunk is a tree); key0: the first position that a row may sit at
 // and, of a tree, the slot of its first node
-struct ChunkItem { int first, n_tiles, row0, n_tok; int seq, p0, key0, pad; };
+struct ChunkItem { int first, n_tiles, row0, n_tok; int seq, p0, key0, weight; };
 // `first`, `total`, `share` count (tile, KV head)s, and `over` more for every (item, KV head): what filling the pipeline for
-// it and writing its result costs, in tiles, so that CTAs with many short pieces get fewer tiles.
+// it and writing its result costs, in tiles, so that CTAs with many short pieces get fewer tiles.  A tile counts `weight` (1, but
+// in calls of 16-bit trees whose items may have one sub-tile of rows or two: 4 and 3, as their tiles took 1.57 and 1.17 us side by side).
 struct ChunkPlan { int n_items, total, share, over; };
 
 // Key tiles of an item: the sinks' pages, then the window's, each padded to whole tiles.
@@ -124,7 +125,8 @@ __global__ void __launch_bounds__(1024) chunk_prepare_kernel(PagedView<T> kv, Ch
       // (16-bit trees: a tile is one half where the item has two sub-tiles of rows)
       if (TREE && sizeof(T) == 2 && it.n_tok > tok / 2) it.n_tiles = KeyTiles<PAGES / 2>(c, it.key0, it.p0 + it.n_tok - 1).n;
       else it.n_tiles = KeyTiles<PAGES>(c, it.key0, it.p0 + it.n_tok - 1).n;
-      n = (int64_t)(it.n_tiles + over) * kv.hkv;
+      it.weight = TREE && sizeof(T) == 2 && c.max_chunk > tok / 2 ? (it.n_tok > tok / 2 ? 3 : 4) : 1;
+      n = ((int64_t)it.n_tiles * it.weight + over) * kv.hkv;
     }
     int64_t before, all;
     plan_scan(n, before, all, s_warp);
@@ -140,8 +142,10 @@ __global__ void __launch_bounds__(1024) chunk_prepare_kernel(PagedView<T> kv, Ch
   if (tid == 0) *plan = ChunkPlan{n_items, (int)total, max(min_share, (int)((total + n_ctas - 1) / n_ctas)), over};
 }
 
-// The pieces of one CTA, in order: every role of the CTA walks the same ones.
-struct PieceWalk {
+// The pieces of one CTA, in order: every role of the CTA walks the same ones.  WEIGHED: tiles count their items' weights (a share counts at
+// least the largest); a tile is the CTA's in whose share it begins.
+template <bool WEIGHED>
+struct PieceWalkOf {
   const ChunkItem* items;
   int f, f_end, idx, hkv, over;
   // of the current piece
@@ -149,19 +153,23 @@ struct PieceWalk {
   __device__ __forceinline__ bool next() {
     while (f < f_end) {
       it = items[idx];
-      if (f >= it.first + (it.n_tiles + over) * hkv) it = items[++idx];  // items hold at least one tile
-      const int w = it.n_tiles + over, in_item = f - it.first, v0 = in_item % w, v1 = min(w, v0 + (f_end - f));
+      if (f >= it.first + len() * hkv) it = items[++idx];                // items hold at least one tile
+      const int w = len(), in_item = f - it.first, v0 = in_item % w, v1 = min(w, v0 + (f_end - f));
       head = in_item / w;
-      t0 = max(0, v0 - over);                                        // the first `over` places of an item hold no tile
-      t1 = v1 - over;
+      t0 = tile(max(0, v0 - over));                                  // the first `over` places of an item hold no tile
+      t1 = tile(v1 - over);
       f += v1 - v0;
       if (t0 < t1) return true;
     }
     return false;
   }
   // CTAs that work on the current (item, KV head), when it begins in CTA b.
-  __device__ __forceinline__ int parts(int share, int b) const { return (it.first + (head + 1) * (it.n_tiles + over) - 1) / share - b + 1; }
+  __device__ __forceinline__ int parts(int share, int b) const { return (it.first + (head + 1) * len() - weight()) / share - b + 1; }
+  __device__ __forceinline__ int weight() const { return WEIGHED ? it.weight : 1; }
+  __device__ __forceinline__ int len() const { return it.n_tiles * weight() + over; }
+  __device__ __forceinline__ int tile(int at) const { return !WEIGHED ? at : at <= 0 ? 0 : (at + it.weight - 1) / it.weight; }      // the first that begins there or behind
 };
+using PieceWalk = PieceWalkOf<false>;
 
 template <int DH>
 struct ChunkCfg {

@@ -82,6 +82,11 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
     a.ws.rec[blockIdx.x] = SplitRec{0, 0, 0, 0};
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (warp == 2 && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+  }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -90,14 +95,14 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
   __syncthreads();
   tc::tmem_fence_after();
   const uint32_t tmem = *tmem_slot;
-  PieceWalk walk;
+  PieceWalkOf<!SINGLE> walk;
   walk.items = a.items; walk.hkv = hkv; walk.over = plan.over;
   walk.f = (int)min((int64_t)plan.total, (int64_t)blockIdx.x * plan.share);
   walk.f_end = (int)min((int64_t)plan.total, (int64_t)(blockIdx.x + 1) * plan.share);
   if (walk.f < walk.f_end)
     for (int i = threadIdx.x; i < plan.n_items; i += Cfg::THREADS) {
       const int2 x = *reinterpret_cast<const int2*>(a.items + i);      // (first, n_tiles)
-      if (x.x <= walk.f && walk.f < x.x + (x.y + plan.over) * hkv) *s_first = i;
+      if (x.x <= walk.f && walk.f < x.x + (x.y * (SINGLE ? 1 : a.items[i].weight) + plan.over) * hkv) *s_first = i;
     }
   __syncthreads();
   walk.idx = *s_first;
