@@ -164,6 +164,16 @@ def test_tree_attention_with_single_keys_that_decide(contexts, dtype):
         c.check(*c.attend(contexts[dtype]))
 
 
+@pytest.mark.parametrize("hq,hkv,dh", [(14, 2, 128), (8, 2, 64), (64, 1, 128)])
+@pytest.mark.parametrize("seed", range(4))
+def test_tree_attention_of_large_and_small_trees_side_by_side(contexts, hq, hkv, dh, seed):
+    """Work lists whose items cost different amounts, cut anywhere."""
+    rng = np.random.default_rng(seed)
+    nodes, past = rng.integers(1, 120, 5), rng.integers(0, (100, 1000, 3000, 6000)[seed], 5)
+    t = Tree("bf16", hq, hkv, dh, nodes.tolist(), past.tolist(), seed=seed, window=0 if seed % 2 else 500, sinks=0 if seed % 2 else 9)
+    t.check(*t.attend(contexts["bf16"], append=True))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("n", [5, 60])
 def test_a_chain_is_a_chunk(contexts, dtype, n):
