@@ -15,9 +15,10 @@
 // more for 410 MB more, 6.4 TB/s); what a call costs beyond its bytes is filling and draining the rings, 12 units (192 KB) a CTA, and the
 // kernels around.  Steps: one producer for K and V and 8 units 174 (K waits in line behind V); two producers 140; 12 units 121 to 129;
 // keys of the next piece sent before its queries, rows of V zeroed by the issuers instead of the producer 125 where it was 129.  Not
-// kept: pages prefetched to L2 half a batch ahead, 129 where it was 123.
-// 2 trees of 48 nodes on 40000 .. 60001: 133 to 141 us, 123 of this kernel; their 336 rows are an item of two sub-tiles and one of one,
-// which read the keys once each (372 MB instead of 233).
+// kept: pages prefetched to L2 half a batch ahead, 129 where it was 123; tensor maps prefetched, 123.5 where it was 120.7.
+// 2 trees of 48 nodes on 40000 .. 60001: 126 us; their 336 rows are an item of two sub-tiles and one of one, which read the keys once
+// each (372 MB instead of 233).  Side by side a unit of the first took 1.17 us and the two units of a tile of the second 1.57, so they
+// count 3 and 4 in the list that is cut into shares (135 where they counted the same).
 #pragma once
 #include "paged_chunk.cuh"
 #include "paged_tree.cuh"
@@ -81,11 +82,6 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constan
     *abort_flag = 0; *s_first = 0;
     a.ws.rec[blockIdx.x] = SplitRec{0, 0, 0, 0};
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == 2 && lane == 0) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(tmem_slot)), "r"(512u) : "memory");
