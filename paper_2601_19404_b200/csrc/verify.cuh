@@ -89,6 +89,7 @@ template <int C>
 __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
   constexpr int PARTS = C * VF_WARPS, PPL = PARTS / 32;                  // sums of the cluster's warps, per lane
   extern __shared__ __align__(16) uint8_t vf_smem[];
+  fa::cluster_arrive();                           // (waited for before the walk)
   MassPair* h1 = reinterpret_cast<MassPair*>(vf_smem);                   // [bucket][copy]: this CTA's masses
   uint64_t* t1 = reinterpret_cast<uint64_t*>(h1 + VF_B1 * VF_COPIES);     // [bucket]: the cluster's
   MassPair* h2 = h1;                                                     // of later rounds
@@ -234,6 +235,8 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
     for (int i = tid; i < VF_B1; i += VF_THREADS) t1[i] = 0;
     for (int i = tid; i < 2 * VF_B2; i += VF_THREADS) t2[i] = 0;
   }
+  // No CTA writes to another's shared memory before all of the cluster have started.
+  fa::cluster_wait();
   __syncthreads();
   int cur = 0, count = 0, next = -1;
   bool live = rows > 0;

@@ -296,6 +296,29 @@ def test_verification_of_many_sequences(contexts):
         c.check(*c.run(contexts["bf16"]))
 
 
+@pytest.mark.parametrize("n", [6, 200])
+def test_verification_whose_clusters_start_apart(n):
+    """CTAs of a cluster speak to one another once all have started: clusters of sixteen and of eight, some without rows, begin whenever another
+    call's leave room for them."""
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    made = [make_context("bf16", s) for s in streams]
+    cases = [Drafts(20011, [(TREES + CHAINS)[(i + k) % 10] for i in range(n)], seed=20 + k, top_p=0.9) for k in range(2)]
+    inputs, outs = [], []
+    for c in cases:
+        inputs.append(([c.device(c.logits), i32(c.tokens), i32(c.parents), i32(c.off), torch.from_numpy(c.uniform).to(DEV), rpo.Sampler(top_p=0.9)], c.device(c.probs)))
+        outs.append([[torch.full(s, 77, dtype=torch.int32, device=DEV) for s in ((n, c.max_path), (n,), (n,))] + [torch.full((n, c.max_path), 7.0, device=DEV)]
+                     for _ in range(12)])
+    torch.cuda.synchronize()
+    for i in range(12):
+        for ctx, (args, probs), out in zip(made, inputs, outs):
+            ctx.verify_drafts(*args, *out[i], d_draft_probs=probs)
+    torch.cuda.synchronize()
+    for ctx, c, out in zip(made, cases, outs):
+        c.check(*out[0])
+        assert all(torch.equal(x, y) for again in out[1:] for x, y in zip(again, out[0])) and ctx.device_status() == 0
+        ctx.close()
+
+
 def test_verification_on_padded_rows_short_paths_and_without_logprobs(contexts):
     for pad in (1, 4):
         c = Drafts(1003, TREES, seed=4, pad=pad, top_p=0.9, max_path=2)
