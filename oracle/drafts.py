@@ -105,14 +105,15 @@ def verify(logits, tokens, parents, uniform, max_path, temperature=1.0, top_p=1.
         accepted = -1
         for child in [j for j in range(node + 1, len(tokens)) if parents[j] == node] if len(path) < max_path else []:
             x, mass = int(tokens[child]), int(a.sum())
-            if not 0 <= x < vocab:
+            if x < 0:                                    # no draft in this place
                 continue
             if probs is None:
                 d = np.where(np.arange(vocab) == x, mass, 0)
             else:
                 q = np.where(probs[node] > 0, probs[node], 0).astype(np.float64)
                 d = np.minimum(np.floor(q * float(mass)), 4.0e18).astype(np.int64)
-            if (int(d[x]) * u24(uniform[child])) >> 24 < int(a[x]):
+            # (a token beyond the target's vocabulary, of a draft model with a larger one, has no weight)
+            if x < vocab and (int(d[x]) * u24(uniform[child])) >> 24 < int(a[x]):
                 accepted = child
                 break
             if np.maximum(a - d, 0).any():

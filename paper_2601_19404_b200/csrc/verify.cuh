@@ -5,7 +5,8 @@
 //   d_i = floor(q_i A)     with the draft's probabilities q (one product in 64 bits), or A at the child's token and 0 elsewhere
 //   accepted when (d_x u24) >> 24 < a_x,  x the child's token; the walk goes on there
 //   refused: a_i becomes max(a_i - d_i, 0) (unless nothing would be left: then a stays), the next child is tested
-// and where no child is left the next token is the first whose running sum of a exceeds (A u24) >> 24.  All integers but the
+// A child with a negative token is passed over; one beyond the vocabulary has a_x = 0, so it is refused as any other.
+// Where no child is left the next token is the first whose running sum of a exceeds (A u24) >> 24.  All integers but the
 // product, so that decisions do not depend on the order of sums; each emitted token is distributed as the sampler's.
 //
 // Only the nodes on the accepted path are looked at, one after the other.  A cluster of C CTAs holds a node's row as weights
@@ -473,6 +474,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) verify_kernel(VerifyArgs a) {
       const VerifyNode v = child < VF_NODES ? s_node[child] : gather(child);
       const bool in = v.token >= 0 && v.token < V;
       if (!in && tid == 0) atomicOr(a.status, STATUS_BAD_TOKEN);
+      if (v.token < 0) continue;                  // no draft: what is left stays
       uint32_t w = 0;
       if (in) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(w) : "r"(remote(wt + v.token % a.slice, v.token / a.slice)) : "memory");
       auto passes = [&]() { return mul_shift24(q ? __double2ull_rz(verify_scaled(v.q, (double)mass)) : mass, v.u24) < w; };

@@ -393,6 +393,23 @@ def test_verification_at_the_borders(contexts):
     assert ctx.device_status() & 8
 
 
+@pytest.mark.parametrize("given", [True, False])
+@pytest.mark.parametrize("top_p", [1.0, 0.9, 0.3])
+@pytest.mark.parametrize("vocab", [40, 5003])
+def test_verification_of_tokens_outside_the_vocabulary(contexts, given, top_p, vocab):
+    """A negative token is no draft: what is left for others stays as it is.  One beyond the vocabulary is refused as any that the target excludes."""
+    wide = [[-1, 0, 0, 0, 0, 0, 0, 1, 2, 3, 4, 5, 6]] * 12
+    for bad in ([-1], [vocab], [-2 ** 31, 2 ** 31 - 1], [-1, vocab + 7, -5]):
+        for seed in range(4):
+            c = Drafts(vocab, wide + TREES, seed=30 + seed, given=given, top_p=top_p, greedy=seed == 3)
+            rng = np.random.default_rng(seed)
+            for i in range(int(c.off[-1])):
+                if c.parents[i] >= 0 and rng.random() < (0.3, 0.6, 1.0, 0.5)[seed]:
+                    c.tokens[i] = bad[int(rng.integers(len(bad)))]
+            c.check(*c.run(contexts["bf16"]))
+            assert contexts["bf16"].device_status() in ((0, 2) if seed < 2 else (2,))
+
+
 def test_verification_without_drafts_is_the_sampler(contexts):
     """One row per sequence: rpo_sample_rows with the same random numbers gives the same tokens and log-probabilities."""
     ctx, n, vocab = contexts["fp32"], 40, 5003

@@ -59,6 +59,94 @@ def test_emitted_tokens_are_distributed_as_sampled_ones(given):
     assert np.all(np.abs(counts / n - p) <= 5 * np.sqrt(p * (1 - p) / n))
 
 
+STEPS = 2 ** 24
+ROOT, LEVEL2 = [1.0, 0.3, -0.5, 2.0], [[0.0, 1.0, 2.0, -1.0], [2.0, 0.0, 0.1, 0.2], [0.5, 0.5, 3.0, 0.4], [-1.0, 0.0, 1.0, 1.5]]
+
+
+def first_u(holds):
+    """How many of the numbers u24 = 0, 1, ... come before the first for which `holds` (once true, true for all behind)."""
+    lo, hi = 0, STEPS
+    while lo < hi:
+        mid = (lo + hi) // 2
+        lo, hi = (lo, mid) if holds(mid / STEPS) else (mid + 1, hi)
+    return lo
+
+
+def emitted(walk, tokens, vocab):
+    """Distribution of the token that walk(u, u0) emits behind its last accepted node, or at the accepted child: child by child and with
+    the last number u0, in exact counts of the numbers that lead there.  walk(u, u0) -> (accepted child or -1, next token)."""
+    p, left, refused = np.zeros(vocab), 1.0, {}
+    for c, x in tokens.items():
+        n = first_u(lambda u: walk({**refused, c: u}, 0.0)[0] != c)
+        p[x if n else 0] += left * n / STEPS
+        left *= 1 - n / STEPS
+        refused[c] = 1 - 1 / STEPS
+        if n == STEPS:
+            return p
+    at = [0] + [first_u(lambda u0: walk(refused, u0)[1] >= t) for t in range(1, vocab)] + [STEPS]
+    return p + left * np.diff(at) / STEPS
+
+
+@pytest.mark.parametrize("top_p", [1.0, 0.9])
+@pytest.mark.parametrize("kind", ["drawn", "given", "larger", "padded"])
+def test_all_draws_together_are_the_sampler(kind, top_p):
+    """Every draw of two children of the root and of one child of each, every random number, at both levels.
+
+    drawn    children drawn from q independently             larger   from a q of five tokens, of which the target has four
+    given    other children, without probabilities           padded   drawn, with a row without a draft (-1) before and between
+    Drafted probabilities are sums of powers of two that add up to one, so the draws' weights are exact.  An acceptance is then off by at most
+    2^-24 + 2^-29 (numbers u24, whole weights of a mass above 2^30), an entry of the last draw by twice that: below 8 x 2^-24 in all."""
+    vocab = 4
+    q = {"larger": [0.25, 0.25, 0.125, 0.125, 0.25]}.get(kind, [0.5, 0.25, 0.125, 0.125])
+    place = {"padded": [2, 4]}.get(kind, [1, 2])                           # rows of the root's children
+    parents = [-1, 0, 0, 0, 0, 2, 4] if kind == "padded" else [-1, 0, 0, 1, 2]
+    below = [5, 6] if kind == "padded" else [3, 4]
+    pairs = [(x, y, q[x] * q[y]) for x in range(len(q)) for y in range(len(q))] if kind != "given" else [(1, 2, 1.0), (3, 0, 1.0), (0, 3, 1.0), (1, 1, 1.0)]
+
+    def verify(tokens, u, u0, max_path=3):
+        logits = np.zeros((len(parents), vocab), dtype=np.float32)
+        logits[0] = ROOT
+        for row in place:
+            if 0 <= tokens[row] < vocab:
+                logits[row] = LEVEL2[tokens[row]]
+        probs = None if kind == "given" else np.tile(np.array(q[:vocab], dtype=np.float32), (len(parents), 1))
+        uniform = np.zeros(len(parents))
+        uniform[0] = u0
+        for row, x in u.items():
+            uniform[row] = x
+        return drafts.verify(logits, tokens, parents, uniform, max_path, 1.0, top_p, probs=probs)
+
+    def share(row):
+        w = drafts.kept_weights(np.array(row, dtype=np.float32), 1.0, top_p, False)
+        return w / w.sum()
+
+    got = [np.zeros(vocab) for _ in range(len(pairs) if kind == "given" else 1)]
+    for i, (x, y, weight) in enumerate(pairs):
+        tokens = [0] * len(parents)
+        tokens[place[0]], tokens[place[1]] = x, y
+        for row in ([1, 3] if kind == "padded" else []):
+            tokens[row] = -1
+        behind = lambda u, u0: (lambda path, token, _: (path[1] if len(path) > 1 else -1, token))(*verify(tokens, u, u0, 2))
+        got[i % len(got)] += weight * emitted(behind, {row: tokens[row] for row in place}, vocab)
+    for p in got:
+        assert np.all(np.abs(p - share(ROOT)) <= 8 / STEPS)
+    # behind an accepted child
+    for first in (0, 1) if kind != "given" else ():
+        for x in range(vocab):
+            if share(ROOT)[x] == 0:
+                continue
+            got = np.zeros(vocab)
+            for y, weight in enumerate(q):
+                tokens = [0] * len(parents)
+                for row in ([1, 3] if kind == "padded" else []):
+                    tokens[row] = -1
+                tokens[place[first]], tokens[below[first]] = x, y
+                tokens[place[1 - first]] = -1                              # (only the other one can be accepted)
+                behind = lambda u, u0: (lambda path, token, _: (path[2] if len(path) > 2 else -1, token))(*verify(tokens, u, u0))
+                got += weight * emitted(behind, {below[first]: y}, vocab)
+            assert np.all(np.abs(got - share(LEVEL2[x])) <= 8 / STEPS)
+
+
 def test_greedy_eos_and_rows_that_exclude_everything():
     logits = np.full((3, 4), -np.inf, dtype=np.float32)
     logits[0] = [0, 5, 5, 1]
