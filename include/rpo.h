@@ -369,7 +369,8 @@ int rpo_evict_cache(rpo_ctx* ctx, const rpo_paged_kv* kv, const float* d_mass, c
  * A tree is a list of nodes: rows [d_offsets[s], d_offsets[s+1]) of sequence s, node i of it naming its parent
  * among the nodes before it, d_parents[row] < i.  -1: the node follows the last cached token.  -2: there is no
  * node in this row (padding); neither is there where the chain of parents ends in one.  Any other number is
- * taken for -2, and rpo_tree_attention sets bit 3 of the status word. */
+ * taken for -2, and rpo_tree_attention sets bit 3 of the status word; so it does for rows whose slot would be negative (fewer
+ * tokens than nodes). */
 
 /* Attention of a tree of drafted tokens per sequence over the paged cache.  Node i of n lies in slot len - n + i
  * and sits at position p = len - n + depth (0 for a child of the last cached token).  It sees the len - n cached

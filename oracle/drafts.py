@@ -1,7 +1,7 @@
 """Drafted tokens and shared pages on a caller-owned cache, by definition, in plain numpy and Python integers.
 
 Trees: node i of a sequence's n nodes lies in slot len - n + i, its parent is a node before it, or -1 (the last cached
-token); -2, or a chain of parents that ends in one: no node.  Verification: the sampler's integer weights.  Pages: reference
+token); -2, or a chain of parents that ends in one: no node, nor is there one where the slot would be negative.  Verification: the sampler's integer weights.  Pages: reference
 counts and a stack of free pages; which page goes where is decided by the order of forks or sequences alone.
 """
 import numpy as np
@@ -12,18 +12,19 @@ PAGE = paged.PAGE
 
 
 # ---- trees ---------------------------------------------------------------------------------------------------------
-def chains(parents):
-    """Every node's ancestors from itself up (None: no node)."""
+def chains(parents, first=0):
+    """Every node's ancestors from itself up (None: no node, as before the first-th)."""
     got = []
     for i, p in enumerate(parents):
-        up = None if p < -1 or p >= i else [] if p == -1 else got[p]
+        up = None if p < -1 or p >= i or i < first else [] if p == -1 else got[p]
         got.append(None if up is None else [i] + up)
     return got
 
 
 def visible(parents, n_keys, window=0, sinks=0):
     """[node][key] of a tree in the last slots of n_keys."""
-    past, up = n_keys - len(parents), chains(parents)
+    past = n_keys - len(parents)
+    up = chains(parents, -past)
     seen = np.zeros((len(parents), n_keys), dtype=bool)
     for i, chain in enumerate(up):
         if chain is None:
@@ -66,7 +67,7 @@ def append(cache, new, table, lens, offsets, parents):
     """The nodes' rows into their slots (in place)."""
     for s, n in enumerate(lens):
         a, b = offsets[s], offsets[s + 1]
-        for i, chain in enumerate(chains(parents[a:b])):
+        for i, chain in enumerate(chains(parents[a:b], b - a - n)):
             if chain is not None:
                 p = n - (b - a) + i
                 cache[:, table[s][p // PAGE], p % PAGE] = new[a + i]

@@ -66,6 +66,7 @@ __device__ __forceinline__ void f32_scores(const float* sq, const float* sk, int
 template <int DH, int BM, bool TREE>
 __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F32Args a) {
   using Cfg = F32Cfg<DH, BM>;
+  constexpr int NO_NODE = -(1 << 30);                      // below every position (those of a tree longer than its sequence may be negative)
   constexpr int BN = Cfg::BN, TM = BM / 16, KPT = BN / 16, DG = DH / 64, QS = Cfg::QS, PS = Cfg::PS, CPR = DH / 4, LD = BN * CPR / 256;
   extern __shared__ __align__(16) float f32_smem[];
   float *sq = f32_smem, *sk = sq + BM * QS, *sv = sk + BN * QS, *sp = sv + BN * DH;
@@ -133,7 +134,7 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
       prow[i] = min(p0 + (r0 + i) / rep, p1);
       if (TREE) {
         node[i] = nodes + (prow[i] - walk.it.key0);
-        prow[i] = node[i]->depth < 0 ? -1 : walk.it.key0 + node[i]->depth;
+        prow[i] = node[i]->depth < 0 ? NO_NODE : walk.it.key0 + node[i]->depth;
       }
 #pragma unroll
       for (int g = 0; g < DG; ++g) o[i][g][0] = o[i][g][1] = o[i][g][2] = o[i][g][3] = 0.f;
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
           const int key = key0 + tx + 16 * j;
           if (TREE && !whole && key >= walk.it.key0) {
             const int slot = key - walk.it.key0;
-            if (prow[i] < 0 || first_range || slot >= TREE_MAX_NODES || !((node[i]->seen[slot >> 5] >> (slot & 31)) & 1)) s[i][j] = -INFINITY;
+            if (prow[i] == NO_NODE || first_range || slot >= TREE_MAX_NODES || !((node[i]->seen[slot >> 5] >> (slot & 31)) & 1)) s[i][j] = -INFINITY;
           } else if (!whole && (!chunk_visible(a.c, key, prow[i]) || (first_range && key >= a.c.sinks))) s[i][j] = -INFINITY;
           mx = fmaxf(mx, s[i][j]);
         }
@@ -212,7 +213,7 @@ __global__ void __launch_bounds__(256, F32Cfg<DH, BM>::CTAS) paged_f32_kernel(F3
       for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
       const int r = r0 + i;
       if (r >= R) continue;
-      if (TREE && prow[i] < 0) {                             // no node: whatever the tiles without masks gave
+      if (TREE && prow[i] == NO_NODE) {                       // no node: whatever the tiles without masks gave
         m[i] = -INFINITY; l[i] = 0.f;
 #pragma unroll
         for (int g = 0; g < DG; ++g) o[i][g][0] = o[i][g][1] = o[i][g][2] = o[i][g][3] = 0.f;

@@ -200,6 +200,33 @@ def test_trees_without_any_node_and_bad_parents(contexts, dtype):
         assert torch.isfinite(got.float()).all() and torch.isneginf(lse[rows + 1:]).all() and (got[rows + 1:] == 0).all() and torch.isfinite(lse[rows]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hq,hkv,dh", [(4, 2, 64), (12, 2, 128)])
+@pytest.mark.parametrize("mask", [(0, 0), (3, 0), (4, 9)])
+@pytest.mark.parametrize("append", [False, True])
+def test_trees_longer_than_their_sequences(contexts, dtype, hq, hkv, dh, mask, append):
+    """Fewer tokens than nodes: nodes whose slots would be negative are none, the others see one another; bit 3."""
+    for nodes, lens in (([6, 8, 5, 3, 7], [5, 1, 0, 3, 4]), ([40, 20, 33, 90], [39, 3, 0, 50])):
+        c = Tree(dtype, hq, hkv, dh, nodes, [0] * len(nodes), seed=dh, extra_rows=1, window=mask[0], sinks=mask[1],
+                 parents=[[-1 if i % 7 == 0 or i == 4 else i - 1 - (i % 3 == 2) for i in range(n)] for n in nodes])
+        k, v = c.k.clone(), c.v.clone()
+        for s, n in enumerate(lens):                                     # (also what lies behind the sequences' new ends)
+            for j in range(n, c.lens[s]):
+                k[:, c.table[s, j // 16], j % 16] = v[:, c.table[s, j // 16], j % 16] = float("nan")
+        c.k.copy_(k), c.v.copy_(v)
+        c.lens = lens
+        c.kv.d_lens.copy_(i32(lens))
+        if append:
+            k, v = f64(c.k), f64(c.v)
+            for cache, new in ((k, c.k_new), (v, c.v_new)):
+                drafts.append(cache, f64(new), c.table, c.lens, c.off, c.parents)
+        out, lse = c.attend(contexts[dtype], append=append)
+        assert contexts[dtype].device_status() == 8
+        if append:
+            assert np.array_equal(f64(c.k), k, equal_nan=True) and np.array_equal(f64(c.v), v, equal_nan=True)
+        c.check(out, lse)
+
+
 def test_tree_attention_refusals(contexts):
     c, ctx = Tree("bf16", 4, 2, 64, [3], [20]), contexts["bf16"]
     out = torch.empty_like(c.q.contiguous())
