@@ -461,7 +461,8 @@ int rpo_fork_pages(rpo_ctx* ctx, const rpo_page_pool* pool, const rpo_paged_kv* 
 /* Every sequence holds the pages of d_target_lens[s] tokens afterwards, more or fewer than before (0: none).  Its first
  * min(d_lens[s], d_target_lens[s]) tokens stay; pages that hold tokens behind those are its own: one that others hold too
  * is replaced, the tokens that stay in it copied in all layers.  Neither d_lens nor the caches' lengths are written.
- * d_lens beyond what is held, or numbers out of range, are clamped and set bit 3.  Errors as in rpo_fork_pages. */
+ * Numbers out of range, and tokens that would stay but are not held (min(d_lens[s], d_target_lens[s]) beyond the pages of s), are
+ * clamped and set bit 3; a sequence that gave its pages back may keep its length in d_lens.  Errors as in rpo_fork_pages. */
 int rpo_reserve_pages(rpo_ctx* ctx, const rpo_page_pool* pool, const rpo_paged_kv* h_layers, int32_t n_layers,
                       const int32_t* d_lens, const int32_t* d_target_lens);
 

@@ -608,6 +608,21 @@ def test_bad_arguments_of_page_calls(contexts):
         assert ctx.device_status() & 8
 
 
+def test_lengths_beyond_what_is_held(contexts):
+    """Bit 3 where tokens that would stay are not there; not for a length that the target cuts to what is held."""
+    ctx = contexts["bf16"]
+    for held, lens, target, bit in ((16, 40, 40, 8), (16, 40, 17, 8), (16, 17, 80, 8), (16, 40, 16, 0), (16, 40, 5, 0), (16, 40, 0, 0), (0, 40, 0, 0), (0, 1, 1, 8), (16, 16, 80, 0),
+                                    (80, 81, 0, 8), (80, -1, 0, 8), (80, 80, 81, 8), (80, 80, -1, 8)):
+        c = Cache("bf16", 1, 1, 64, 20, 3, 5)
+        ctx.reserve_pages(c.pool, c.layers, i32([0] * 3), i32([20, held, 33]))
+        c.twin.reserve([0] * 3, [20, held, 33])
+        assert ctx.device_status() == 0
+        ctx.reserve_pages(c.pool, c.layers, i32([20, lens, 33]), i32([40, target, 20]))
+        c.twin.reserve([20, lens, 33], [40, target, 20])
+        c.same()
+        assert ctx.device_status() == bit, (held, lens, target)
+
+
 @pytest.mark.parametrize("dtype,layers,hkv,dh", [("bf16", 3, 2, 128), ("fp32", 2, 3, 64), ("bf16", 1, 1, 64), ("fp32", 1, 2, 128)])
 def test_commit(contexts, dtype, layers, hkv, dh):
     ctx, rng = contexts[dtype], np.random.default_rng(dh)
