@@ -128,11 +128,11 @@ struct ItemBits {
 };
 
 // f(slot, page) for the slots [lo, hi) of a table row, 32 PG_ROWS at a time: slot and page of each of a lane's PG_ROWS; page -1: no
-// slot, or none of the pool.  MARKS: entries may carry PG_MARK.
+// slot, or none of the pool.  Entries of slots below `marked` may carry PG_MARK; elsewhere a number with that bit is none of the pool.
 constexpr int PG_ROWS = 4;
 
-template <bool MARKS = false, typename F>
-__device__ __forceinline__ void page_slots(const PagePoolArgs& p, int s, int lo, int hi, F f) {
+template <typename F>
+__device__ __forceinline__ void page_slots(const PagePoolArgs& p, int s, int lo, int hi, F f, int marked = 0) {
   const int lane = threadIdx.x & 31;
   int32_t* row = p.table + (int64_t)s * p.stride;
   for (int j = lo; j < hi; j += 32 * PG_ROWS) {
@@ -140,7 +140,7 @@ __device__ __forceinline__ void page_slots(const PagePoolArgs& p, int s, int lo,
 #pragma unroll
     for (int k = 0; k < PG_ROWS; ++k) { slot[k] = j + 32 * k + lane; page[k] = slot[k] < hi ? row[slot[k]] : 0; }
 #pragma unroll
-    for (int k = 0; k < PG_ROWS; ++k) if (slot[k] >= hi || !p.in_pool(MARKS ? page[k] & ~PG_MARK : page[k])) page[k] = -1;
+    for (int k = 0; k < PG_ROWS; ++k) if (slot[k] >= hi || !p.in_pool(slot[k] < marked ? page[k] & ~PG_MARK : page[k])) page[k] = -1;
     f(slot, page);
   }
 }
@@ -398,30 +398,30 @@ __global__ void __launch_bounds__(PG_THREADS) reserve_pages_kernel(ReserveArgs a
                [&](int s, auto f) {
                  if (!ok.get((s - warp) / warps)) return;
                  const ReserveSeq x = seq(s);
-                 page_slots<true>(p, s, x.len / KV_BLOCK, x.held, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+                 page_slots(p, s, x.len / KV_BLOCK, x.held, [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
                    int old[PG_ROWS];
 #pragma unroll
                    for (int k = 0; k < PG_ROWS; ++k) {
                      old[k] = -1;
-                     if (page[k] >= 0 && (page[k] & PG_MARK)) {
+                     if (page[k] >= 0 && (page[k] & PG_MARK)) {        // (below want alone)
                        old[k] = p.count_of(page[k] & ~PG_MARK) - PG_OLD;
                        if (old[k] < 0 || old[k] >= p.n_blocks) old[k] = -1;
                      } else if (slot[k] >= x.want) old[k] = page[k];
                    }
                    f(slot, old);
-                 });
+                 }, x.want);
                },
                [&](int s) {
                  if (!ok.get((s - warp) / warps)) return;
                  const ReserveSeq x = seq(s);
-                 page_slots<true>(p, s, x.len / KV_BLOCK, min(x.held, x.want), [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
+                 page_slots(p, s, x.len / KV_BLOCK, min(x.held, x.want), [&](const int (&slot)[PG_ROWS], const int (&page)[PG_ROWS]) {
 #pragma unroll
                    for (int k = 0; k < PG_ROWS; ++k) {
                      if (page[k] < 0 || !(page[k] & PG_MARK)) continue;
                      p.table[(int64_t)s * p.stride + slot[k]] = page[k] & ~PG_MARK;
                      p.refs[page[k] & ~PG_MARK] = 1;
                    }
-                 });
+                 }, x.want);
                  __syncwarp();
                  if (lane == 0) p.held[s] = x.want;
                });

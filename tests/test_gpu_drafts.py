@@ -623,6 +623,54 @@ def test_lengths_beyond_what_is_held(contexts):
         assert ctx.device_status() == bit, (held, lens, target)
 
 
+@pytest.mark.parametrize("entry", [-1, 30, 2 ** 31 - 1, -2 ** 31, 2 ** 30 + 3])
+def test_a_bad_entry_concerns_its_sequence_alone(contexts, entry):
+    """One number of a table, or of the stack, that names no page: what all others hold, and where pages go, is as without it."""
+    ctx, n = contexts["bf16"], 4
+
+    def made():
+        c = Cache("bf16", 1, 1, 64, 30, n, 5)
+        lens = [40, 80, 0, 20]
+        ctx.reserve_pages(c.pool, c.layers, i32([0] * n), i32(lens))
+        c.twin.reserve([0] * n, lens)
+        c.same()
+        return c
+
+    calls = [("fork", [1, 1], [2, 0], [33, 20]), ("fork", [1], [0], [64]), ("reserve", [40, 80, 0, 20], [0, 20, 50, 40]), ("reserve", [5, 80, 0, 20], [40, 81 - 1, 16, 0])]
+    for what, *args in calls:
+        run = lambda c: (ctx.fork_pages if what == "fork" else ctx.reserve_pages)(c.pool, c.layers, *[i32(x) for x in args])
+        twin = lambda c: getattr(c.twin, what)(*args)
+        # the second page of sequence 0
+        c = made()
+        lost = c.twin.table[0][1]
+        c.pool.d_block_table[0, 1] = entry
+        run(c), twin(c)
+        given_up = c.twin.table[0][1] != lost or c.twin.held[0] < 2
+        assert ctx.device_status() == (4 if given_up or what == "reserve" else 0), what
+        assert c.pool.d_held.tolist() == c.twin.held and c.pool.d_block_table.tolist()[1:] == c.twin.table[1:]
+        refs, free = list(c.twin.refs), c.twin.free[:c.twin.n_free]
+        if c.twin.refs[lost] == 0:                                       # nobody can say any more that it was held
+            refs[lost] = 1
+            free.remove(lost)
+        assert c.pool.d_refs.tolist() == refs and c.pool.d_free.tolist()[:int(c.pool.d_n_free)] == free
+        # the second page that a call takes
+        c = made()
+        lost = c.twin.free[c.twin.n_free - 2]
+        c.pool.d_free[c.twin.n_free - 2] = entry
+        run(c), twin(c)
+        taken = c.twin.refs[lost] > 0
+        assert ctx.device_status() == (4 if taken else 0)
+        got, want = c.pool.d_block_table.tolist(), c.twin.table
+        for s in range(n):
+            for j in range(5):
+                assert got[s][j] == (-1 if want[s][j] == lost and j < c.twin.held[s] else want[s][j]), (what, s, j)
+        refs = list(c.twin.refs)
+        refs[lost] = 0
+        assert c.pool.d_held.tolist() == c.twin.held and c.pool.d_refs.tolist() == refs and int(c.pool.d_n_free) == c.twin.n_free
+        if taken:
+            assert c.pool.d_free.tolist()[:c.twin.n_free] == c.twin.free[:c.twin.n_free]
+
+
 @pytest.mark.parametrize("dtype,layers,hkv,dh", [("bf16", 3, 2, 128), ("fp32", 2, 3, 64), ("bf16", 1, 1, 64), ("fp32", 1, 2, 128)])
 def test_commit(contexts, dtype, layers, hkv, dh):
     ctx, rng = contexts[dtype], np.random.default_rng(dh)
