@@ -201,6 +201,29 @@ def test_trees_without_any_node_and_bad_parents(contexts, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads", [(2, 2, 64), (3, 3, 128), (8, 4, 64), (4, 2, 128), (6, 2, 64), (16, 4, 128), (5, 1, 128)])
+@pytest.mark.parametrize("mask", [(0, 0), (2, 0), (7, 40), (64, 3)])
+@pytest.mark.parametrize("append", [False, True])
+def test_trees_of_at_most_sixteen_packed_rows(contexts, dtype, heads, mask, append):
+    """Nodes x query heads of a KV head within one tile of sixteen rows: chains, stars, siblings at every level, holes in the middle, random ones."""
+    most = 16 // (heads[0] // heads[1])
+    shapes = [list(range(-1, most - 1)), [-1] + [0] * (most - 1), [(i - 1) // 2 if i else -1 for i in range(most)], [-1] * most,
+              [-2 if i == most // 2 else i - 1 for i in range(most)], [-1, 0, 0, 1, 1, 2, 2, 3, -2, 5, 8, 4, 11, 12, -1, 14][:most],
+              [-2] + [max(i - 2, -1) for i in range(1, most)], [-1]]
+    trees = shapes + [random_tree(most - k % 2, np.random.default_rng(k), 0.15 * (k % 3)) for k in range(8)] + [[]]
+    past = [0, 1, 15, 16, 17, 31, 100, 0, 300, 2000, 7, 33, 48, 250, 640, 5, 9]
+    c = Tree(dtype, *heads, [len(t) for t in trees], past, seed=sum(heads) + mask[0], extra_rows=1, window=mask[0], sinks=mask[1], parents=trees)
+    k, v = f64(c.k), f64(c.v)
+    if append:
+        for cache, new in ((k, c.k_new), (v, c.v_new)):
+            drafts.append(cache, f64(new), c.table, c.lens, c.off, c.parents)
+    out, lse = c.attend(contexts[dtype], append=append)
+    assert np.array_equal(f64(c.k), k, equal_nan=True) and np.array_equal(f64(c.v), v, equal_nan=True)
+    c.check(out, lse)
+    assert contexts[dtype].device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("hq,hkv,dh", [(4, 2, 64), (12, 2, 128)])
 @pytest.mark.parametrize("mask", [(0, 0), (3, 0), (4, 9)])
 @pytest.mark.parametrize("append", [False, True])
