@@ -369,6 +369,40 @@ def test_verification_whose_clusters_start_apart(n):
         ctx.close()
 
 
+@pytest.mark.parametrize("given", [True, False])
+@pytest.mark.parametrize("top_p", [1.0, 0.9])
+def test_verification_of_many_nodes(contexts, given, top_p):
+    """Sequences of more than 128 rows: random trees, a root whose children, equal tokens among them, lie on both sides of row 128 (and are
+    all refused before some row), and accepted chains that cross it."""
+    ctx = contexts["bf16"]
+    trees = [random_tree(n, np.random.default_rng(n)) for n in (129, 128, 256, 300)] + [[-1] + [0] * 255, [-1] + [0] * 128, list(range(-1, 199)), [-1, 0] * 100]
+    for seed in range(3):
+        c = Drafts(97, trees, seed=40 + seed, given=given, top_p=top_p, spread=1.0)
+        c.check(*c.run(ctx))
+        for first in (100, 128, 129, 200):                               # refused with the largest number, as a rule, before that row
+            for s in (4, 5):
+                a, b = int(c.off[s]), int(c.off[s + 1])
+                c.uniform[a + 1:min(a + first, b)] = 1.0 - 2.0 ** -24
+                c.uniform[a + first:b] = 0.0
+            c.check(*c.run(ctx))
+        for u0 in (0.0, 0.6, 1.0 - 2.0 ** -24):                          # all refused: what is drawn then
+            c.uniform[:] = 1.0 - 2.0 ** -24
+            c.uniform[c.off[:-1]] = u0
+            c.check(*c.run(ctx))
+        c.cfg["greedy"] = True
+        best = c.logits.argmax(1)
+        for s in range(len(trees)):                                      # the target's own choice, but for one node behind row 128
+            for i, p in enumerate(trees[s]):
+                if p >= 0 and i != 150 + 10 * seed:
+                    c.tokens[c.off[s] + i] = best[c.off[s] + p]
+        got = c.run(ctx)
+        c.check(*got)
+        assert int(got[1][6]) == 150 + 10 * seed
+        c.cfg["eos_id"] = int(c.tokens[c.off[6] + 140])
+        c.check(*c.run(ctx))
+    assert ctx.device_status() == 0
+
+
 def test_verification_on_padded_rows_short_paths_and_without_logprobs(contexts):
     for pad in (1, 4):
         c = Drafts(1003, TREES, seed=4, pad=pad, top_p=0.9, max_path=2)
