@@ -757,6 +757,31 @@ def test_commit(contexts, dtype, layers, hkv, dh):
         assert want[7:] == lens[7:]
 
 
+@pytest.mark.parametrize("dtype,layers,hkv,dh", [("fp32", 2, 1, 128), ("bf16", 3, 2, 128), ("fp32", 1, 2, 64), ("bf16", 2, 1, 64)])
+def test_commit_of_long_paths(contexts, dtype, layers, hkv, dh):
+    """Paths of many batches of rows (64 to 256, by type and head size; places are looked up 256 at a time): nearly every row moves by a few slots,
+    onto rows that others come from."""
+    ctx, rng = contexts[dtype], np.random.default_rng(dh)
+    nodes, past = [300, 400, 129, 700, 65, 257, 0], [5, 37, 100, 1, 16, 0, 9]
+    n = len(nodes)
+    lens = [a + b for a, b in zip(nodes, past)]
+    off = np.concatenate([[0], np.cumsum(nodes)])
+    for drops in (1, 5, 60):
+        c = Cache(dtype, layers, hkv, dh, sum(-(-x // 16) for x in lens) + 4, n, 48, seed=drops)
+        ctx.reserve_pages(c.pool, c.layers, i32([0] * n), i32(lens))
+        c.twin.reserve([0] * n, lens)
+        path, n_path = np.full((n, 700), -1, dtype=np.int32), np.zeros(n, dtype=np.int32)
+        for s in range(n):
+            lost = {0} | set(rng.integers(0, max(nodes[s], 1), drops).tolist()) if drops != 5 else set(rng.integers(0, max(nodes[s], 1), drops).tolist())
+            keep = [i for i in range(nodes[s]) if i not in lost]
+            path[s, :len(keep)], n_path[s] = keep, len(keep)
+        c.lens.copy_(i32(lens))
+        before = f64(c.kv)
+        want = drafts.commit(before, c.twin.table, lens, off, path, n_path)
+        ctx.commit_path(c.layers, i32(off), i32(path), i32(n_path), c.lens)
+        assert c.lens.tolist() == want and np.array_equal(f64(c.kv), before) and ctx.device_status() == 0
+
+
 def test_commit_with_bad_tables(contexts):
     ctx = contexts["bf16"]
     c = Cache("bf16", 2, 1, 64, 10, 2, 3)
