@@ -241,7 +241,7 @@ def _head_rows(t, name, dtype, heads, dh, device, n_rows=None):
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the cache on {device}")
     stride = t.stride()
-    if stride[2] != 1 or (heads > 1 and stride[1] != dh):
+    if shape[0] and (stride[2] != 1 or (heads > 1 and stride[1] != dh)):      # (strides of nothing may be anything)
         raise ValueError(f"{name}: the heads of a row must be contiguous")
     return stride[0] if shape[0] > 1 else heads * dh
 
@@ -454,7 +454,7 @@ class Context:
             if t is None:
                 strides.append(0)
                 continue
-            if t.dim() != 2 or t.dtype is not _dtype("float32") or t.shape != d_logits.shape or t.device != dev or (t.shape[1] > 1 and t.stride(1) != 1):
+            if t.dim() != 2 or t.dtype is not _dtype("float32") or t.shape != d_logits.shape or t.device != dev or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
                 raise ValueError(f"{name} must be float32 [rows, vocab] on {dev} with contiguous rows, got {t.dtype} {tuple(t.shape)}")
             strides.append(t.stride(0) if t.shape[0] > 1 else t.shape[1])
         n, vocab = d_logits.shape

@@ -2,6 +2,7 @@
 refusals that need no device."""
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
@@ -52,6 +53,19 @@ def test_verification_checks_its_arguments():
               dict(d_offsets=torch.zeros(0, dtype=I32)), dict(d_n_path_out=one[:1]), dict(d_next_out=one.long()), dict(d_logprobs_out=logp[:, :3])])
     with pytest.raises(rpo.RpoError):
         ctx.verify_drafts(**{**good, "d_logits": torch.zeros(rows, 12)[:, :vocab], "d_draft_probs": None, "d_logprobs_out": None})      # strided rows pass
+
+
+def test_calls_without_rows_pass_whatever_their_strides():
+    """Tensors without elements may have any strides: those that come from numpy have zeros."""
+    ctx, n, vocab = _ctx(0), 2, 10
+    (_, _, layers), none = _cache(torch.float32, n=n), torch.from_numpy(np.zeros((0, vocab), dtype=np.float32))
+    rows = torch.from_numpy(np.zeros((0, 4, 64), dtype=np.float32))
+    assert none.stride() == (0, 0) and rows.stride() == (0, 0, 0)
+    ints, off, one = torch.zeros(0, dtype=I32), torch.zeros(n + 1, dtype=I32), torch.zeros(n, dtype=I32)
+    with pytest.raises(rpo.RpoError):                                       # through the binding, refused: NULL context
+        ctx.verify_drafts(none, ints, ints, off, torch.zeros(0), rpo.Sampler(), torch.zeros(n, 4, dtype=I32), one, one, d_draft_probs=none)
+    with pytest.raises(rpo.RpoError):
+        ctx.tree_attention(rows, layers[0], off, ints, 3, torch.zeros(0, 4, 64))
 
 
 def test_layers_and_pools_check_their_tensors():
