@@ -412,7 +412,7 @@ int rpo_tree_attention(rpo_ctx* ctx, const rpo_paged_kv* kv, int32_t n_rows, int
  * A child whose token is negative is no draft: it is passed over, a and A stay.  A child whose token is vocab or more (drawn from a draft
  * model with a larger vocabulary, of whose probabilities the first vocab are given) has a_x = 0 and is refused as any other.  Both set
  * bit 1 of the status word, bad offsets set bit 3.
- * Errors: RPO_ERR_INVALID_ARG, RPO_ERR_LIMIT (vocab >= 2^18). */
+ * Errors: RPO_ERR_INVALID_ARG, RPO_ERR_LIMIT (vocab >= 2^18, n_seqs > 2^24). */
 int rpo_verify_drafts(rpo_ctx* ctx, int32_t n_seqs, int32_t n_rows, int32_t vocab, const float* d_logits,
                       int64_t logits_stride, const float* d_draft_probs, int64_t probs_stride, const int32_t* d_tokens,
                       const int32_t* d_parents, const int32_t* d_offsets, const float* d_uniform,

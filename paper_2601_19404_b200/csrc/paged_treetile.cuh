@@ -6,19 +6,19 @@
 // for one sub-tile of rows as a rule, and one sub-tile alone is bound by the chain S -> softmax -> P V of its 64-key units (2200
 // clocks a unit, 63 % of a copy's rate).  Here both softmax warpgroups and both issuers serve such an item: they take
 // alternate units, each with a sum and an output of its own; at the end of a piece warpgroup 0 joins both outputs, which lie in the
-// same lanes of tensor memory.  Items of two
-// sub-tiles work as there, one for each warpgroup.  K and V come in rings of 64-key units, and both issuers follow every unit's
-// barriers, also those of units that are the other's.
+// same lanes of tensor memory.  Items of two sub-tiles work as there, one for each warpgroup.  K and V come in rings of 64-key units,
+// and both issuers follow every unit's barriers, also those of units that are the other's.
 //
-// 64 trees of 16 nodes on 1024 .. 6144 tokens, 28 on 4 heads of 128: 121 to 125 us with the list of items before (7) and the join behind
-// (8), in paged_chunk.cuh's way 136.  Long runs go at a copy's rate (2 trees of 18 nodes on three times 40000 .. 60001 tokens: 64 us
-// more for 410 MB more, 6.4 TB/s); what a call costs beyond its bytes is filling and draining the rings, 12 units (192 KB) a CTA, and the
-// kernels around.  Steps: one producer for K and V and 8 units 174 (K waits in line behind V); two producers 140; 12 units 121 to 129;
-// keys of the next piece sent before its queries, rows of V zeroed by the issuers instead of the producer 125 where it was 129.  Not
-// kept: pages prefetched to L2 half a batch ahead, 129 where it was 123; tensor maps prefetched, 123.5 where it was 120.7.
-// 2 trees of 48 nodes on 40000 .. 60001: 126 us; their 336 rows are an item of two sub-tiles and one of one, which read the keys once
-// each (372 MB instead of 233).  Side by side a unit of the first took 1.17 us and the two units of a tile of the second 1.57, so they
-// count 3 and 4 in the list that is cut into shares (135 where they counted the same).
+// 64 trees of 16 nodes on 1024 .. 6144 tokens, 28 on 4 heads of 128: 121 to 134 us on different cards, with the list of items before
+// (7) and the join behind (8); in paged_chunk.cuh's way 136 where it was 123.  Long runs go at a copy's rate (2 trees of 18 nodes on
+// three times 40000 .. 60001 tokens: 64 us more for 410 MB more, 6.4 TB/s); what a call costs beyond its bytes is filling and draining
+// the rings, 12 units (192 KB) a CTA, and the kernels around.  Steps: one producer for K and V and 8 units 174 (K waits in line behind
+// V); two producers 140; 12 units 121 to 129; keys of the next piece sent before its queries, rows of V zeroed by the issuers instead of
+// the producer 125 where it was 129.  Not kept: pages prefetched to L2 half a batch ahead, 129 where it was 123; tensor maps
+// prefetched, 123.5 where it was 120.7.
+// 2 trees of 48 nodes on 40000 .. 60001: 126 to 141 us; their 336 rows are an item of two sub-tiles and one of one, which read the keys
+// once each (372 MB instead of 233).  Side by side a unit of the first took 1.17 us and the two units of a tile of the second 1.57, so
+// they count 3 and 4 in the list that is cut into shares (126, and 135 where they counted the same, on one card).
 #pragma once
 #include "paged_chunk.cuh"
 #include "paged_tree.cuh"

@@ -5,7 +5,7 @@
 // once each way).  Fork and reserve change tables, counts and the stack of free pages in one cluster, whose barriers order the
 // phases, and leave a list of pages to copy; a second kernel copies those in all layers, a CTA per page and group of planes (a
 // plane is K or V of one KV head of one layer) with eight 16-byte pieces per thread in flight.  128 forks of 28 layers of 4 heads of
-// 128: 42 us, half of it tables and counts.  Which page goes where is a matter of the order of forks or sequences alone, never of timing:
+// 128: 41 to 45 us, half of it tables and counts.  Which page goes where is a matter of the order of forks or sequences alone, never of timing:
 //   taken    the k-th page that the call needs, in order of (fork or sequence, page of it), is free[n_free - 1 - k]
 //   released a page whose count falls to 0 is pushed once, at the place of the first (fork or sequence, page) that drops it
 #pragma once

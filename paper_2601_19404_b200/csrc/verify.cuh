@@ -18,10 +18,10 @@
 //
 // Bound by instructions and barriers, not by HBM: a row of 152064 costs a cluster 13 000 clocks without the nucleus (2900 fetch, 3700
 // exponentials, two exchanges of 2000, the test 1000), the nucleus 15 000, the difference with q 4000 to 6000.  128 chains of 9 with
-// probabilities, nucleus 0.95, 2.96 rows looked at on average, nine at most: 247 us (floor 41 us for their bytes).  Steps: scalar loads
+// probabilities, nucleus 0.95, 2.96 rows looked at on average, nine at most: 240 to 262 us (floor 41 us for their bytes).  Steps: scalar loads
 // and weights 764; loads in flight, sums pushed through the cluster 662; two CTAs per SM 398; columns for the histograms 369; accepted
 // drafts without the nucleus 275; packed arithmetic 247.  256 threads rather than 512: every warp repeats the decisions.
-// 4 trees of 24 without probabilities, five levels at most: 32 us.
+// 4 trees of 24 without probabilities, five levels at most: 22 to 37 us.
 #pragma once
 #include <type_traits>
 
